@@ -52,7 +52,8 @@ typedef enum {
                                       kernel gave up a bounded wait (see
                                       fibattn_check_status)                        */
     FIBATTN_ERR_RANGE = 5          /* an operand left the range of the library's
-                                      16-bit rotated rows (fibattn_check_status)   */
+                                      16-bit rotated rows, or a target that of the
+                                      vocabulary (fibattn_check_status)            */
 } fibattn_status;
 
 typedef enum { FIBATTN_F32 = 0, FIBATTN_BF16 = 1 } fibattn_dtype;
@@ -166,7 +167,7 @@ size_t fibattn_residual_bytes(int B, int H, int T, int D, int W, int K, int dtyp
 const char* fibattn_last_error(void);
 
 /* ---------------------------------------------------------------------------
- * Device status (no counterpart in the paper).  Kernels report two conditions
+ * Device status (no counterpart in the paper).  Kernels report conditions
  * that no argument check can catch before launch into a per-device status
  * word, without stopping:
  *   bit 0 -- a kernel gave up waiting for one of its own shared-memory staging
@@ -176,10 +177,12 @@ const char* fibattn_last_error(void);
  *            the bf16 path keeps the RoPE-rotated keys, and the rotated
  *            queries times the score scale, in fp16 (for score precision),
  *            which cannot hold it.
+ *   bit 2 -- fibattn_linear_xent_fwd or _bwd met a target outside [0, V) that
+ *            is not ignore_index (that row's loss is NaN).
  * fibattn_check_status synchronises `stream`, reads the calling thread's
  * current device's word into *flags (may be NULL) and clears it.  Returns
- * FIBATTN_ERR_INTERNAL if bit 0 was set, else FIBATTN_ERR_RANGE if bit 1 was
- * set, else FIBATTN_OK.  Compute calls never synchronise to look at it.
+ * FIBATTN_ERR_INTERNAL if bit 0 was set, else FIBATTN_ERR_RANGE if bit 1 or 2
+ * was set, else FIBATTN_OK.  Compute calls never synchronise to look at it.
  * ------------------------------------------------------------------------- */
 int fibattn_check_status(void* stream, unsigned* flags);
 
@@ -272,6 +275,65 @@ int fibattn_staging_layout(int kind, int T, int W, float alpha, const float* off
 int fibattn_fwd_noalloc(const void* q, const void* k, const void* v, void* out, float* lse,
                         int B, int H, int T, int D, int W, float alpha, const float* offsets, int K,
                         int dtype, const fibattn_opts* opts, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * What follows the layers in a training step (Section 3, "Model and training":
+ * a tied embedding over 32768 tokens, gradients clipped to norm 1).
+ *
+ * Cross entropy of a linear head, in pieces of the vocabulary, logits not kept:
+ *   s[n][v] = sum_d x[n][d] w[v][d],  lse[n] = log sum_v exp s[n][v],
+ *   loss[n] = lse[n] - s[n][targets[n]],  0 where targets[n] == ignore_index.
+ * x [N][D] and w [V][D] in `dtype`, row-major and contiguous; targets [N]
+ * 64-bit; loss, lse [N] fp32 (lse is written for ignored rows too).
+ * A target outside [0, V) that is not ignore_index is never read through: its
+ * loss is NaN, it adds nothing to the gradients, and status bit 2 is set
+ * (fibattn_check_status).  Limits: 0 <= N <= 2^24, 1 <= D <= 8192,
+ * 1 <= V <= 2^24.  N == 0 launches nothing but the zeroing of dw.
+ * Every product is accumulated in fp32; results do not depend on timing.
+ * As in any matrix product, an ignored row of x that holds an infinity or NaN
+ * still reaches dw as 0 * NaN.
+ * ------------------------------------------------------------------------- */
+size_t fibattn_linear_xent_fwd_workspace_bytes(int N, int D, int V, int dtype);
+
+int fibattn_linear_xent_fwd(const void* x, const void* w, const long long* targets,
+                            float* loss, float* lse,
+                            int N, int D, int V, long long ignore_index, int dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of sum_n dloss[n] * loss[n] (dloss [N] fp32, on the device), with
+ * lse from the forward of the same x and w:
+ *   g[n][v] = dloss[n] (exp(s[n][v] - lse[n]) - [v == targets[n]]), 0 for ignored rows;
+ *   dx = g w [N][D],  dw = g^T x [V][D], in `dtype`, overwritten.
+ * The logits are formed again, a piece of the vocabulary at a time; g of one
+ * piece is held in the workspace (bf16 for bf16 I/O).  dx and dw may not alias
+ * each other, an input or the workspace. */
+size_t fibattn_linear_xent_bwd_workspace_bytes(int N, int D, int V, int dtype);
+
+int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targets,
+                            const float* lse, const float* dloss,
+                            void* dx, void* dw,
+                            int N, int D, int V, long long ignore_index, int dtype,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Global norm of n tensors and clipping:
+ *   norm = sqrt(sum of the squares of all values),
+ *   out_i = grad_i * min(1, max_norm / (norm + 1e-6)).
+ * grads, outs, numels and dtypes are HOST arrays of n entries, read during the
+ * call only; grads[i] and outs[i] are device pointers to numels[i] >= 0
+ * contiguous values of dtypes[i], aligned to their element (any view of a flat
+ * buffer will do).  outs == NULL: the norm alone.  outs[i] == grads[i] clips
+ * in place (and, with norm below max_norm, writes nothing); otherwise an out
+ * may not overlap a grad or another out.  max_norm >= 0 (infinity: no
+ * clipping).  norm: device, 1 float.  A norm that is not finite passes into
+ * the outputs by the formula above (NaN, or 0 with NaN where the infinities
+ * were); the caller that wants to skip such a step looks at norm.  Squares
+ * are summed in fp32 within a run of at most 256 values of one thread and in
+ * fp64 beyond; the result does not depend on timing. */
+size_t fibattn_clip_grads_workspace_bytes(int n);
+
+int fibattn_clip_grads(int n, const void* const* grads, void* const* outs,
+                       const long long* numels, const int* dtypes, float max_norm,
+                       float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Opt-in kernel timing (no counterpart in the paper; used to attribute time

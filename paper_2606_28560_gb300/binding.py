@@ -81,6 +81,19 @@ def lib():
             L.fibattn_check_status.restype = ci
             L.fibattn_test_wait_timeout.argtypes = [ctypes.c_uint, vp]
             L.fibattn_test_wait_timeout.restype = ci
+            ll = ctypes.c_longlong
+            L.fibattn_linear_xent_fwd_workspace_bytes.argtypes = [ci] * 4
+            L.fibattn_linear_xent_fwd_workspace_bytes.restype = sz
+            L.fibattn_linear_xent_fwd.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ll, ci, vp, sz, vp]
+            L.fibattn_linear_xent_fwd.restype = ci
+            L.fibattn_linear_xent_bwd_workspace_bytes.argtypes = [ci] * 4
+            L.fibattn_linear_xent_bwd_workspace_bytes.restype = sz
+            L.fibattn_linear_xent_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ll, ci, vp, sz, vp]
+            L.fibattn_linear_xent_bwd.restype = ci
+            L.fibattn_clip_grads_workspace_bytes.argtypes = [ci]
+            L.fibattn_clip_grads_workspace_bytes.restype = sz
+            L.fibattn_clip_grads.argtypes = [ci, vp, vp, vp, vp, cf, vp, vp, sz, vp]
+            L.fibattn_clip_grads.restype = ci
             _lib = L
     return _lib
 
@@ -357,13 +370,124 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
     return dq, dk, dv, (dtheta[:1] if dtheta is not None else None), (dd[:K] if dd is not None else None)
 
 
+# ------------------------------------------- loss head, gradient clipping ----
+
+def _check_xent(x, w, targets, ignore_index):
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or targets.shape != x.shape[:1]:
+        raise ValueError("linear cross entropy takes x [N, D], w [V, D] and targets [N]")
+    for t in (x, w):
+        if not (t.is_cuda and t.is_contiguous() and t.dtype == x.dtype):
+            raise ValueError("x and w must be contiguous CUDA tensors of one dtype")
+    if not (targets.is_cuda and targets.is_contiguous() and targets.dtype == torch.int64):
+        raise ValueError("targets must be a contiguous CUDA int64 tensor")
+    if x.device != w.device or x.device != targets.device:
+        raise ValueError("x, w and targets must be on one device")
+    return x.shape[0], x.shape[1], w.shape[0], _dtype_code(x)
+
+
+def _f32_row(t, N, device, name):
+    if not (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (N,) and t.device == device):
+        raise ValueError(f"{name} must be a contiguous fp32 tensor of N values on x's device")
+    return t
+
+
+def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=None, workspace=None, stream=None):
+    """Cross entropy of the linear head ``x @ w.T`` without forming it in
+    memory (fibattn_linear_xent_fwd).  x [N, D], w [V, D] (fp32 or bf16, CUDA,
+    contiguous), targets [N] int64; rows whose target is ``ignore_index`` have
+    loss 0.  Returns (loss [N], lse [N]) in fp32; ``lse`` goes to
+    ``linear_xent_bwd``."""
+    N, D, V, code = _check_xent(x, w, targets, ignore_index)
+    loss = x.new_empty(N, dtype=torch.float32) if loss is None else _f32_row(loss, N, x.device, "loss")
+    lse = x.new_empty(N, dtype=torch.float32) if lse is None else _f32_row(lse, N, x.device, "lse")
+    if workspace is None:                        # (a given workspace's size is checked by the library)
+        need = lib().fibattn_linear_xent_fwd_workspace_bytes(N, D, V, code)
+        workspace = x.new_empty(max(need, 256), dtype=torch.uint8)
+    _check(lib().fibattn_linear_xent_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(),
+                                         lse.data_ptr(), N, D, V, int(ignore_index), code, workspace.data_ptr(),
+                                         workspace.numel(), _stream_ptr(stream)))
+    return loss, lse
+
+
+def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=None, dw=None, workspace=None,
+                    stream=None):
+    """Gradients of ``sum(dloss * loss)`` by x and w (fibattn_linear_xent_bwd).
+    lse [N] from ``linear_xent_fwd`` of the same inputs; dloss [N] fp32.
+    Returns (dx [N, D], dw [V, D]) in x's dtype."""
+    N, D, V, code = _check_xent(x, w, targets, ignore_index)
+    _f32_row(lse, N, x.device, "lse")
+    _f32_row(dloss, N, x.device, "dloss")
+    dx = torch.empty_like(x) if dx is None else dx
+    dw = torch.empty_like(w) if dw is None else dw
+    for t, of in ((dx, x), (dw, w)):
+        if not (t.is_contiguous() and t.dtype == of.dtype and t.shape == of.shape and t.device == of.device):
+            raise ValueError("dx and dw must be contiguous tensors like x and w")
+    if workspace is None:
+        need = lib().fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
+        workspace = x.new_empty(max(need, 256), dtype=torch.uint8)
+    _check(lib().fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(),
+                                         dloss.data_ptr(), dx.data_ptr(), dw.data_ptr(), N, D, V, int(ignore_index),
+                                         code, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+    return dx, dw
+
+
+_CLIP_CODE = {torch.float32: FIBATTN_F32, torch.bfloat16: FIBATTN_BF16}
+
+
+def clip_grads(grads, max_norm: float, *, out=None, norm=None, workspace=None, stream=None):
+    """Scales tensors by min(1, max_norm / (norm + 1e-6)), norm being the square
+    root of the sum of the squares of all their values (fibattn_clip_grads).
+    grads: contiguous CUDA tensors on one device, fp32 and bf16 in any mix, any
+    offset into a buffer.  ``out``: tensors of the same sizes and dtypes, or
+    None to clip in place.  Returns norm, a 0-dim fp32 tensor on the device."""
+    return _clip(list(grads), float(max_norm), out, norm, workspace, stream, True)
+
+
+def grad_norm(grads, *, norm=None, workspace=None, stream=None):
+    """The norm alone, as ``clip_grads`` computes it; nothing else is written."""
+    return _clip(list(grads), float("inf"), None, norm, workspace, stream, False)
+
+
+def _clip(grads, max_norm, out, norm, workspace, stream, scale):
+    n = len(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != n:
+        raise ValueError("out must hold one tensor for each gradient")
+    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    try:
+        codes = [_CLIP_CODE[t.dtype] for t in grads]
+    except KeyError:
+        raise TypeError("unsupported dtype: fp32 or bf16") from None
+    sizes = [t.numel() for t in grads]
+    for t in grads:
+        if not (t.is_cuda and t.is_contiguous() and t.device == device):
+            raise ValueError("gradients must be contiguous CUDA tensors on one device")
+    if out is not None:
+        for t, g, m in zip(outs, grads, sizes):
+            if not (t.is_cuda and t.is_contiguous() and t.device == device and t.dtype == g.dtype and t.numel() == m):
+                raise ValueError("out must hold contiguous tensors like the gradients")
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=device)
+    elif not (norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == device):
+        raise ValueError("norm must be one fp32 value on the gradients' device")
+    if workspace is None:
+        workspace = torch.empty(max(lib().fibattn_clip_grads_workspace_bytes(n), 256), dtype=torch.uint8,
+                                device=device)
+    ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in grads])
+    optrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs]) if scale else None
+    _check(lib().fibattn_clip_grads(n, ptrs, optrs, (ctypes.c_longlong * n)(*sizes), (ctypes.c_int * n)(*codes),
+                                    max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                    _stream_ptr(stream)))
+    return norm
+
+
 # ---------------------------------------------------------- device status ----
 
 def check_status(stream=None):
     """Synchronise ``stream`` and read and clear the device status word
     (fibattn_check_status).  Returns the flags; raises FibattnError when a
-    kernel gave up a bounded wait (status 4) or a rotated row overflowed fp16
-    (status 5)."""
+    kernel gave up a bounded wait (status 4), a rotated row overflowed fp16 or a
+    cross-entropy target was outside the vocabulary (status 5)."""
     flags = ctypes.c_uint(0)
     rc = lib().fibattn_check_status(_stream_ptr(stream), ctypes.byref(flags))
     if rc != 0:

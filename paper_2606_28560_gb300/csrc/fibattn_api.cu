@@ -262,6 +262,16 @@ cudaEvent_t prof_event() {
 
 namespace fibattn {
 int set_error(int code, const char* msg) { return fail(code, "%s", msg); }
+int set_errorf(int code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    return fail(code, "%s", buf);
+}
+int bind_device_context() { return bind_context(); }
+int device_status_word(unsigned** out) { return status_word(out); }
 
 // During stream capture the records become external event nodes of the
 // graph, so every replay of the graph re-times the kernel.
@@ -603,6 +613,9 @@ int fibattn_check_status(void* stream, unsigned* flags) {
     if (h & kStatusRange)
         return fail(FIBATTN_ERR_RANGE, "a RoPE-rotated q or k entry reached 65520 in magnitude, beyond the fp16 "
                                        "rows of the bf16 path (scores with such operands are not meaningful)");
+    if (h & kStatusTarget)
+        return fail(FIBATTN_ERR_RANGE, "a cross-entropy target was outside the vocabulary and not ignore_index "
+                                       "(the loss of such rows is NaN)");
     return FIBATTN_OK;
 }
 

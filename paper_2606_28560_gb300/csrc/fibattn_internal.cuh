@@ -67,6 +67,7 @@ struct Shape {
 // fibattn_check_status): kernels OR these bits into it.
 constexpr unsigned kStatusWaitTimeout = 1u;   // a bounded wait on a staging copy ran out
 constexpr unsigned kStatusRange = 2u;         // a rotated row overflowed its fp16 storage
+constexpr unsigned kStatusTarget = 4u;        // a cross-entropy target outside the vocabulary
 __device__ __forceinline__ void raise_status(unsigned* st, unsigned bits) {
     if (st) atomicOr(st, bits);
 }
@@ -330,6 +331,12 @@ int bwd_simple_blocks(const Shape& s);
 
 // Records a message for fibattn_last_error() and returns `code`.
 int set_error(int code, const char* msg);
+int set_errorf(int code, const char* fmt, ...);
+
+// Host: makes the primary context of the thread's current device current;
+// the device address of its status word.  Both return a fibattn_status.
+int bind_device_context();
+int device_status_word(unsigned** out);
 
 // Opt-in per-kernel timing: when enabled, each launch is bracketed by CUDA
 // events recorded on the caller's stream (see fibattn_profile_* in the ABI).

@@ -1,0 +1,60 @@
+"""What follows the layers in a training step: the loss of a linear head over
+a large vocabulary, and gradient clipping (arXiv 2606.28560, Section 3, "Model
+and training": a tied embedding over 32768 tokens, gradients clipped to 1).
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+
+class LinearCrossEntropyFunction(torch.autograd.Function):
+    """loss[n] = log sum_v exp(x[n] . w[v]) - x[n] . w[targets[n]], 0 where
+    targets[n] is ignore_index.  Neither the logits nor their gradient are kept
+    between the forward and the backward; gradients flow to x and w."""
+
+    @staticmethod
+    def forward(ctx, x, w, targets, ignore_index):
+        loss, lse = B.linear_xent_fwd(x, w, targets, ignore_index=ignore_index)
+        ctx.save_for_backward(x, w, targets, lse)
+        ctx.ignore_index = ignore_index
+        return loss
+
+    @staticmethod
+    def backward(ctx, dloss):
+        x, w, targets, lse = ctx.saved_tensors
+        dx, dw = B.linear_xent_bwd(x, w, targets, lse, dloss.contiguous(), ignore_index=ctx.ignore_index)
+        return dx, dw, None, None
+
+
+def linear_cross_entropy(x, w, targets, *, ignore_index: int = -100, reduction: str = "mean"):
+    """Cross entropy of the logits ``x @ w.T``.  x [..., D] hidden states, w
+    [V, D] head weights of the same dtype (fp32 or bf16, CUDA, contiguous),
+    targets [...] int64.  ``reduction``: "mean" over the rows with a target (NaN
+    when there is none, as the mean of nothing is), "sum", or "none" (the shape
+    of targets).  The loss is fp32."""
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError("reduction must be 'mean', 'sum' or 'none'")
+    if x.shape[:-1] != targets.shape:
+        raise ValueError("targets must have x's shape without its last dimension")
+    flat = targets.reshape(-1)
+    loss = LinearCrossEntropyFunction.apply(x.reshape(-1, x.shape[-1]), w, flat, int(ignore_index))
+    if reduction == "none":
+        return loss.reshape(targets.shape)
+    if reduction == "sum":
+        return loss.sum()
+    return loss.sum() / (flat != ignore_index).sum()
+
+
+def clip_grad_norm_(parameters, max_norm: float) -> torch.Tensor:
+    """Clips the gradients of ``parameters`` (an iterable, or one tensor) to a
+    global norm of ``max_norm`` in place; parameters without a gradient are left
+    out.  Returns the norm before clipping, a 0-dim fp32 tensor on the device;
+    nothing waits for the GPU."""
+    if torch.is_tensor(parameters):
+        parameters = [parameters]
+    grads = [p.grad for p in parameters if p.grad is not None]
+    if not grads:
+        return torch.zeros(())
+    return B.clip_grads(grads, max_norm)

@@ -1,0 +1,369 @@
+"""Linear cross entropy (loss, lse and both gradients) against the definition
+in 64 bits, over types, sizes from one row to many, odd and ragged ones, rows
+without a target, and refusals.
+
+Tolerances follow from the arithmetic.  With u = 2^-23 (an fp32 sum that may
+truncate) and S = max |x| . |w| over the products of a logit, a logit is within
+e = (D + 8) u S; lse and loss within 2 e + 16 u (1 + |lse|).  A gradient entry
+is a sum of |g| |w| terms, |g| <= dloss (p + onehot): each term is off by 2 e
+(through p) and, with bf16 I/O, by the 2^-8 of g's own rounding; the sum adds K u
+and the result's rounding 2^-8 (bf16) or u.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_28560_gb300 as fa
+from paper_2606_28560_gb300 import binding as B
+from paper_2606_28560_gb300 import build as build_mod
+
+U = 2.0 ** -23
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def make(N, D, V, dtype, seed, mask="some", scale=2.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(N, D, generator=g)
+    w = torch.randn(V, D, generator=g) * (scale / D ** 0.5)
+    t = torch.randint(0, V, (N,), generator=g)
+    if N:
+        t[0], t[-1] = 0, V - 1                    # the first and the last column
+    if mask == "some":
+        t[torch.rand(N, generator=g) < 0.3] = -100
+    elif mask == "all":
+        t[:] = -100
+    dl = torch.rand(N, generator=g) + 0.1
+    return x.to(dtype).cuda(), w.to(dtype).cuda(), t.cuda(), dl.cuda()
+
+
+def truth(x, w, t, dl):
+    """The definition in fp64, and the bounds of the module's docstring."""
+    D, V, N = x.shape[1], w.shape[0], x.shape[0]
+    x, w, dl = x.double(), w.double(), dl.double()
+    s = x @ w.t()
+    e = (D + 8) * U * float((x.abs() @ w.abs().t()).max())
+    lse = torch.logsumexp(s, 1)
+    has = t != -100
+    one = torch.zeros_like(s)
+    one[has, t[has]] = 1.0
+    loss = (lse - (s * one).sum(1)) * has
+    p = torch.exp(s - lse[:, None])
+    c = (dl * has)[:, None]
+    g, a = c * (p - one), c * (p + one)
+    return dict(lse=lse, loss=loss, dx=g @ w, dw=g.t() @ x, e=e, tol=2 * e + 16 * U * (1 + lse.abs().max()),
+                ax=a @ w.abs(), aw=a.t() @ x.abs())
+
+
+def check(x, w, t, dl, tag=""):
+    r = truth(x, w, t, dl)
+    bf = x.dtype == torch.bfloat16
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    assert (lse.double() - r["lse"]).abs().max() <= r["tol"], tag
+    assert (loss.double() - r["loss"]).abs().max() <= r["tol"], tag
+    assert not loss[t == -100].any()
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    for name, got, want, mag, K in (("dx", dx, r["dx"], r["ax"], w.shape[0]), ("dw", dw, r["dw"], r["aw"], x.shape[0])):
+        rel = 2 * r["tol"] + (K + 8) * U + (2.0 ** -8 if bf else 0.0)
+        tol = rel * mag + (2.0 ** -8 if bf else U) * want.abs() + 1e-30
+        bad = (got.double() - want).abs() > tol
+        assert not bad.any(), f"{tag} {name}: {int(bad.sum())} of {bad.numel()} beyond the bound"
+        norm = float(want.norm())
+        if norm > 0:                              # two independent bf16 roundings: 2^-9 sqrt(2/3) = 1.6e-3, twice that at most
+            off = float((got.double() - want).norm()) / norm
+            assert off <= (3.2e-3 if bf else 1e-5), f"{tag} {name}: {off}"
+    assert not dx[t == -100].any()
+    return loss, lse, dx, dw
+
+
+SIZES = [(1, 1, 1), (1, 64, 257), (3, 7, 5), (2, 512, 4096), (100, 64, 257), (129, 100, 1000), (257, 72, 513),
+         (256, 64, 256), (255, 128, 255), (1001, 100, 5003), (300, 520, 20011), (64, 2048, 3001), (513, 1030, 700),
+         (1024, 512, 2048), (7, 1536, 30000), (2049, 8, 31), (128, 333, 128)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+def test_matches_definition(size, dtype):
+    check(*make(*size, TYPES[dtype], seed=sum(size)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("mask", ["none", "all"])
+def test_masks(mask, dtype):
+    x, w, t, dl = make(300, 96, 777, TYPES[dtype], 5, mask)
+    loss, lse, dx, dw = check(x, w, t, dl)
+    if mask == "all":
+        assert not loss.any() and not dx.any() and not dw.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_several_pieces_of_the_vocabulary(dtype):
+    # g of all columns is above the piece limit: several pieces, the last one ragged
+    check(*make(20000, 72, 20003, TYPES[dtype], 6))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_large_logits(dtype):
+    # spread of thousands: exp of anything but the maximum vanishes, nothing overflows
+    x, w, t, dl = make(130, 64, 1000, TYPES[dtype], 7, scale=2000.0)
+    loss, lse, dx, dw = check(x, w, t, dl)
+    assert all(torch.isfinite(v).all() for v in (loss, lse, dx, dw))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_zero_rows_and_columns(dtype):
+    x, w, t, dl = make(200, 64, 300, TYPES[dtype], 8)
+    x[5], w[:] = 0, w
+    w[17] = 0
+    check(x, w, t, dl)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_a_row_that_is_not_finite_stays_alone(value, dtype):
+    x, w, t, dl = make(200, 64, 300, TYPES[dtype], 9, "none")
+    clean, _ = fa.linear_xent_fwd(x, w, t)
+    lse0 = fa.linear_xent_fwd(x, w, t)[1]
+    dx0, _ = fa.linear_xent_bwd(x, w, t, lse0, dl)
+    x[37, 3] = value
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    keep = torch.arange(200, device="cuda") != 37
+    assert torch.equal(loss[keep], clean[keep]) and not torch.isfinite(loss[37])
+    dx, _ = fa.linear_xent_bwd(x, w, t, lse, dl)
+    assert torch.equal(dx[keep], dx0[keep])
+    t[37] = -100                                  # without a target: loss and dx are exactly zero
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    dx, _ = fa.linear_xent_bwd(x, w, t, lse, dl)
+    assert loss[37] == 0 and not dx[37].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_target_outside_the_vocabulary(dtype):
+    x, w, t, dl = make(150, 64, 300, TYPES[dtype], 10, "none")
+    fa.check_status()
+    want = t.clone()
+    want[[3, 140, 149]] = -100
+    t[3], t[140], t[149] = 300, -1, 2 ** 40
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    with pytest.raises(fa.FibattnError) as ei:
+        fa.check_status()
+    assert ei.value.status == 5 and ei.value.flags == 4
+    assert torch.isnan(loss[[3, 140, 149]]).all() and int(torch.isnan(loss).sum()) == 3
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    with pytest.raises(fa.FibattnError):
+        fa.check_status()
+    dx2, dw2 = fa.linear_xent_bwd(x, w, want, lse, dl)
+    assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+    assert fa.check_status() == 0
+
+
+@pytest.mark.gpu
+def test_other_ignore_index():
+    x, w, t, dl = make(90, 64, 200, torch.bfloat16, 11)
+    t2 = torch.where(t == -100, torch.full_like(t, 7), torch.where(t == 7, torch.full_like(t, 8), t))
+    want = torch.where(t2 == 7, torch.full_like(t, -100), t2)
+    a, b = fa.linear_xent_fwd(x, w, t2, ignore_index=7), fa.linear_xent_fwd(x, w, want)
+    assert torch.equal(a[0], b[0])
+    g, h = fa.linear_xent_bwd(x, w, t2, a[1], dl, ignore_index=7), fa.linear_xent_bwd(x, w, want, b[1], dl)
+    assert torch.equal(g[0], h[0]) and torch.equal(g[1], h[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_no_rows(dtype):
+    x, w, t, dl = make(0, 64, 300, TYPES[dtype], 12)
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    assert loss.shape == (0,)
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    assert dx.shape == (0, 64) and not dw.any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_same_result_every_time_and_on_another_stream(dtype):
+    x, w, t, dl = make(700, 200, 9001, TYPES[dtype], 13)
+    first = fa.linear_xent_fwd(x, w, t)
+    first += fa.linear_xent_bwd(x, w, t, first[1], dl)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        with torch.cuda.stream(s):
+            again = fa.linear_xent_fwd(x, w, t)
+            again += fa.linear_xent_bwd(x, w, t, again[1], dl)
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_writes_only_its_outputs(dtype):
+    """Outputs and workspace lie between guards of a known pattern."""
+    N, D, V = 130, 72, 515
+    x, w, t, dl = make(N, D, V, TYPES[dtype], 14)
+
+    def guarded(nbytes):
+        pad = 4096
+        buf = torch.full((pad + (nbytes + 255) // 256 * 256 + pad,), 0x5a, dtype=torch.uint8, device="cuda")
+        return buf, buf[pad:pad + nbytes]
+
+    code = B._dtype_code(x)
+    es = x.element_size()
+    sizes = dict(loss=N * 4, lse=N * 4, dx=N * D * es, dw=V * D * es,
+                 wf=B.lib().fibattn_linear_xent_fwd_workspace_bytes(N, D, V, code),
+                 wb=B.lib().fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code))
+    bufs = {k: guarded(v) for k, v in sizes.items()}
+    v = {k: b[1] for k, b in bufs.items()}
+    loss, lse = fa.linear_xent_fwd(x, w, t, loss=v["loss"].view(torch.float32), lse=v["lse"].view(torch.float32),
+                                   workspace=v["wf"])
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl, dx=v["dx"].view(x.dtype).view(N, D), dw=v["dw"].view(x.dtype).view(V, D),
+                                workspace=v["wb"])
+    torch.cuda.synchronize()
+    for k, (buf, _) in bufs.items():
+        n = sizes[k]
+        assert bool((buf[:4096] == 0x5a).all()) and bool((buf[4096 + n:] == 0x5a).all()), k
+    plain = fa.linear_xent_fwd(x, w, t)
+    assert torch.equal(plain[0], loss) and torch.equal(plain[1], lse)
+    g = fa.linear_xent_bwd(x, w, t, lse, dl)
+    assert torch.equal(g[0], dx) and torch.equal(g[1], dw)
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences():
+    """Central differences of the library's own loss; a loss is within some 1e-6 in
+    fp32, so a quotient over 2 h = 0.04 is within 1e-4, plus h^2 of the third derivative."""
+    x, w, t, dl = make(5, 6, 7, torch.float32, 15, "none")
+    t[2] = -100
+    h = 0.02
+
+    def total(x, w):
+        return float((fa.linear_xent_fwd(x, w, t)[0].double() * dl.double()).sum())
+
+    _, lse = fa.linear_xent_fwd(x, w, t)
+    grads = fa.linear_xent_bwd(x, w, t, lse, dl)
+    for which, g in enumerate(grads):
+        for i in range(g.shape[0]):
+            for j in range(g.shape[1]):
+                at = []
+                for sign in (1, -1):
+                    y = [x.clone(), w.clone()]
+                    y[which][i, j] += sign * h
+                    at.append(total(*y))
+                assert abs((at[0] - at[1]) / (2 * h) - float(g[i, j])) <= 2e-3
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+def test_autograd(reduction, dtype):
+    x, w, t, _ = make(60, 64, 131, TYPES[dtype], 16)
+    x, t = x.view(3, 20, 64), t.view(3, 20)
+    x.requires_grad_(True)
+    w.requires_grad_(True)
+    loss = fa.linear_cross_entropy(x, w, t, reduction=reduction)
+    up = torch.rand(loss.shape, device="cuda") + 0.5
+    (loss * up).sum().backward()
+    has = (t != -100).view(-1)
+    dl = {"mean": (up / has.sum()).expand(60), "sum": up.expand(60), "none": up.reshape(-1)}[reduction] if \
+        reduction != "none" else up.reshape(-1)
+    r = truth(x.detach().view(60, 64), w.detach(), t.view(-1), dl.contiguous())
+    want = {"mean": r["loss"].sum() / has.sum(), "sum": r["loss"].sum(), "none": r["loss"].view(3, 20)}[reduction]
+    assert (loss.double() - want).abs().max() <= (1 if reduction != "sum" else 60) * r["tol"] + 64 * U * want.abs().max()
+    bf = dtype == "bf16"
+    for got, ref in ((x.grad.view(60, 64), r["dx"]), (w.grad, r["dw"])):
+        assert float((got.double() - ref).norm() / ref.norm()) <= (3.2e-3 if bf else 1e-5)
+
+
+# -------------------------------------------------------------- refusals ----
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    build_mod.build()
+
+
+def _fwd(x=256, w=256, t=256, loss=256, lse=256, N=4, D=8, V=16, dtype=1, ws=256, nbytes=1 << 30):
+    vp = ctypes.c_void_p
+    return B.lib().fibattn_linear_xent_fwd(vp(x), vp(w), vp(t), vp(loss), vp(lse), N, D, V, -100, dtype, vp(ws), nbytes,
+                                           None)
+
+
+def _bwd(x=256, w=256, t=256, lse=256, dl=256, dx=256, dw=256, N=4, D=8, V=16, dtype=1, ws=256, nbytes=1 << 30):
+    vp = ctypes.c_void_p
+    return B.lib().fibattn_linear_xent_bwd(vp(x), vp(w), vp(t), vp(lse), vp(dl), vp(dx), vp(dw), N, D, V, -100, dtype,
+                                           vp(ws), nbytes, None)
+
+
+@pytest.mark.parametrize("call", [_fwd, _bwd])
+@pytest.mark.parametrize("bad", [dict(N=-1), dict(N=(1 << 24) + 1), dict(D=0), dict(D=8193), dict(V=0),
+                                 dict(V=(1 << 24) + 1), dict(dtype=2), dict(x=0), dict(w=0), dict(t=0), dict(lse=0),
+                                 dict(ws=0), dict(x=264), dict(w=257), dict(t=260), dict(lse=260), dict(ws=264),
+                                 dict(nbytes=16)], ids=str)
+def test_refused_before_any_launch(call, bad):
+    assert call(**bad) == 1
+    assert B.lib().fibattn_last_error()
+
+
+def test_refused_outputs():
+    assert _fwd(loss=0) == 1 and _fwd(loss=264) == 1
+    for name in ("dl", "dx", "dw"):
+        assert _bwd(**{name: 0}) == 1 and _bwd(**{name: 264}) == 1
+
+
+def test_no_rows_need_no_pointers():
+    assert _fwd(0, 0, 0, 0, 0, N=0, ws=0, nbytes=0) == 0
+
+
+def test_workspace_sizes():
+    f, b = B.lib().fibattn_linear_xent_fwd_workspace_bytes, B.lib().fibattn_linear_xent_bwd_workspace_bytes
+    assert f(-1, 64, 100, 1) == 0 and b(4, 0, 100, 1) == 0 and b(4, 64, 100, 7) == 0
+    # far below the fp32 logits of the same call
+    assert 0 < f(16384, 512, 32768, 1) < 16384 * 32768 * 4 // 64
+    assert 0 < b(16384, 512, 32768, 1) < 16384 * 32768 * 4 // 3
+
+
+def test_python_checks():
+    x, w, t = torch.zeros(4, 8), torch.zeros(16, 8), torch.zeros(4, dtype=torch.int64)
+    with pytest.raises(ValueError, match="CUDA"):
+        fa.linear_xent_fwd(x, w, t)
+    with pytest.raises(ValueError, match=r"\[N, D\]"):
+        fa.linear_xent_fwd(x, w[:, :4], t)
+    with pytest.raises(ValueError, match=r"\[N, D\]"):
+        fa.linear_xent_fwd(x, w, t[:3])
+    with pytest.raises(ValueError, match="reduction"):
+        fa.linear_cross_entropy(x, w, t, reduction="max")
+    with pytest.raises(ValueError, match="targets"):
+        fa.linear_cross_entropy(x, w, t.view(2, 2))
+
+
+@pytest.mark.gpu
+def test_python_checks_on_tensors():
+    x, w, t, dl = make(8, 16, 20, torch.bfloat16, 17)
+    with pytest.raises(ValueError, match="contiguous"):
+        fa.linear_xent_fwd(x.t().contiguous().t(), w, t)
+    with pytest.raises(ValueError, match="one dtype"):
+        fa.linear_xent_fwd(x, w.float(), t)
+    with pytest.raises(TypeError):
+        fa.linear_xent_fwd(x.half(), w.half(), t)
+    with pytest.raises(ValueError, match="int64"):
+        fa.linear_xent_fwd(x, w, t.int())
+    _, lse = fa.linear_xent_fwd(x, w, t)
+    with pytest.raises(ValueError, match="dloss"):
+        fa.linear_xent_bwd(x, w, t, lse, dl.double())
+    with pytest.raises(ValueError, match="lse"):
+        fa.linear_xent_bwd(x, w, t, lse[:4], dl)
+    with pytest.raises(ValueError, match="dx and dw"):
+        fa.linear_xent_bwd(x, w, t, lse, dl, dx=x.float())
+    with pytest.raises(fa.FibattnError, match="aligned"):
+        flat = torch.zeros(8 * 16 + 1, dtype=torch.bfloat16, device="cuda")
+        fa.linear_xent_fwd(flat[1:].view(8, 16), w, t)
+    with pytest.raises(fa.FibattnError, match="workspace"):
+        fa.linear_xent_fwd(x, w, t, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
