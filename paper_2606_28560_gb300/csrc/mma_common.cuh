@@ -10,6 +10,10 @@
 #include "fwd_mma.cuh"
 
 namespace fibattn {
+
+// Host: the driver's tensor-map encoder (nullptr when it has none).
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder();
+
 namespace mma {
 
 // A wait on a staging copy gives up after this long (the copies are of at

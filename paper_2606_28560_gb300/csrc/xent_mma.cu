@@ -1,0 +1,759 @@
+// xent_mma.cu -- linear cross entropy on the fifth-generation tensor cores.
+//
+// Three passes share one engine, a product C[i][j] = sum_k A[i][k] B[j][k] in
+// tiles of 256 x 256 over a pair of CTAs (each holds 128 rows of A and half of
+// the columns' B; one thread of the even CTA issues the MMAs for both):
+//   forward  A = x, B = w, depth D: a row's running maximum and sum of exp
+//   gradient A = x, B = w of a piece of the vocabulary: g in bf16 to memory
+//   products A = g, B = w (dx, depth: the piece) and A = g^T, B = x (dw, depth N)
+// Warp 0 loads (TMA), warp 1 multiplies, warps 4..11 take the accumulators out
+// of TMEM: warp w reads lanes 32 (w % 4).. and columns 128 ((w - 4) / 4)... of
+// the tile, so a thread owns 128 columns of one row and a row's statistics need
+// no exchange.  Two accumulators of 256 columns alternate (or, for products
+// wider than 256 columns, are two halves of a tile of 512 that shares A).
+//
+// The tensor core truncates as it accumulates (some 2e-8 of the running sum
+// for each 16 of depth), so a long depth is cut into runs whose sums are added
+// in registers: 512 deep for bf16 logits, whose loss and lse are fp32 results.
+// The products of bf16 gradients, rounded to 8 bits at the end, are not cut.
+#include <algorithm>
+
+#include "tc5.cuh"
+#include "xent.cuh"
+#include "xent_mma.cuh"
+
+namespace fibattn {
+namespace xent {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr unsigned kOperandBytes = 16384;          // 128 rows x 64 deep, bf16
+constexpr float kLog2e = 1.4426950408889634f;
+
+enum Mode { kForward, kGradient, kProducts };
+
+template <int MODE, int NB> struct Config {
+    static constexpr unsigned kStageBytes = kOperandBytes * (1 + NB);
+    static constexpr int kStages = NB == 2 ? 4 : MODE == kGradient ? 5 : 6;
+    static constexpr unsigned kStoreBytes = MODE == kGradient ? kEpilogueWarps * 2 * 4096 : 0;   // two 32 x 64 boxes a warp
+    static constexpr unsigned kSmem = kStages * kStageBytes + kStoreBytes + 1024;
+};
+
+// One tile (or a part of its depth): rows from m0, columns from n0, depth in
+// chunks of 64 from k0 to k1.
+struct Item {
+    int m0, n0, k0, k1;
+    int problem;                                   // products: 0 dx, 1 dw
+    int unit;                                      // forward: segment of the vocabulary
+    bool first, last;                              // forward: of its unit
+    bool whole;                                    // products: the whole depth
+    int tile_lo, tile_hi;                          // products: the tile's range of the iteration space
+};
+
+// The items of cluster c, in order.
+template <int MODE> struct Walk {
+    const Args& a;
+    int c, clusters, at, sub, end;
+    __device__ Walk(const Args& args, int cluster, int n) : a(args), c(cluster), clusters(n), at(cluster), sub(0), end(0) {
+        if (MODE == kProducts) {
+            at = bound(c);
+            end = bound(c + 1);
+        }
+    }
+    // Products: start of cluster c's range of the iteration space (all tiles'
+    // chunks of depth one after another).  Equal shares, but a boundary within
+    // `snap` chunks of a tile's end moves there: a sliver is not worth the
+    // exchange of a whole tile of partial sums.
+    __device__ int bound(int cluster) const {
+        const int b = (int)((long long)a.total * cluster / clusters);
+        if (b <= 0 || b >= a.total) return b <= 0 ? 0 : a.total;
+        const int p = b < a.split ? 0 : 1, base = p ? a.split : 0, kc = a.prob[p].chunks;
+        const int off = (b - base) % kc;
+        if (off <= a.snap) return b - off;
+        if (kc - off <= a.snap) return b - off + kc;
+        return b;
+    }
+    __device__ bool next(Item& it) {
+        if (MODE == kForward) {
+            if (at >= a.units) return false;
+            const int mt = at % a.row_tiles, s = at / a.row_tiles;
+            const int lo = s * a.unit_tiles, hi = min(a.col_tiles, lo + a.unit_tiles);
+            it.m0 = mt * 256;
+            it.n0 = (lo + sub) * 256;
+            it.k0 = 0;
+            it.k1 = a.chunks;
+            it.unit = s;
+            it.first = sub == 0;
+            it.last = lo + sub + 1 >= hi;
+            if (it.last) { sub = 0; at += clusters; }
+            else ++sub;
+            return true;
+        } else if (MODE == kGradient) {
+            if (at >= a.units) return false;
+            it.m0 = (at % a.row_tiles) * 256;
+            it.n0 = (at / a.row_tiles) * 256;
+            it.k0 = 0;
+            it.k1 = a.chunks;
+            at += clusters;
+            return true;
+        } else {
+            if (at >= end) return false;
+            it.problem = at < a.split ? 0 : 1;
+            const Product& p = a.prob[it.problem];
+            const int base = it.problem ? a.split : 0, t = (at - base) / p.chunks;
+            it.tile_lo = base + t * p.chunks;
+            it.tile_hi = it.tile_lo + p.chunks;
+            const int stop = min(end, it.tile_hi);
+            it.m0 = (t / p.col_tiles) * 256;
+            it.n0 = (t % p.col_tiles) * a.tile_cols;
+            it.k0 = at - it.tile_lo;
+            it.k1 = stop - it.tile_lo;
+            it.whole = it.k0 == 0 && it.k1 == p.chunks;
+            at = stop;
+            return true;
+        }
+    }
+};
+
+// Columns of block b of a product's tile that are multiplied: a multiple of 32.
+__device__ __forceinline__ int block_columns(const Args& a, const Item& it, int b) {
+    return min(256, max(0, (a.out_cols - it.n0 - 256 * b + 31) & ~31));
+}
+
+// fp32 operands are sums of three bf16 planes; six of the nine products of
+// planes are kept (the others are below 2^-24), the small ones first: while
+// the running sum is small so is what truncation takes from it.
+__device__ __forceinline__ void planes_of(int combo, int& pa, int& pb) {
+    switch (combo) {
+    case 0: pa = 0; pb = 2; break;
+    case 1: pa = 2; pb = 0; break;
+    case 2: pa = 1; pb = 1; break;
+    case 3: pa = 0; pb = 1; break;
+    case 4: pa = 1; pb = 0; break;
+    default: pa = 0; pb = 0; break;
+    }
+}
+
+// 128 columns of one output row from registers.  `aligned`: rows start on
+// 16-byte boundaries (then no group of 16 bytes straddles the end of a row).
+__device__ __forceinline__ void put_row(float* out, const float* v, int n, bool aligned) {
+    if (aligned) {
+#pragma unroll
+        for (int j = 0; j < 128; j += 4)
+            if (j < n) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 128; ++j)
+            if (j < n) out[j] = v[j];
+    }
+}
+__device__ __forceinline__ void put_row(__nv_bfloat16* out, const float* v, int n, bool aligned) {
+    if (aligned) {
+#pragma unroll
+        for (int j = 0; j < 128; j += 8)
+            if (j < n) Vec8<__nv_bfloat16>::store(out + j, v + j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 128; ++j)
+            if (j < n) out[j] = __float2bfloat16(v[j]);
+    }
+}
+
+// A product's sums leave the tile: at once where the tile's whole depth is in
+// them; else to this cluster's slot of partial sums, and the warp that finds
+// itself last adds the parts up in the order of the depth (so the result does
+// not depend on which one is last) and writes the row.
+template <int NB, bool F32>
+__device__ __forceinline__ void finish_product(const Args& a, const Item& it, const Walk<kProducts>& walk, int cluster, int rank,
+                                               int b, int ew, int lane, int row, int c0, float* acc) {
+    if (!it.whole) {
+        const auto slot = [&](int c) {
+            const size_t s = 2 * (size_t)c + (walk.bound(c) >= it.tile_lo ? 0 : 1);
+            return a.partials + (((s * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + lane;
+        };
+        float* mine = slot(cluster);
+#pragma unroll
+        for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
+        __threadfence();
+        __syncwarp();
+        int lo = cluster, hi = cluster, parts = 0;
+        while (walk.bound(lo) > it.tile_lo) --lo;
+        while (walk.bound(hi + 1) < it.tile_hi) ++hi;
+        for (int c = lo; c <= hi; ++c) parts += walk.bound(c + 1) > walk.bound(c);
+        unsigned before = 0;
+        if (lane == 0) before = atomicAdd(a.counters + ((lo * 2 + rank) * NB + b) * kEpilogueWarps + ew, 1u);
+        if ((int)__shfl_sync(0xffffffffu, before, 0) != parts - 1) return;
+        __threadfence();
+#pragma unroll
+        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+        for (int c = lo; c <= hi; ++c) {
+            if (walk.bound(c + 1) <= walk.bound(c)) continue;
+            const float* p = slot(c);
+#pragma unroll
+            for (int j = 0; j < 128; ++j) acc[j] += __ldcg(p + 32 * j);
+        }
+    }
+    if (row >= a.prob[it.problem].rows) return;
+    const int n = a.out_cols - c0;
+    const size_t at = (size_t)row * a.out_cols + c0;
+    const bool al4 = a.out_cols % 4 == 0;
+    if (it.problem == 0) {
+        if (a.dx_add) {
+            const float* p = a.dx_acc + at;
+#pragma unroll
+            for (int j = 0; j < 128; ++j)
+                if (j < n) acc[j] += p[j];
+        }
+        if (!a.dx_done) {
+            put_row(a.dx_acc + at, acc, n, al4);
+            return;
+        }
+    }
+    void* out = it.problem == 0 ? a.dx : a.dw;
+    if (F32) put_row(static_cast<float*>(out) + (it.problem == 0 ? at : at + (size_t)a.v0 * a.out_cols), acc, n, al4);
+    else put_row(static_cast<__nv_bfloat16*>(out) + (it.problem == 0 ? at : at + (size_t)a.v0 * a.out_cols), acc, n, a.out_cols % 8 == 0);
+}
+
+__device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
+
+template <int MODE, int NB, bool F32>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
+    using C = Config<MODE, NB>;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ unsigned long long bars[2 * C::kStages + 4];
+    __shared__ unsigned tmem_base_s;
+    const unsigned smem0 = (tc5::smem_u32(smem_raw) + 1023u) & ~1023u;
+    const unsigned full = tc5::smem_u32(bars), empty = full + 8 * C::kStages;
+    const unsigned acc_full = empty + 8 * C::kStages, acc_empty = acc_full + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned rank = tc5::cluster_rank();
+    const int cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+
+    if (warp == 0 && lane == 0) {
+        for (int s = 0; s < C::kStages; ++s) {
+            tc5::init_barrier(full + 8 * s, 1);
+            tc5::init_barrier(empty + 8 * s, 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            tc5::init_barrier(acc_full + 8 * b, 1);
+            tc5::init_barrier(acc_empty + 8 * b, 2 * kEpilogueWarps);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+        tc5::prefetch_map(&maps.m[0]);
+        tc5::prefetch_map(&maps.m[1]);
+    }
+    if (warp == 2) tc5::tmem_alloc(tc5::smem_u32(&tmem_base_s));
+    tc5::fence_before();
+    __syncthreads();
+    tc5::cluster_sync();
+    tc5::fence_after();
+    const unsigned tmem = tmem_base_s;
+    grid_dependency_sync();
+    asm volatile("fence.proxy.async.global;\n" ::: "memory");   // operands written by the kernel before are read by TMA
+
+    constexpr int kPlanes = F32 ? 6 : 1;           // products of planes for one of values
+    // Depth of a run (chunks of 64) whose sums stay in the tensor core.
+    constexpr int kRun = F32 ? 2 : MODE == kProducts ? (1 << 30) : 8;
+
+    if (warp < 4) {
+        tc5::registers_down<56>();
+        if (warp == 0 && tc5::elect_one()) {
+            // ---- loads: this CTA's operands; the even CTA's barrier counts both's bytes
+            const unsigned full0 = tc5::map_to(full, 0);
+            Walk<MODE> walk(a, cluster, clusters);
+            Item it;
+            int stage = 0;
+            unsigned phase = 0;
+            long long issued = 0;
+            bool ok = true;
+            while (ok && walk.next(it)) {
+                for (int r0 = it.k0; ok && r0 < it.k1; r0 += min(kRun, it.k1 - r0)) {
+                    const int len = min(kRun, it.k1 - r0);
+                    for (int i = 0; i < kPlanes * len; ++i) {
+                        const int chunk = r0 + (F32 ? i % len : i);
+                        int pa = 0, pb = 0;
+                        if (F32) planes_of(i / len, pa, pb);
+                        ok = tc5::wait_parity(empty + 8 * stage, phase ^ 1u);
+                        if (!ok) break;
+                        if (rank == 0) tc5::expect_bytes(full + 8 * stage, 2 * C::kStageBytes);
+                        const unsigned bar = full0 + 8 * stage, dst = smem0 + stage * C::kStageBytes;
+                        if (MODE != kProducts) {
+                            tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar);
+                            tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar);
+                        } else {
+                            if (it.problem == 0) {
+                                tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar);
+                            } else {
+                                for (int h = 0; h < 2; ++h)
+                                    tc5::load_box(dst + 8192 * h, &maps.m[2], it.m0 + 128 * rank + 64 * h, chunk * 64, pa, bar);
+                            }
+                            for (int b = 0; b < NB; ++b) {
+                                const int n = it.n0 + 256 * b + (int)rank * (block_columns(a, it, b) / 2);
+                                // the innermost coordinate starts on a 16-byte boundary: block_columns / 2 is a multiple of 16
+                                for (int h = 0; h < 2; ++h)
+                                    tc5::load_box(dst + kOperandBytes * (1 + b) + 8192 * h, &maps.m[it.problem == 0 ? 1 : 3],
+                                                  n + 64 * h, (it.problem == 0 ? a.v0 : 0) + chunk * 64, pb, bar);
+                            }
+                        }
+                        ++issued;
+                        if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+                    }
+                }
+            }
+            if (!ok) {
+                // Copies may still be under way into this pair's shared memory: wait
+                // for the stages issued last (bounded as every wait is).
+                raise_status(a.p.status, kStatusWaitTimeout);
+                if (rank == 0)
+                    for (int s = 0; s < C::kStages && s < issued; ++s) {
+                        const int st = (stage + C::kStages - 1 - s) % C::kStages;
+                        tc5::wait_parity(full + 8 * st, st < stage ? phase : phase ^ 1u);
+                    }
+            }
+        } else if (warp == 1 && rank == 0 && tc5::elect_one()) {
+            // ---- multiplications
+            Walk<MODE> walk(a, cluster, clusters);
+            Item it;
+            int stage = 0;
+            unsigned phase = 0, run = 0;
+            bool ok = true;
+            while (ok && walk.next(it)) {
+                const bool a_rows = MODE == kProducts && it.problem == 1, b_rows = MODE == kProducts;
+                unsigned idesc[NB];
+                int cols[NB];
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    cols[b] = MODE == kProducts ? block_columns(a, it, b) : 256;
+                    idesc[b] = tc5::instruction(cols[b], a_rows, b_rows);
+                }
+                const unsigned a_step = a_rows ? 128u : 2u, b_step = b_rows ? 128u : 2u;   // 16 of depth, in 16 bytes
+                for (int r0 = it.k0; ok && r0 < it.k1; r0 += min(kRun, it.k1 - r0), ++run) {
+                    const int len = min(kRun, it.k1 - r0);
+                    const unsigned buf = NB == 2 ? 0u : run & 1u, use = NB == 2 ? run : run >> 1;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) ok = ok && tc5::wait_parity(acc_empty + 8 * (buf + b), (use & 1u) ^ 1u);
+                    if (!ok) break;
+                    tc5::fence_after();
+                    for (int i = 0; i < kPlanes * len; ++i) {
+                        ok = tc5::wait_parity(full + 8 * stage, phase);
+                        if (!ok) break;
+                        tc5::fence_after();
+                        const unsigned src = smem0 + stage * C::kStageBytes;
+                        const unsigned long long da = tc5::descriptor(src, a_rows ? 8192u : 16u);
+#pragma unroll
+                        for (int b = 0; b < NB; ++b) {
+                            const unsigned long long db = tc5::descriptor(src + kOperandBytes * (1 + b), b_rows ? 8192u : 16u);
+                            if (cols[b] > 0) {
+#pragma unroll
+                                for (unsigned k = 0; k < 4; ++k)
+                                    tc5::multiply(tmem + 256 * (buf + b), da + a_step * k, db + b_step * k, idesc[b], i > 0 || k > 0);
+                            }
+                        }
+                        tc5::commit_pair(empty + 8 * stage);
+                        if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) tc5::commit_pair(acc_full + 8 * (buf + b));
+                }
+            }
+            if (!ok) raise_status(a.p.status, kStatusWaitTimeout);
+        } else if (MODE == kGradient && warp == 3 && blockIdx.x == 0) {
+            for (int i = lane; i < a.n_counters; i += 32) a.counters[i] = 0u;   // for the products that follow
+        }
+    } else {
+        tc5::registers_up<224>();
+        // ---- epilogue: 128 columns of one row per thread
+        const int ew = warp - 4, half = ew >> 2;
+        const int lane_row = (warp & 3) * 32 + lane;
+        const unsigned t_lane = tmem + ((unsigned)(warp & 3) << 21) + 128u * half;
+        const unsigned acc_empty0 = tc5::map_to(acc_empty, 0);
+        const unsigned stage_out = smem0 + C::kStages * C::kStageBytes + ew * 8192u;
+        Walk<MODE> walk(a, cluster, clusters);
+        Item it;
+        unsigned run = 0;
+        bool ok = true;
+        float m = -INFINITY, l = 0.f;
+        int target = kIgnored;
+        unsigned stores = 0;
+        while (walk.next(it)) {
+            const int row = it.m0 + 128 * (int)rank + lane_row;
+            float z2 = 0.f, z = 0.f, dl = 0.f;
+            if (MODE == kForward && it.first) {
+                m = -INFINITY;
+                l = 0.f;
+                target = row < a.p.N ? target_column(a.p, row) : kIgnored;
+            }
+            if (MODE == kGradient) {
+                target = row < a.p.N ? target_column(a.p, row) : kIgnored;
+                if (target >= 0) {
+                    z = a.lse[row];
+                    dl = a.dloss[row];
+                }
+                z2 = z * kLog2e;
+                if (target == kBad && a.v0 + it.n0 == 0 && half == 0) raise_status(a.p.status, kStatusTarget);
+            }
+#pragma unroll 1
+            for (int b = 0; b < NB; ++b) {
+                float acc[128];
+                const int runs = (it.k1 - it.k0 + kRun - 1) / kRun;
+                unsigned n_run = run;
+#pragma unroll 1
+                for (int r = 0; r < runs; ++r, ++n_run) {
+                    const unsigned buf = NB == 2 ? (unsigned)b : n_run & 1u, use = NB == 2 ? n_run : n_run >> 1;
+                    ok = ok && tc5::wait_parity(acc_full + 8 * buf, use & 1u);
+                    if (!ok) continue;
+                    tc5::fence_after();
+                    const unsigned t = t_lane + 256u * buf;
+                    if (r == 0) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) tc5::tmem_load32(t + 32 * q, acc + 32 * q);
+                        tc5::tmem_wait_loads();
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float v[32];
+                            tc5::tmem_load32(t + 32 * q, v);
+                            tc5::tmem_wait_loads();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) acc[32 * q + j] += v[j];
+                        }
+                    }
+                    tc5::fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc5::arrive_cluster(acc_empty0 + 8 * buf);
+                }
+                if (b == NB - 1) run = n_run;
+                if (!ok) {                          // the accumulators never came: every output of this tile is NaN
+                    if (lane == 0) raise_status(a.p.status, kStatusWaitTimeout);
+#pragma unroll
+                    for (int j = 0; j < 128; ++j) acc[j] = NAN;
+                }
+                const int c0 = it.n0 + 256 * b + 128 * half;
+
+                if (MODE == kForward) {
+                    if (c0 + 128 > a.p.V) {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j)
+                            if (c0 + j >= a.p.V) acc[j] = -INFINITY;
+                    }
+                    if ((unsigned)(target - c0) < 128u) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) s = c0 + j == target ? acc[j] : s;
+                        a.parts.target_logit[row] = s;
+                    }
+                    float mx[4] = {acc[0], acc[1], acc[2], acc[3]};
+#pragma unroll
+                    for (int j = 4; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], acc[j]);
+                    const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                    const float ms = top == -INFINITY ? 0.f : top;
+                    float s[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (F32) {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) s[j & 3] += expf(acc[j] - ms);
+                        l = l * expf(m - ms);
+                    } else {
+                        const float off = -ms * kLog2e;
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) s[j & 3] += ex2(fmaf(acc[j], kLog2e, off));
+                        l = l * ex2(fmaf(m, kLog2e, off));
+                    }
+                    l += (s[0] + s[1]) + (s[2] + s[3]);
+                    m = top;
+                    if (it.last && row < a.p.N) {
+                        const size_t at = (size_t)(2 * it.unit + half) * a.p.N + row;
+                        a.parts.m[at] = m;
+                        a.parts.l[at] = l;
+                    }
+                } else if (MODE == kGradient) {
+                    // a row without a target gives exact zeros, whatever its logits
+                    if (target < 0) {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) acc[j] = ok ? 0.f : NAN;
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j)
+                            acc[j] = dl * (F32 ? expf(acc[j] - z) : ex2(fmaf(acc[j], kLog2e, -z2)));
+                        const int local = target - a.v0 - c0;
+                        if ((unsigned)local < 128u) {
+#pragma unroll
+                            for (int j = 0; j < 128; ++j)
+                                if (j == local) acc[j] -= dl;
+                        }
+                    }
+                    const int r0 = it.m0 + 128 * (int)rank + (warp & 3) * 32;
+#pragma unroll
+                    for (int plane = 0; plane < (F32 ? 3 : 1); ++plane) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int col = c0 + 64 * h;
+                            if (r0 < a.p.N && col < a.cols) {        // (uniform over the warp)
+                                const unsigned dst = stage_out + 4096u * (stores & 1u);
+                                ++stores;
+                                if (lane == 0) tc5::store_wait_read<1>();
+                                __syncwarp();
+#pragma unroll
+                                for (int ch = 0; ch < 8; ++ch) {
+                                    unsigned u[4];
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const int j = 64 * h + 8 * ch + 2 * e;
+                                        u[e] = mma::pack_bf16(acc[j], acc[j + 1]);
+                                        if (F32) {           // what the next plane has to hold
+                                            acc[j] -= __uint_as_float(u[e] << 16);
+                                            acc[j + 1] -= __uint_as_float(u[e] & 0xffff0000u);
+                                        }
+                                    }
+                                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n"
+                                                 :: "r"(mma::row_chunk(dst, lane, ch)), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3])
+                                                 : "memory");
+                                }
+                                tc5::fence_async_smem();
+                                __syncwarp();
+                                if (lane == 0) {
+                                    tc5::store_box(&maps.m[2], dst, col, r0, plane);
+                                    tc5::store_commit();
+                                }
+                            }
+                        }
+                    }
+                } else if constexpr (MODE == kProducts) {
+                    if (c0 >= a.out_cols) continue;          // (uniform over the warp)
+                    finish_product<NB, F32>(a, it, walk, cluster, (int)rank, b, ew, lane, row, c0, acc);
+                }
+            }
+        }
+        if (MODE == kGradient && lane == 0) tc5::store_wait_all();
+    }
+    // Neither CTA leaves, or gives up its TMEM, while the other may still use it.
+    tc5::fence_before();
+    __syncwarp();
+    tc5::cluster_sync();
+    tc5::fence_after();
+    if (warp == 2) tc5::tmem_free(tmem);
+}
+
+// Rows of T as `planes` bf16 planes of row length `depth` (zeros past D): one
+// plane rounds nothing (bf16 rows of a length that TMA cannot address), three
+// hold an fp32 value to 24 bits.
+template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const T* src, long long rows, int D, int depth, int planes,
+                                                                         __nv_bfloat16* dst) {
+    grid_dependency_sync();
+    const long long pairs = rows * (depth / 2);
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < pairs; i += gridDim.x * 256ll) {
+        const long long r = i / (depth / 2);
+        const int c = (int)(i % (depth / 2)) * 2;
+        float x0 = c < D ? to_f(src[r * D + c]) : 0.f, x1 = c + 1 < D ? to_f(src[r * D + c + 1]) : 0.f;
+        for (int p = 0; p < planes; ++p) {
+            const unsigned u = mma::pack_bf16(x0, x1);
+            reinterpret_cast<unsigned*>(dst)[p * pairs + i] = u;
+            x0 -= __uint_as_float(u << 16);
+            x1 -= __uint_as_float(u & 0xffff0000u);
+        }
+    }
+}
+
+cudaError_t pack(const void* src, long long rows, int D, int depth, int planes, void* dst, bool bf16, cudaStream_t st) {
+    const long long pairs = rows * (depth / 2);
+    const dim3 grid((unsigned)std::max(1ll, std::min(pairs / 256 + 1, 152ll * 8)));
+    if (bf16)
+        return launch_kernel(pack_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, static_cast<const __nv_bfloat16*>(src), rows, D,
+                             depth, planes, static_cast<__nv_bfloat16*>(dst));
+    return launch_kernel(pack_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(src), rows, D, depth, planes,
+                         static_cast<__nv_bfloat16*>(dst));
+}
+
+bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, int planes, long long row_len, int box_cols,
+            int box_rows) {
+    auto fn = tensor_map_encoder();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)row_len * 2, (cuuint64_t)(rows * row_len) * 2};
+    cuuint32_t box[3] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE, int NB, bool F32> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
+    auto kern = xent_kernel<MODE, NB, F32>;
+    // The register split of the two halves of a block draws on what the block
+    // was launched with: refuse to launch a build that was given less.
+    static const int registers = [&] {
+        cudaFuncAttributes at{};
+        return cudaFuncGetAttributes(&at, kern) == cudaSuccess ? at.numRegs : 0;
+    }();
+    if (registers * kThreads < 56 * 128 + 224 * 256) return cudaErrorInvalidDeviceFunction;
+    constexpr unsigned smem = Config<MODE, NB>::kSmem;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+    return launch_kernel(kern, dim3(2 * clusters), dim3(kThreads), smem, st, a, maps);
+}
+
+int tiles256(long long n) { return (int)((n + 255) / 256); }
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Length, and need, of packed operand rows.
+void plan_operands(int D, bool bf16, bool* pack, int* planes, int* depth) {
+    *pack = !bf16 || D % 8 != 0;
+    *planes = bf16 ? 1 : 3;
+    *depth = (D + 7) / 8 * 8;
+}
+
+}  // namespace
+
+// The forward's unit: tiles of one row of tiles that a cluster takes in a row
+// before it writes its rows' statistics.  The fewest rounds over the clusters
+// win; at most 64 segments of the vocabulary, so that the statistics stay small.
+FwdPlan plan_forward(int N, int D, int V, bool bf16) {
+    FwdPlan f{};
+    plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
+    const int rt = tiles256(N), ct = tiles256(V);
+    double best = 0;
+    for (int u = std::max(1, (ct + 63) / 64); u <= std::max(16, (ct + 63) / 64); ++u) {
+        const int segs = (ct + u - 1) / u;
+        const long long units = (long long)rt * segs;
+        const double cost = (double)((units + kClusters - 1) / kClusters) * (u + 0.25);
+        if (f.unit_tiles == 0 || cost < best) {
+            best = cost;
+            f.unit_tiles = u;
+            f.segments = 2 * segs;
+        }
+    }
+    size_t off = 0;
+    const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };
+    f.x = take(f.pack ? (size_t)f.planes * N * f.depth * 2 : 0);
+    f.w = take(f.pack ? (size_t)f.planes * V * f.depth * 2 : 0);
+    f.m = take((size_t)f.segments * N * 4);
+    f.l = take((size_t)f.segments * N * 4);
+    f.target = take((size_t)N * 4);
+    f.total = off;
+    return f;
+}
+
+cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st) {
+    const void *x = p.x, *w = p.w;
+    cudaError_t e;
+    if (f.pack) {
+        ProfScope s("xent_pack", st);
+        if ((e = pack(p.x, p.N, p.D, f.depth, f.planes, ws + f.x, bf16, st)) != cudaSuccess) return e;
+        if ((e = pack(p.w, p.V, p.D, f.depth, f.planes, ws + f.w, bf16, st)) != cudaSuccess) return e;
+        x = ws + f.x;
+        w = ws + f.w;
+    }
+    Maps maps{};
+    if (!encode(&maps.m[0], x, f.depth, p.N, f.planes, f.depth, 64, 128) ||
+        !encode(&maps.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 128))
+        return cudaErrorInvalidValue;
+    Args a{};
+    a.p = p;
+    a.chunks = (p.D + 63) / 64;
+    a.row_tiles = tiles256(p.N);
+    a.col_tiles = tiles256(p.V);
+    a.unit_tiles = f.unit_tiles;
+    a.units = a.row_tiles * (f.segments / 2);
+    a.parts = FwdParts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l), reinterpret_cast<float*>(ws + f.target)};
+    const int clusters = std::min(kClusters, a.units);
+    {
+        ProfScope s("xent_fwd", st);
+        e = bf16 ? launch<kForward, 1, false>(a, maps, clusters, st) : launch<kForward, 1, true>(a, maps, clusters, st);
+    }
+    if (e != cudaSuccess) return e;
+    ProfScope s("xent_combine", st);
+    return launch_combine(p, a.parts, f.segments, loss, lse, st);
+}
+
+// g of a piece is held in memory for the two products: at most 256 MiB of it
+// (at least 256 columns).
+BwdPlan plan_backward(int N, int D, int V, bool bf16) {
+    BwdPlan f{};
+    plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
+    const long long fit = (256ll << 20) / (2ll * f.planes * std::max(N, 1)) / 256 * 256;
+    f.cols = (int)std::min<long long>(V, std::max(256ll, fit));
+    f.ldg = (f.cols + 7) / 8 * 8;
+    size_t off = 0;
+    const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };
+    const int nb = bf16 && D > 256 ? 2 : 1;
+    f.x = take(f.pack ? (size_t)f.planes * N * f.depth * 2 : 0);
+    f.w = take(f.pack ? (size_t)f.planes * V * f.depth * 2 : 0);
+    f.g = take((size_t)f.planes * N * f.ldg * 2);
+    f.dx_acc = take(f.cols < V ? (size_t)N * D * 4 : 0);
+    f.partials = take((size_t)kClusters * 2 * nb * 256 * 256 * 4);
+    f.counters = take((size_t)kClusters * 2 * nb * kEpilogueWarps * 4);
+    f.total = off;
+    return f;
+}
+
+cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16, const float* lse, const float* dloss, void* dx,
+                         void* dw, cudaStream_t st) {
+    const void *x = p.x, *w = p.w;
+    cudaError_t e;
+    if (f.pack) {
+        ProfScope s("xent_pack", st);
+        if ((e = pack(p.x, p.N, p.D, f.depth, f.planes, ws + f.x, bf16, st)) != cudaSuccess) return e;
+        if ((e = pack(p.w, p.V, p.D, f.depth, f.planes, ws + f.w, bf16, st)) != cudaSuccess) return e;
+        x = ws + f.x;
+        w = ws + f.w;
+    }
+    const int nb = bf16 && p.D > 256 ? 2 : 1;
+    Maps logits{}, products{};
+    if (!encode(&logits.m[0], x, f.depth, p.N, f.planes, f.depth, 64, 128) ||
+        !encode(&logits.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 128) ||
+        !encode(&products.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 64) ||
+        !encode(&products.m[3], x, f.depth, p.N, f.planes, f.depth, 64, 64))
+        return cudaErrorInvalidValue;
+    Args a{};
+    a.p = p;
+    a.lse = lse;
+    a.dloss = dloss;
+    a.out_cols = p.D;
+    a.tile_cols = 256 * nb;
+    a.snap = bf16 ? 16 : 4;
+    a.partials = reinterpret_cast<float*>(ws + f.partials);
+    a.counters = reinterpret_cast<unsigned*>(ws + f.counters);
+    a.n_counters = kClusters * 2 * nb * kEpilogueWarps;
+    a.dx_acc = reinterpret_cast<float*>(ws + f.dx_acc);
+    a.dx = dx;
+    a.dw = dw;
+    for (int v0 = 0; v0 < p.V; v0 += f.cols) {
+        const int cols = std::min(f.cols, p.V - v0);
+        if (!encode(&logits.m[2], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 32) ||
+            !encode(&products.m[0], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 128) ||
+            !encode(&products.m[2], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 64))
+            return cudaErrorInvalidValue;
+        a.v0 = v0;
+        a.cols = cols;
+        a.chunks = (p.D + 63) / 64;
+        a.row_tiles = tiles256(p.N);
+        a.col_tiles = tiles256(cols);
+        a.units = a.row_tiles * a.col_tiles;
+        {
+            ProfScope s("xent_grad", st);
+            const int clusters = std::min(kClusters, a.units);
+            e = bf16 ? launch<kGradient, 1, false>(a, logits, clusters, st) : launch<kGradient, 1, true>(a, logits, clusters, st);
+        }
+        if (e != cudaSuccess) return e;
+        const int d_tiles = (p.D + a.tile_cols - 1) / a.tile_cols;
+        a.prob[0] = Product{p.N, d_tiles, (cols + 63) / 64};
+        a.prob[1] = Product{cols, d_tiles, (p.N + 63) / 64};
+        a.split = tiles256(p.N) * d_tiles * a.prob[0].chunks;
+        a.total = a.split + tiles256(cols) * d_tiles * a.prob[1].chunks;
+        a.dx_add = v0 > 0;
+        a.dx_done = v0 + cols >= p.V;
+        {
+            ProfScope s("xent_products", st);
+            e = !bf16 ? launch<kProducts, 1, true>(a, products, kClusters, st)
+                : nb == 2 ? launch<kProducts, 2, false>(a, products, kClusters, st)
+                          : launch<kProducts, 1, false>(a, products, kClusters, st);
+        }
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace xent
+}  // namespace fibattn

@@ -1,0 +1,64 @@
+// xent_mma.cuh -- host/device interface of the tensor-core cross entropy.
+#pragma once
+#include <cuda.h>
+
+#include "xent.cuh"
+
+namespace fibattn {
+namespace xent {
+
+constexpr int kClusters = 76;                      // CTA pairs of a GB300 (152 SMs)
+
+// One product of the backward: rows x (the tile's) columns, depth in chunks of 64.
+struct Product {
+    int rows, col_tiles, chunks;
+};
+
+struct Args {
+    Problem p;
+    // forward and gradient: tiles of 256 x 256, depth in chunks of 64.  A unit
+    // of the forward is unit_tiles tiles of one row of tiles.
+    int chunks, row_tiles, col_tiles, unit_tiles, units;
+    FwdParts parts;
+    const float* lse;
+    const float* dloss;
+    int v0, cols;                                  // the piece of the vocabulary
+    // products: the chunks of all tiles of prob[0] (dx), then of prob[1] (dw),
+    // one after another, make `total`; prob[1] starts at `split`
+    Product prob[2];
+    int split, total, snap;
+    int tile_cols, out_cols;                       // columns of a tile, of the results (D)
+    float* partials;                               // sums over a part of a tile's depth
+    unsigned* counters;                            // parts of a tile that have arrived
+    int n_counters;
+    float* dx_acc;                                 // dx over the earlier pieces, fp32
+    bool dx_add, dx_done;                          // there are earlier pieces; this is the last one
+    void* dx;
+    void* dw;
+};
+
+struct Maps {
+    CUtensorMap m[4];
+};
+
+struct FwdPlan {
+    bool pack;
+    int planes, depth;                             // of packed operands: planes, row length
+    int unit_tiles, segments;                      // segments: entries of a row in FwdParts
+    size_t x, w, m, l, target, total;              // workspace offsets
+};
+FwdPlan plan_forward(int N, int D, int V, bool bf16);
+cudaError_t run_forward(const Problem& p, const FwdPlan& plan, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st);
+
+struct BwdPlan {
+    bool pack;
+    int planes, depth;
+    int cols, ldg;                                 // columns of a piece; row length of g
+    size_t x, w, g, dx_acc, partials, counters, total;
+};
+BwdPlan plan_backward(int N, int D, int V, bool bf16);
+cudaError_t run_backward(const Problem& p, const BwdPlan& plan, char* ws, bool bf16, const float* lse, const float* dloss,
+                         void* dx, void* dw, cudaStream_t st);
+
+}  // namespace xent
+}  // namespace fibattn
