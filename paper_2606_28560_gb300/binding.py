@@ -7,6 +7,7 @@ a call returns a non-OK status -- there is no fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
 import os
@@ -372,21 +373,33 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
 
 # ------------------------------------------- loss head, gradient clipping ----
 
-def _check_xent(x, w, targets, ignore_index):
-    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1] or targets.shape != x.shape[:1]:
+# The current stream of a device by its index, without the Stream object that
+# torch.cuda.current_stream() builds (some 4 us of every call).
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    lambda index: torch.cuda.current_stream(index).cuda_stream
+
+
+def _stream_of(stream, index: int) -> int:
+    return int(stream.cuda_stream) if stream is not None else _raw_stream(index)
+
+
+def _check_xent(x, w, targets):
+    if x.dim() != 2 or w.dim() != 2 or targets.dim() != 1:
         raise ValueError("linear cross entropy takes x [N, D], w [V, D] and targets [N]")
-    for t in (x, w):
-        if not (t.is_cuda and t.is_contiguous() and t.dtype == x.dtype):
-            raise ValueError("x and w must be contiguous CUDA tensors of one dtype")
-    if not (targets.is_cuda and targets.is_contiguous() and targets.dtype == torch.int64):
+    (N, D), (V, Dw), dtype, index = x.shape, w.shape, x.dtype, x.get_device()
+    if Dw != D or targets.shape[0] != N:
+        raise ValueError("linear cross entropy takes x [N, D], w [V, D] and targets [N]")
+    if index < 0 or w.dtype != dtype or w.get_device() < 0 or not (x.is_contiguous() and w.is_contiguous()):
+        raise ValueError("x and w must be contiguous CUDA tensors of one dtype")
+    if targets.get_device() < 0 or targets.dtype != torch.int64 or not targets.is_contiguous():
         raise ValueError("targets must be a contiguous CUDA int64 tensor")
-    if x.device != w.device or x.device != targets.device:
+    if w.get_device() != index or targets.get_device() != index:
         raise ValueError("x, w and targets must be on one device")
-    return x.shape[0], x.shape[1], w.shape[0], _dtype_code(x)
+    return N, D, V, _dtype_code(x), index
 
 
-def _f32_row(t, N, device, name):
-    if not (t.is_cuda and t.is_contiguous() and t.dtype == torch.float32 and t.shape == (N,) and t.device == device):
+def _f32_row(t, N, index, name):
+    if t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != N or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous fp32 tensor of N values on x's device")
     return t
 
@@ -397,15 +410,16 @@ def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=N
     contiguous), targets [N] int64; rows whose target is ``ignore_index`` have
     loss 0.  Returns (loss [N], lse [N]) in fp32; ``lse`` goes to
     ``linear_xent_bwd``."""
-    N, D, V, code = _check_xent(x, w, targets, ignore_index)
-    loss = x.new_empty(N, dtype=torch.float32) if loss is None else _f32_row(loss, N, x.device, "loss")
-    lse = x.new_empty(N, dtype=torch.float32) if lse is None else _f32_row(lse, N, x.device, "lse")
+    N, D, V, code, index = _check_xent(x, w, targets)
+    loss = torch.empty(N, dtype=torch.float32, device=x.device) if loss is None else _f32_row(loss, N, index, "loss")
+    lse = torch.empty_like(loss) if lse is None else _f32_row(lse, N, index, "lse")
+    L = lib()
     if workspace is None:                        # (a given workspace's size is checked by the library)
-        need = lib().fibattn_linear_xent_fwd_workspace_bytes(N, D, V, code)
-        workspace = x.new_empty(max(need, 256), dtype=torch.uint8)
-    _check(lib().fibattn_linear_xent_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(),
-                                         lse.data_ptr(), N, D, V, int(ignore_index), code, workspace.data_ptr(),
-                                         workspace.numel(), _stream_ptr(stream)))
+        need = L.fibattn_linear_xent_fwd_workspace_bytes(N, D, V, code)
+        workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
+    _check(L.fibattn_linear_xent_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+                                     N, D, V, ignore_index, code, workspace.data_ptr(), workspace.numel(),
+                                     _stream_of(stream, index)))
     return loss, lse
 
 
@@ -414,21 +428,25 @@ def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=N
     """Gradients of ``sum(dloss * loss)`` by x and w (fibattn_linear_xent_bwd).
     lse [N] from ``linear_xent_fwd`` of the same inputs; dloss [N] fp32.
     Returns (dx [N, D], dw [V, D]) in x's dtype."""
-    N, D, V, code = _check_xent(x, w, targets, ignore_index)
-    _f32_row(lse, N, x.device, "lse")
-    _f32_row(dloss, N, x.device, "dloss")
-    dx = torch.empty_like(x) if dx is None else dx
-    dw = torch.empty_like(w) if dw is None else dw
-    for t, of in ((dx, x), (dw, w)):
-        if not (t.is_contiguous() and t.dtype == of.dtype and t.shape == of.shape and t.device == of.device):
-            raise ValueError("dx and dw must be contiguous tensors like x and w")
+    N, D, V, code, index = _check_xent(x, w, targets)
+    _f32_row(lse, N, index, "lse")
+    _f32_row(dloss, N, index, "dloss")
+    dx = torch.empty_like(x) if dx is None else _grad_like(dx, x)
+    dw = torch.empty_like(w) if dw is None else _grad_like(dw, w)
+    L = lib()
     if workspace is None:
-        need = lib().fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
-        workspace = x.new_empty(max(need, 256), dtype=torch.uint8)
-    _check(lib().fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(),
-                                         dloss.data_ptr(), dx.data_ptr(), dw.data_ptr(), N, D, V, int(ignore_index),
-                                         code, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+        need = L.fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
+        workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
+    _check(L.fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
+                                     dx.data_ptr(), dw.data_ptr(), N, D, V, ignore_index, code, workspace.data_ptr(),
+                                     workspace.numel(), _stream_of(stream, index)))
     return dx, dw
+
+
+def _grad_like(t, of):
+    if t.dtype != of.dtype or t.shape != of.shape or t.get_device() != of.get_device() or not t.is_contiguous():
+        raise ValueError("dx and dw must be contiguous tensors like x and w")
+    return t
 
 
 _CLIP_CODE = {torch.float32: FIBATTN_F32, torch.bfloat16: FIBATTN_BF16}
@@ -449,35 +467,37 @@ def grad_norm(grads, *, norm=None, workspace=None, stream=None):
 
 
 def _clip(grads, max_norm, out, norm, workspace, stream, scale):
+    # (a model has hundreds of tensors: each is looked at with as few calls as will do)
     n = len(grads)
     outs = grads if out is None else list(out)
     if len(outs) != n:
         raise ValueError("out must hold one tensor for each gradient")
-    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
-    try:
-        codes = [_CLIP_CODE[t.dtype] for t in grads]
-    except KeyError:
-        raise TypeError("unsupported dtype: fp32 or bf16") from None
+    index = grads[0].get_device() if n else torch.cuda.current_device()
+    dtypes = [t.dtype for t in grads]
+    if not _CLIP_CODE.keys() >= set(dtypes):
+        raise TypeError("unsupported dtype: fp32 or bf16")
+    codes = [_CLIP_CODE[d] for d in dtypes]
     sizes = [t.numel() for t in grads]
-    for t in grads:
-        if not (t.is_cuda and t.is_contiguous() and t.device == device):
-            raise ValueError("gradients must be contiguous CUDA tensors on one device")
-    if out is not None:
-        for t, g, m in zip(outs, grads, sizes):
-            if not (t.is_cuda and t.is_contiguous() and t.device == device and t.dtype == g.dtype and t.numel() == m):
-                raise ValueError("out must hold contiguous tensors like the gradients")
+    if index < 0 or n and {t.get_device() for t in grads} != {index} or not all([t.is_contiguous() for t in grads]):
+        raise ValueError("gradients must be contiguous CUDA tensors on one device")
+    if out is not None and n:
+        if [t.dtype for t in outs] != dtypes or [t.numel() for t in outs] != sizes or \
+                {t.get_device() for t in outs} != {index} or not all([t.is_contiguous() for t in outs]):
+            raise ValueError("out must hold contiguous tensors like the gradients")
+    device = grads[0].device if n else torch.device("cuda", index)
     if norm is None:
         norm = torch.empty((), dtype=torch.float32, device=device)
-    elif not (norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1 and norm.device == device):
+    elif norm.dtype != torch.float32 or norm.numel() != 1 or norm.get_device() != index:
         raise ValueError("norm must be one fp32 value on the gradients' device")
+    L = lib()
     if workspace is None:
-        workspace = torch.empty(max(lib().fibattn_clip_grads_workspace_bytes(n), 256), dtype=torch.uint8,
-                                device=device)
-    ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in grads])
-    optrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in outs]) if scale else None
-    _check(lib().fibattn_clip_grads(n, ptrs, optrs, (ctypes.c_longlong * n)(*sizes), (ctypes.c_int * n)(*codes),
-                                    max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                    _stream_ptr(stream)))
+        workspace = torch.empty(L.fibattn_clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
+    arrays = [array.array("Q", [t.data_ptr() for t in grads]),
+              array.array("Q", [t.data_ptr() for t in outs]) if scale else None,
+              array.array("q", sizes), array.array("i", codes)]
+    at = [a.buffer_info()[0] if a is not None else None for a in arrays]
+    _check(L.fibattn_clip_grads(n, *at, max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                _stream_of(stream, index)))
     return norm
 
 

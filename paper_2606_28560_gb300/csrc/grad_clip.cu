@@ -19,8 +19,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 16384;              // values of a chunk: 64 of each thread
-constexpr int kBlocks = 152 * 4;           // blocks of a launch, at most
+constexpr int kResident = 4;               // blocks of an SM
+constexpr int kBlocks = 152 * kResident;   // blocks of a launch, at most
 constexpr int kTable = 512;                // tensors of a launch, at most
+constexpr int kShort = 48;                 // tensors of a short table (a launch carries its whole table)
 constexpr long long kMaxChunks = 1ll << 30;
 
 struct Entry {
@@ -30,14 +32,14 @@ struct Entry {
     int first_chunk;                       // of the launch's chunks
     int bf16;
 };
-struct Table {
+template <int N> struct Table {
     int entries, chunks;
-    Entry e[kTable];
+    Entry e[N];
 };
 
 // The entry that chunk c belongs to: the last one with first_chunk <= c
 // (entries without values have no chunk).
-__device__ __forceinline__ int entry_of(const Table& t, int c) {
+template <int N> __device__ __forceinline__ int entry_of(const Table<N>& t, int c) {
     int lo = 0, hi = t.entries - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) / 2;
@@ -47,13 +49,51 @@ __device__ __forceinline__ int entry_of(const Table& t, int c) {
     return lo;
 }
 
-template <typename T> __device__ __forceinline__ float sum_squares(const T* p, int n) {
-    float s = 0.f;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const float x = to_f(p[i]);
-        s = fmaf(x, x, s);
+// A run of n values is taken in vectors of 16 bytes between its first and last
+// 16-byte boundary, and value by value before and after.
+template <typename T> __device__ __forceinline__ int head_of(const T* p, int n) {
+    return min(n, (int)(((16u - ((unsigned)(uintptr_t)p & 15u)) & 15u) / sizeof(T)));
+}
+
+template <typename T> struct Vector {
+    static constexpr int kValues = 16 / sizeof(T);
+    uint4 u;
+    __device__ __forceinline__ float get(int i) const {
+        const unsigned* w = &u.x;
+        if (sizeof(T) == 4) return __uint_as_float(w[i]);
+        return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
     }
-    return s;
+};
+
+constexpr int kNormBatch = 8, kClipBatch = 4;   // vectors that a thread has under way at a time
+
+template <typename T> __device__ __forceinline__ float sum_squares(const T* p, int n) {
+    using V = Vector<T>;
+    const int head = head_of(p, n), vectors = (n - head) / V::kValues, tail = head + vectors * V::kValues;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if ((int)threadIdx.x < head) {         // (head and tail hold fewer than 8 values)
+        const float x = to_f(p[threadIdx.x]);
+        s[0] = x * x;
+    }
+    if (tail + (int)threadIdx.x < n) {
+        const float x = to_f(p[tail + threadIdx.x]);
+        s[1] = x * x;
+    }
+    const uint4* body = reinterpret_cast<const uint4*>(p + head);
+    for (int i = threadIdx.x; i < vectors; i += kNormBatch * kThreads) {
+        V v[kNormBatch];
+#pragma unroll
+        for (int k = 0; k < kNormBatch; ++k)
+            v[k].u = i + k * kThreads < vectors ? __ldg(body + i + k * kThreads) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < kNormBatch; ++k)
+#pragma unroll
+            for (int j = 0; j < V::kValues; ++j) {
+                const float x = v[k].get(j);
+                s[j & 3] = fmaf(x, x, s[j & 3]);
+            }
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
 }
 
 __device__ double block_sum(double s, double* red) {
@@ -68,7 +108,8 @@ __device__ double block_sum(double s, double* red) {
 }
 
 // partial[b]: block b's sum of squares over its chunks b, b + gridDim, ...
-__global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ Table t, double* partial) {
+template <int N>
+__global__ void __launch_bounds__(kThreads, kResident) norm_kernel(const __grid_constant__ Table<N> t, double* partial) {
     __shared__ double red[kThreads / 32];
     grid_dependency_sync();
     double s = 0.0;
@@ -83,16 +124,55 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const __grid_constant__ 
     if (threadIdx.x == 0) partial[blockIdx.x] = r;
 }
 
-__device__ __forceinline__ void scale(const float* in, float* out, int n, float c) {
-    for (int i = threadIdx.x; i < n; i += kThreads) out[i] = in[i] * c;
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16(x); }
+__device__ __forceinline__ uint4 scaled(const Vector<float>& v, float c) {
+    return make_uint4(__float_as_uint(v.get(0) * c), __float_as_uint(v.get(1) * c), __float_as_uint(v.get(2) * c),
+                      __float_as_uint(v.get(3) * c));
 }
-__device__ __forceinline__ void scale(const __nv_bfloat16* in, __nv_bfloat16* out, int n, float c) {
-    for (int i = threadIdx.x; i < n; i += kThreads) out[i] = __float2bfloat16(to_f(in[i]) * c);
+__device__ __forceinline__ uint4 scaled(const Vector<__nv_bfloat16>& v, float c) {
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v.get(2 * i) * c, v.get(2 * i + 1) * c);
+        w[i] = *reinterpret_cast<const unsigned*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// (in == out is allowed: a thread reads a value before it writes it, and no other does.)
+template <typename T> __device__ __forceinline__ void scale(const T* in, T* out, int n, float c) {
+    using V = Vector<T>;
+    const bool together = (((uintptr_t)in ^ (uintptr_t)out) & 15u) == 0;
+    const int head = together ? head_of(in, n) : 0;
+    const int vectors = together ? (n - head) / V::kValues : 0, tail = head + vectors * V::kValues;
+    if ((int)threadIdx.x < head) put(out + threadIdx.x, to_f(in[threadIdx.x]) * c);
+    const uint4* body = reinterpret_cast<const uint4*>(in + head);
+    uint4* to = reinterpret_cast<uint4*>(out + head);
+    for (int i = threadIdx.x; i < vectors; i += kClipBatch * kThreads) {
+        V v[kClipBatch];
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k)
+            if (i + k * kThreads < vectors) v[k].u = __ldcs(body + i + k * kThreads);
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k)
+            if (i + k * kThreads < vectors) __stcs(to + i + k * kThreads, scaled(v[k], c));
+    }
+    // the tail, or everything where in and out start at different offsets within 16 bytes
+    for (int i = tail + threadIdx.x; i < n; i += kClipBatch * kThreads) {
+        float x[kClipBatch];
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k) x[k] = i + k * kThreads < n ? to_f(in[i + k * kThreads]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k)
+            if (i + k * kThreads < n) put(out + i + k * kThreads, x[k] * c);
+    }
 }
 
 // Every block adds up all partials, in the same order, and scales its chunks.
-__global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ Table t, const double* partial, int partials,
-                                                        float max_norm, float* norm) {
+template <int N>
+__global__ void __launch_bounds__(kThreads, kResident) clip_kernel(const __grid_constant__ Table<N> t, const double* partial,
+                                                                   int partials, float max_norm, float* norm) {
     __shared__ double red[kThreads / 32];
     grid_dependency_sync();
     double s = 0.0;
@@ -101,7 +181,8 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = total;
     // a norm that is NaN stays NaN
     const float q = max_norm / (total + 1e-6f), coef = q > 1.f ? 1.f : q;
-    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    // from the last chunk to the first: the norm's pass read the last ones last, and L2 still holds them
+    for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const Entry& e = t.e[entry_of(t, c)];
         if (e.out == e.in && coef == 1.f) continue;
         const long long at = (long long)(c - e.first_chunk) * kChunk;
@@ -113,7 +194,8 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ 
 
 int tables_of(int n) { return n > kTable ? (n + kTable - 1) / kTable : 1; }
 
-void fill(Table* t, int first, int last, const void* const* grads, void* const* outs, const long long* numels,
+template <int N>
+void fill(Table<N>* t, int first, int last, const void* const* grads, void* const* outs, const long long* numels,
           const int* dtypes) {
     t->entries = last - first;
     long long chunks = 0;
@@ -127,6 +209,46 @@ void fill(Table* t, int first, int last, const void* const* grads, void* const* 
         chunks += (numels[i] + kChunk - 1) / kChunk;
     }
     t->chunks = (int)chunks;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t start(void (*kern)(KArgs...), int grid, cudaStream_t st, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 1 : 0;
+    void* at[] = {const_cast<void*>(static_cast<const void*>(&args))...};   // (the tables are not copied on the way)
+    return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kern), at);
+}
+
+template <int N>
+cudaError_t run(int n, const void* const* grads, void* const* outs, const long long* numels, const int* dtypes, float max_norm,
+                float* norm, double* partial, cudaStream_t st) {
+    const int tables = n > N ? (n + N - 1) / N : 1;
+    static thread_local Table<N> t;
+    int partials = 0;
+    cudaError_t e = cudaSuccess;
+    for (int k = 0; k < tables && e == cudaSuccess; ++k) {
+        fill(&t, k * N, std::min(n, (k + 1) * N), grads, outs, numels, dtypes);
+        const int grid = std::max(1, std::min(kBlocks, t.chunks));
+        ProfScope s("grad_norm", st);
+        e = start(norm_kernel<N>, grid, st, t, partial + partials);
+        partials += grid;
+    }
+    for (int k = 0; k < (outs ? tables : 1) && e == cudaSuccess; ++k) {
+        if (tables > 1) fill(&t, k * N, std::min(n, (k + 1) * N), grads, outs, numels, dtypes);
+        if (!outs) t.chunks = 0;                 // the norm alone
+        const int grid = std::max(1, std::min(kBlocks, t.chunks));
+        ProfScope s("grad_clip", st);
+        e = start(clip_kernel<N>, grid, st, t, static_cast<const double*>(partial), partials, max_norm,
+                  k == 0 ? norm : static_cast<float*>(nullptr));
+    }
+    return e;
 }
 
 }  // namespace
@@ -169,25 +291,8 @@ int fibattn_clip_grads(int n, const void* const* grads, void* const* outs, const
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     double* partial = static_cast<double*>(workspace);
-    const int tables = tables_of(n);
-    int partials = 0;
-    static thread_local Table t;
-    cudaError_t e = cudaSuccess;
-    for (int k = 0; k < tables && e == cudaSuccess; ++k) {
-        fill(&t, k * kTable, std::min(n, (k + 1) * kTable), grads, outs, numels, dtypes);
-        const int grid = std::max(1, std::min(kBlocks, t.chunks));
-        ProfScope s("grad_norm", st);
-        e = launch_kernel(norm_kernel, dim3(grid), dim3(kThreads), 0, st, t, partial + partials);
-        partials += grid;
-    }
-    for (int k = 0; k < tables && e == cudaSuccess; ++k) {
-        fill(&t, k * kTable, std::min(n, (k + 1) * kTable), grads, outs, numels, dtypes);
-        const int grid = outs ? std::max(1, std::min(kBlocks, t.chunks)) : 1;
-        if (!outs) t.chunks = 0;
-        ProfScope s("grad_clip", st);
-        e = launch_kernel(clip_kernel, dim3(grid), dim3(kThreads), 0, st, t, partial, partials, max_norm, k == 0 ? norm : nullptr);
-        if (!outs) break;
-    }
+    const cudaError_t e = n <= kShort ? run<kShort>(n, grads, outs, numels, dtypes, max_norm, norm, partial, st)
+                                      : run<kTable>(n, grads, outs, numels, dtypes, max_norm, norm, partial, st);
     if (e != cudaSuccess) return set_errorf(FIBATTN_ERR_CUDA, "gradient clipping launch: %s", cudaGetErrorString(e));
     return FIBATTN_OK;
 }

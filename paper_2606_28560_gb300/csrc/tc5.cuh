@@ -50,8 +50,11 @@ __device__ __forceinline__ void init_barrier(unsigned bar, unsigned count) {
 __device__ __forceinline__ void expect_bytes(unsigned bar, unsigned bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" :: "r"(bar), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void arrive_cluster(unsigned bar) {       // bar: a cluster-window address
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" :: "r"(bar) : "memory");
+// bar: a cluster-window address.  Relaxed: what it hands over is TMEM, ordered
+// by fence_before / fence_after; a release at cluster scope would wait for
+// every global access of the thread as well.
+__device__ __forceinline__ void arrive_cluster(unsigned bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" :: "r"(bar) : "memory");
 }
 
 // TMA load of a box into this CTA's shared memory; its bytes are counted by a

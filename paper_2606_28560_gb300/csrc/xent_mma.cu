@@ -16,7 +16,10 @@
 // for each 16 of depth), so a long depth is cut into runs whose sums are added
 // in registers: 512 deep for bf16 logits, whose loss and lse are fp32 results.
 // The products of bf16 gradients, rounded to 8 bits at the end, are not cut.
+// fp32 operands are sums of three bf16 planes ("wide" below: several planes,
+// runs of 128, CUDA's expf).
 #include <algorithm>
+#include <atomic>
 
 #include "tc5.cuh"
 #include "xent.cuh"
@@ -35,8 +38,8 @@ enum Mode { kForward, kGradient, kProducts };
 
 template <int MODE, int NB> struct Config {
     static constexpr unsigned kStageBytes = kOperandBytes * (1 + NB);
-    static constexpr int kStages = NB == 2 ? 4 : MODE == kGradient ? 5 : 6;
-    static constexpr unsigned kStoreBytes = MODE == kGradient ? kEpilogueWarps * 2 * 4096 : 0;   // two 32 x 64 boxes a warp
+    static constexpr int kStages = NB == 2 ? 4 : MODE == kGradient ? 6 : 7;
+    static constexpr unsigned kStoreBytes = MODE == kGradient ? kEpilogueWarps * 4096 : 0;   // a 32 x 64 box a warp
     static constexpr unsigned kSmem = kStages * kStageBytes + kStoreBytes + 1024;
 };
 
@@ -45,8 +48,8 @@ template <int MODE, int NB> struct Config {
 struct Item {
     int m0, n0, k0, k1;
     int problem;                                   // products: 0 dx, 1 dw
-    int unit;                                      // forward: segment of the vocabulary
-    bool first, last;                              // forward: of its unit
+    int unit;                                      // forward, gradient: segment of the columns
+    bool first, last;                              // forward, gradient: tile of its unit
     bool whole;                                    // products: the whole depth
     int tile_lo, tile_hi;                          // products: the tile's range of the iteration space
 };
@@ -75,7 +78,7 @@ template <int MODE> struct Walk {
         return b;
     }
     __device__ bool next(Item& it) {
-        if (MODE == kForward) {
+        if (MODE != kProducts) {
             if (at >= a.units) return false;
             const int mt = at % a.row_tiles, s = at / a.row_tiles;
             const int lo = s * a.unit_tiles, hi = min(a.col_tiles, lo + a.unit_tiles);
@@ -88,14 +91,6 @@ template <int MODE> struct Walk {
             it.last = lo + sub + 1 >= hi;
             if (it.last) { sub = 0; at += clusters; }
             else ++sub;
-            return true;
-        } else if (MODE == kGradient) {
-            if (at >= a.units) return false;
-            it.m0 = (at % a.row_tiles) * 256;
-            it.n0 = (at / a.row_tiles) * 256;
-            it.k0 = 0;
-            it.k1 = a.chunks;
-            at += clusters;
             return true;
         } else {
             if (at >= end) return false;
@@ -119,20 +114,6 @@ template <int MODE> struct Walk {
 // Columns of block b of a product's tile that are multiplied: a multiple of 32.
 __device__ __forceinline__ int block_columns(const Args& a, const Item& it, int b) {
     return min(256, max(0, (a.out_cols - it.n0 - 256 * b + 31) & ~31));
-}
-
-// fp32 operands are sums of three bf16 planes; six of the nine products of
-// planes are kept (the others are below 2^-24), the small ones first: while
-// the running sum is small so is what truncation takes from it.
-__device__ __forceinline__ void planes_of(int combo, int& pa, int& pb) {
-    switch (combo) {
-    case 0: pa = 0; pb = 2; break;
-    case 1: pa = 2; pb = 0; break;
-    case 2: pa = 1; pb = 1; break;
-    case 3: pa = 0; pb = 1; break;
-    case 4: pa = 1; pb = 0; break;
-    default: pa = 0; pb = 0; break;
-    }
 }
 
 // 128 columns of one output row from registers.  `aligned`: rows start on
@@ -160,64 +141,89 @@ __device__ __forceinline__ void put_row(__nv_bfloat16* out, const float* v, int 
     }
 }
 
-// A product's sums leave the tile: at once where the tile's whole depth is in
-// them; else to this cluster's slot of partial sums, and the warp that finds
-// itself last adds the parts up in the order of the depth (so the result does
-// not depend on which one is last) and writes the row.
-template <int NB, bool F32>
-__device__ __forceinline__ void finish_product(const Args& a, const Item& it, const Walk<kProducts>& walk, int cluster, int rank,
-                                               int b, int ew, int lane, int row, int c0, float* acc) {
-    if (!it.whole) {
-        const auto slot = [&](int c) {
-            const size_t s = 2 * (size_t)c + (walk.bound(c) >= it.tile_lo ? 0 : 1);
-            return a.partials + (((s * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + lane;
-        };
-        float* mine = slot(cluster);
-#pragma unroll
-        for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
-        __threadfence();
-        __syncwarp();
-        int lo = cluster, hi = cluster, parts = 0;
-        while (walk.bound(lo) > it.tile_lo) --lo;
-        while (walk.bound(hi + 1) < it.tile_hi) ++hi;
-        for (int c = lo; c <= hi; ++c) parts += walk.bound(c + 1) > walk.bound(c);
-        unsigned before = 0;
-        if (lane == 0) before = atomicAdd(a.counters + ((lo * 2 + rank) * NB + b) * kEpilogueWarps + ew, 1u);
-        if ((int)__shfl_sync(0xffffffffu, before, 0) != parts - 1) return;
-        __threadfence();
-#pragma unroll
-        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-        for (int c = lo; c <= hi; ++c) {
-            if (walk.bound(c + 1) <= walk.bound(c)) continue;
-            const float* p = slot(c);
-#pragma unroll
-            for (int j = 0; j < 128; ++j) acc[j] += __ldcg(p + 32 * j);
-        }
-    }
-    if (row >= a.prob[it.problem].rows) return;
+// Row `row`, columns from c0 of a finished product.  What g was divided by is
+// multiplied back here.
+template <bool WIDE>
+__device__ __forceinline__ void write_product(const Args& a, int problem, int row, int c0, float scale, float* acc) {
+    if (row >= a.prob[problem].rows) return;
     const int n = a.out_cols - c0;
     const size_t at = (size_t)row * a.out_cols + c0;
     const bool al4 = a.out_cols % 4 == 0;
-    if (it.problem == 0) {
+#pragma unroll
+    for (int j = 0; j < 128; ++j) acc[j] *= scale;
+    if (problem == 0) {
         if (a.dx_add) {
             const float* p = a.dx_acc + at;
+            if (al4) {
 #pragma unroll
-            for (int j = 0; j < 128; ++j)
-                if (j < n) acc[j] += p[j];
+                for (int j = 0; j < 128; j += 4)
+                    if (j < n) {
+                        const float4 v = *reinterpret_cast<const float4*>(p + j);
+                        acc[j] += v.x; acc[j + 1] += v.y; acc[j + 2] += v.z; acc[j + 3] += v.w;
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 128; ++j)
+                    if (j < n) acc[j] += p[j];
+            }
         }
         if (!a.dx_done) {
             put_row(a.dx_acc + at, acc, n, al4);
             return;
         }
     }
-    void* out = it.problem == 0 ? a.dx : a.dw;
-    if (F32) put_row(static_cast<float*>(out) + (it.problem == 0 ? at : at + (size_t)a.v0 * a.out_cols), acc, n, al4);
-    else put_row(static_cast<__nv_bfloat16*>(out) + (it.problem == 0 ? at : at + (size_t)a.v0 * a.out_cols), acc, n, a.out_cols % 8 == 0);
+    void* out = problem == 0 ? a.dx : a.dw;
+    const size_t to = problem == 0 ? at : at + (size_t)a.v0 * a.out_cols;
+    if (WIDE && a.out_f32) put_row(static_cast<float*>(out) + to, acc, n, al4);
+    else put_row(static_cast<__nv_bfloat16*>(out) + to, acc, n, a.out_cols % 8 == 0);
+}
+
+// Where cluster c keeps its sums over a part of the depth of a tile: one slot
+// for the tile that its range begins in, one for the tile that it ends in.
+template <int NB>
+__device__ __forceinline__ float* slot_of(const Args& a, const Walk<kProducts>& walk, const Item& it, int c, int rank, int b, int ew,
+                                          int lane) {
+    const size_t s = 2 * (size_t)c + (walk.bound(c) >= it.tile_lo ? 0 : 1);
+    return a.partials + (((s * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + lane;
+}
+
+// The parts of a tile that several clusters share, once this cluster's are
+// stored: for each block of columns the warp that finds itself last adds the
+// parts up in the order of the depth, so the result does not depend on which
+// one is last, and writes the rows.
+template <int NB, bool WIDE>
+__device__ __forceinline__ void join_parts(const Args& a, const Walk<kProducts>& walk, const Item& it, int cluster, int rank, int ew,
+                                           int lane, int row, int half, float scale, float* acc) {
+    __threadfence();
+    __syncwarp();
+    int lo = cluster, hi = cluster, parts = 0;
+    while (walk.bound(lo) > it.tile_lo) --lo;
+    while (walk.bound(hi + 1) < it.tile_hi) ++hi;
+    for (int c = lo; c <= hi; ++c) parts += walk.bound(c + 1) > walk.bound(c);
+    unsigned before = 0;
+    if (lane < NB) before = atomicAdd(a.counters + ((lo * 2 + rank) * NB + lane) * kEpilogueWarps + ew, 1u);
+#pragma unroll 1
+    for (int b = 0; b < NB; ++b) {
+        const int c0 = it.n0 + 256 * b + 128 * half;
+        if ((int)__shfl_sync(0xffffffffu, before, b) != parts - 1) continue;
+        if (lane == b) a.counters[((lo * 2 + rank) * NB + b) * kEpilogueWarps + ew] = 0u;   // for the next piece
+        if (c0 >= a.out_cols) continue;
+        __threadfence();
+#pragma unroll
+        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
+        for (int c = lo; c <= hi; ++c) {
+            if (walk.bound(c + 1) <= walk.bound(c)) continue;
+            const float* p = slot_of<NB>(a, walk, it, c, rank, b, ew, lane);
+#pragma unroll
+            for (int j = 0; j < 128; ++j) acc[j] += __ldcg(p + 32 * j);
+        }
+        write_product<WIDE>(a, it.problem, row, c0, scale, acc);
+    }
 }
 
 __device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
 
-template <int MODE, int NB, bool F32>
+template <int MODE, int NB, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     using C = Config<MODE, NB>;
@@ -253,9 +259,9 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     grid_dependency_sync();
     asm volatile("fence.proxy.async.global;\n" ::: "memory");   // operands written by the kernel before are read by TMA
 
-    constexpr int kPlanes = F32 ? 6 : 1;           // products of planes for one of values
+    const int combos = WIDE ? a.combos : 1;        // products of planes for one of values
     // Depth of a run (chunks of 64) whose sums stay in the tensor core.
-    constexpr int kRun = F32 ? 2 : MODE == kProducts ? (1 << 30) : 8;
+    constexpr int kRun = WIDE ? 2 : MODE == kProducts ? (1 << 30) : 8;
 
     if (warp < 4) {
         tc5::registers_down<56>();
@@ -271,10 +277,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
             while (ok && walk.next(it)) {
                 for (int r0 = it.k0; ok && r0 < it.k1; r0 += min(kRun, it.k1 - r0)) {
                     const int len = min(kRun, it.k1 - r0);
-                    for (int i = 0; i < kPlanes * len; ++i) {
-                        const int chunk = r0 + (F32 ? i % len : i);
-                        int pa = 0, pb = 0;
-                        if (F32) planes_of(i / len, pa, pb);
+                    for (int i = 0; i < combos * len; ++i) {
+                        const int chunk = r0 + (WIDE ? i % len : i);
+                        const int pa = WIDE ? (a.combo_a >> (4 * (i / len))) & 15 : 0;
+                        const int pb = WIDE ? (a.combo_b >> (4 * (i / len))) & 15 : 0;
                         ok = tc5::wait_parity(empty + 8 * stage, phase ^ 1u);
                         if (!ok) break;
                         if (rank == 0) tc5::expect_bytes(full + 8 * stage, 2 * C::kStageBytes);
@@ -336,7 +342,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     for (int b = 0; b < NB; ++b) ok = ok && tc5::wait_parity(acc_empty + 8 * (buf + b), (use & 1u) ^ 1u);
                     if (!ok) break;
                     tc5::fence_after();
-                    for (int i = 0; i < kPlanes * len; ++i) {
+                    for (int i = 0; i < combos * len; ++i) {
                         ok = tc5::wait_parity(full + 8 * stage, phase);
                         if (!ok) break;
                         tc5::fence_after();
@@ -360,8 +366,6 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 }
             }
             if (!ok) raise_status(a.p.status, kStatusWaitTimeout);
-        } else if (MODE == kGradient && warp == 3 && blockIdx.x == 0) {
-            for (int i = lane; i < a.n_counters; i += 32) a.counters[i] = 0u;   // for the products that follow
         }
     } else {
         tc5::registers_up<224>();
@@ -370,34 +374,31 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         const int lane_row = (warp & 3) * 32 + lane;
         const unsigned t_lane = tmem + ((unsigned)(warp & 3) << 21) + 128u * half;
         const unsigned acc_empty0 = tc5::map_to(acc_empty, 0);
-        const unsigned stage_out = smem0 + C::kStages * C::kStageBytes + ew * 8192u;
+        const unsigned stage_out = smem0 + C::kStages * C::kStageBytes + ew * 4096u;
         Walk<MODE> walk(a, cluster, clusters);
         Item it;
         unsigned run = 0;
         bool ok = true;
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, z = 0.f, z2 = 0.f, dl = 0.f;
         int target = kIgnored;
-        unsigned stores = 0;
+        const float out_scale = MODE == kForward ? 1.f : *a.scale;
         while (walk.next(it)) {
             const int row = it.m0 + 128 * (int)rank + lane_row;
-            float z2 = 0.f, z = 0.f, dl = 0.f;
             if (MODE == kForward && it.first) {
                 m = -INFINITY;
                 l = 0.f;
                 target = row < a.p.N ? target_column(a.p, row) : kIgnored;
             }
-            if (MODE == kGradient) {
+            if (MODE == kGradient && it.first) {
                 target = row < a.p.N ? target_column(a.p, row) : kIgnored;
-                if (target >= 0) {
-                    z = a.lse[row];
-                    dl = a.dloss[row];
-                }
+                z = row < a.p.N ? a.lse[row] : 0.f;
+                dl = row < a.p.N ? a.dloss[row] / out_scale : 0.f;
                 z2 = z * kLog2e;
                 if (target == kBad && a.v0 + it.n0 == 0 && half == 0) raise_status(a.p.status, kStatusTarget);
             }
+            float acc[128];
 #pragma unroll 1
             for (int b = 0; b < NB; ++b) {
-                float acc[128];
                 const int runs = (it.k1 - it.k0 + kRun - 1) / kRun;
                 unsigned n_run = run;
 #pragma unroll 1
@@ -451,7 +452,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
                     const float ms = top == -INFINITY ? 0.f : top;
                     float s[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (F32) {
+                    if (WIDE) {
 #pragma unroll
                         for (int j = 0; j < 128; ++j) s[j & 3] += expf(acc[j] - ms);
                         l = l * expf(m - ms);
@@ -476,7 +477,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     } else {
 #pragma unroll
                         for (int j = 0; j < 128; ++j)
-                            acc[j] = dl * (F32 ? expf(acc[j] - z) : ex2(fmaf(acc[j], kLog2e, -z2)));
+                            acc[j] = dl * (WIDE ? expf(acc[j] - z) : ex2(fmaf(acc[j], kLog2e, -z2)));
                         const int local = target - a.v0 - c0;
                         if ((unsigned)local < 128u) {
 #pragma unroll
@@ -486,14 +487,13 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     }
                     const int r0 = it.m0 + 128 * (int)rank + (warp & 3) * 32;
 #pragma unroll
-                    for (int plane = 0; plane < (F32 ? 3 : 1); ++plane) {
+                    for (int plane = 0; plane < (WIDE ? 3 : 1); ++plane) {
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const int col = c0 + 64 * h;
                             if (r0 < a.p.N && col < a.cols) {        // (uniform over the warp)
-                                const unsigned dst = stage_out + 4096u * (stores & 1u);
-                                ++stores;
-                                if (lane == 0) tc5::store_wait_read<1>();
+                                const unsigned dst = stage_out;
+                                if (lane == 0) tc5::store_wait_read<0>();
                                 __syncwarp();
 #pragma unroll
                                 for (int ch = 0; ch < 8; ++ch) {
@@ -502,7 +502,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                                     for (int e = 0; e < 4; ++e) {
                                         const int j = 64 * h + 8 * ch + 2 * e;
                                         u[e] = mma::pack_bf16(acc[j], acc[j + 1]);
-                                        if (F32) {           // what the next plane has to hold
+                                        if (WIDE) {           // what the next plane has to hold
                                             acc[j] -= __uint_as_float(u[e] << 16);
                                             acc[j + 1] -= __uint_as_float(u[e] & 0xffff0000u);
                                         }
@@ -522,9 +522,18 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     }
                 } else if constexpr (MODE == kProducts) {
                     if (c0 >= a.out_cols) continue;          // (uniform over the warp)
-                    finish_product<NB, F32>(a, it, walk, cluster, (int)rank, b, ew, lane, row, c0, acc);
+                    if (it.whole) {
+                        write_product<WIDE>(a, it.problem, row, c0, out_scale, acc);
+                    } else {
+                        float* mine = slot_of<NB>(a, walk, it, cluster, (int)rank, b, ew, lane);
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
+                    }
                 }
             }
+            // (both blocks' accumulators are free by now: the next tile is under way)
+            if constexpr (MODE == kProducts)
+                if (!it.whole) join_parts<NB, WIDE>(a, walk, it, cluster, (int)rank, ew, lane, row, half, out_scale, acc);
         }
         if (MODE == kGradient && lane == 0) tc5::store_wait_all();
     }
@@ -534,6 +543,31 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     tc5::cluster_sync();
     tc5::fence_after();
     if (warp == 2) tc5::tmem_free(tmem);
+}
+
+// scale = the largest |dloss| of the rows with a target (1 if there is none or
+// it is not finite).  g is kept divided by it: with the mean's equal weights
+// the -1 of a target then is exact in bf16, where the weight itself would be
+// off by up to 2^-9 in every row alike.  Also clears the products' counters.
+__global__ void __launch_bounds__(1024) scale_kernel(Problem p, const float* dloss, float* scale, unsigned* counters, int n_counters) {
+    __shared__ float red[32];
+    grid_dependency_sync();
+    for (int i = threadIdx.x; i < n_counters; i += 1024) counters[i] = 0u;
+    float m = 0.f;
+    for (int n = threadIdx.x; n < p.N; n += 1024) {
+        const float d = fabsf(dloss[n]);
+        if (target_column(p, n) >= 0) m = fmaxf(m, d);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = m;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        m = red[threadIdx.x];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (threadIdx.x == 0) *scale = m > 0.f && m < INFINITY ? m : 1.f;
+    }
 }
 
 // Rows of T as `planes` bf16 planes of row length `depth` (zeros past D): one
@@ -579,8 +613,8 @@ bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int NB, bool F32> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
-    auto kern = xent_kernel<MODE, NB, F32>;
+template <int MODE, int NB, bool WIDE> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
+    auto kern = xent_kernel<MODE, NB, WIDE>;
     // The register split of the two halves of a block draws on what the block
     // was launched with: refuse to launch a build that was given less.
     static const int registers = [&] {
@@ -589,8 +623,15 @@ template <int MODE, int NB, bool F32> cudaError_t launch(const Args& a, const Ma
     }();
     if (registers * kThreads < 56 * 128 + 224 * 256) return cudaErrorInvalidDeviceFunction;
     constexpr unsigned smem = Config<MODE, NB>::kSmem;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    static std::atomic<unsigned long long> set{0};          // devices (of the first 64) where the limit is raised already
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    if (dev >= 64 || !(set.load(std::memory_order_relaxed) >> dev & 1)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) set.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     return launch_kernel(kern, dim3(2 * clusters), dim3(kThreads), smem, st, a, maps);
 }
 
@@ -604,26 +645,51 @@ void plan_operands(int D, bool bf16, bool* pack, int* planes, int* depth) {
     *depth = (D + 7) / 8 * 8;
 }
 
+// The products of planes that make up one of values, the small ones first:
+// while the running sum is small so is what truncation takes from it.  Of the
+// nine products of three planes with three, six are kept (the others are below
+// 2^-24 of the value).
+void set_combos(Args* a, int planes_a, int planes_b) {
+    if (planes_a == 3 && planes_b == 3) {
+        a->combos = 6;
+        a->combo_a = 0x010120;                     // read from the right: 0 2 1 0 1 0
+        a->combo_b = 0x001102;                     //                      2 0 1 1 0 0
+    } else if (planes_a == 3) {
+        a->combos = 3;
+        a->combo_a = 0x012;
+        a->combo_b = 0;
+    } else {
+        a->combos = 1;
+        a->combo_a = a->combo_b = 0;
+    }
+}
+
 }  // namespace
 
-// The forward's unit: tiles of one row of tiles that a cluster takes in a row
-// before it writes its rows' statistics.  The fewest rounds over the clusters
-// win; at most 64 segments of the vocabulary, so that the statistics stay small.
+// Tiles of one row of tiles that a cluster takes one after another (a unit):
+// the fewest rounds over the clusters win, with a quarter of a tile for what a
+// unit costs by itself (its rows' targets, the statistics it writes).  At most
+// 64 segments of the columns, so that the forward's statistics stay small.
+static int unit_tiles_of(int row_tiles, int col_tiles) {
+    const int least = std::max(1, (col_tiles + 63) / 64);
+    int unit = least;
+    double best = 0;
+    for (int u = least; u <= std::max(16, least); ++u) {
+        const long long units = (long long)row_tiles * ((col_tiles + u - 1) / u);
+        const double cost = (double)((units + kClusters - 1) / kClusters) * (u + 0.25);
+        if (u == least || cost < best) {
+            best = cost;
+            unit = u;
+        }
+    }
+    return unit;
+}
+
 FwdPlan plan_forward(int N, int D, int V, bool bf16) {
     FwdPlan f{};
     plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
-    const int rt = tiles256(N), ct = tiles256(V);
-    double best = 0;
-    for (int u = std::max(1, (ct + 63) / 64); u <= std::max(16, (ct + 63) / 64); ++u) {
-        const int segs = (ct + u - 1) / u;
-        const long long units = (long long)rt * segs;
-        const double cost = (double)((units + kClusters - 1) / kClusters) * (u + 0.25);
-        if (f.unit_tiles == 0 || cost < best) {
-            best = cost;
-            f.unit_tiles = u;
-            f.segments = 2 * segs;
-        }
-    }
+    f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
+    f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
     size_t off = 0;
     const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };
     f.x = take(f.pack ? (size_t)f.planes * N * f.depth * 2 : 0);
@@ -660,6 +726,7 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     const int clusters = std::min(kClusters, a.units);
     {
         ProfScope s("xent_fwd", st);
+        set_combos(&a, f.planes, f.planes);
         e = bf16 ? launch<kForward, 1, false>(a, maps, clusters, st) : launch<kForward, 1, true>(a, maps, clusters, st);
     }
     if (e != cudaSuccess) return e;
@@ -667,23 +734,30 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     return launch_combine(p, a.parts, f.segments, loss, lse, st);
 }
 
-// g of a piece is held in memory for the two products: at most 256 MiB of it
-// (at least 256 columns).
+// g of a piece is held in memory for the two products: at most 512 MiB of it
+// (at least 256 columns; 16384 rows, 512 wide, 32768 columns: two products launches of
+// 339 us; pieces of 256 MiB 791 us together, one piece 650 us).  One bf16 plane rounds each g to 8 bits, which the
+// products average out over many; fp32 I/O keeps three planes (24 bits), and so
+// does bf16 I/O below 2^26 multiplications, where the further planes hide
+// behind the launches.
 BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     BwdPlan f{};
     plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
-    const long long fit = (256ll << 20) / (2ll * f.planes * std::max(N, 1)) / 256 * 256;
+    f.wide = !bf16 || (double)N * D * V <= (double)(1 << 26);
+    f.g_planes = f.wide ? 3 : 1;
+    f.blocks = !f.wide && D > 256 ? 2 : 1;
+    const long long fit = (512ll << 20) / (2ll * f.g_planes * std::max(N, 1)) / 256 * 256;
     f.cols = (int)std::min<long long>(V, std::max(256ll, fit));
     f.ldg = (f.cols + 7) / 8 * 8;
     size_t off = 0;
     const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };
-    const int nb = bf16 && D > 256 ? 2 : 1;
     f.x = take(f.pack ? (size_t)f.planes * N * f.depth * 2 : 0);
     f.w = take(f.pack ? (size_t)f.planes * V * f.depth * 2 : 0);
-    f.g = take((size_t)f.planes * N * f.ldg * 2);
+    f.g = take((size_t)f.g_planes * N * f.ldg * 2);
     f.dx_acc = take(f.cols < V ? (size_t)N * D * 4 : 0);
-    f.partials = take((size_t)kClusters * 2 * nb * 256 * 256 * 4);
-    f.counters = take((size_t)kClusters * 2 * nb * kEpilogueWarps * 4);
+    f.partials = take((size_t)kClusters * 2 * f.blocks * 256 * 256 * 4);
+    f.counters = take((size_t)kClusters * 2 * f.blocks * kEpilogueWarps * 4);
+    f.scale = take(4);
     f.total = off;
     return f;
 }
@@ -699,7 +773,6 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
         x = ws + f.x;
         w = ws + f.w;
     }
-    const int nb = bf16 && p.D > 256 ? 2 : 1;
     Maps logits{}, products{};
     if (!encode(&logits.m[0], x, f.depth, p.N, f.planes, f.depth, 64, 128) ||
         !encode(&logits.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 128) ||
@@ -711,30 +784,40 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     a.lse = lse;
     a.dloss = dloss;
     a.out_cols = p.D;
-    a.tile_cols = 256 * nb;
-    a.snap = bf16 ? 16 : 4;
+    a.tile_cols = 256 * f.blocks;
+    a.snap = f.wide ? 4 : 16;
+    a.out_f32 = !bf16;
     a.partials = reinterpret_cast<float*>(ws + f.partials);
     a.counters = reinterpret_cast<unsigned*>(ws + f.counters);
-    a.n_counters = kClusters * 2 * nb * kEpilogueWarps;
+    float* scale = reinterpret_cast<float*>(ws + f.scale);
+    a.scale = scale;
     a.dx_acc = reinterpret_cast<float*>(ws + f.dx_acc);
     a.dx = dx;
     a.dw = dw;
+    {
+        ProfScope s("xent_scale", st);
+        e = launch_kernel(scale_kernel, dim3(1), dim3(1024), 0, st, p, dloss, scale, a.counters,
+                          kClusters * 2 * f.blocks * kEpilogueWarps);
+    }
+    if (e != cudaSuccess) return e;
     for (int v0 = 0; v0 < p.V; v0 += f.cols) {
         const int cols = std::min(f.cols, p.V - v0);
-        if (!encode(&logits.m[2], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 32) ||
-            !encode(&products.m[0], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 128) ||
-            !encode(&products.m[2], ws + f.g, cols, p.N, f.planes, f.ldg, 64, 64))
+        if (!encode(&logits.m[2], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 32) ||
+            !encode(&products.m[0], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 128) ||
+            !encode(&products.m[2], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 64))
             return cudaErrorInvalidValue;
         a.v0 = v0;
         a.cols = cols;
         a.chunks = (p.D + 63) / 64;
         a.row_tiles = tiles256(p.N);
         a.col_tiles = tiles256(cols);
-        a.units = a.row_tiles * a.col_tiles;
+        a.unit_tiles = unit_tiles_of(a.row_tiles, a.col_tiles);
+        a.units = a.row_tiles * ((a.col_tiles + a.unit_tiles - 1) / a.unit_tiles);
         {
             ProfScope s("xent_grad", st);
             const int clusters = std::min(kClusters, a.units);
-            e = bf16 ? launch<kGradient, 1, false>(a, logits, clusters, st) : launch<kGradient, 1, true>(a, logits, clusters, st);
+            set_combos(&a, f.planes, f.planes);
+            e = f.wide ? launch<kGradient, 1, true>(a, logits, clusters, st) : launch<kGradient, 1, false>(a, logits, clusters, st);
         }
         if (e != cudaSuccess) return e;
         const int d_tiles = (p.D + a.tile_cols - 1) / a.tile_cols;
@@ -746,8 +829,9 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
         a.dx_done = v0 + cols >= p.V;
         {
             ProfScope s("xent_products", st);
-            e = !bf16 ? launch<kProducts, 1, true>(a, products, kClusters, st)
-                : nb == 2 ? launch<kProducts, 2, false>(a, products, kClusters, st)
+            set_combos(&a, f.g_planes, f.planes);
+            e = f.wide ? launch<kProducts, 1, true>(a, products, kClusters, st)
+                : f.blocks == 2 ? launch<kProducts, 2, false>(a, products, kClusters, st)
                           : launch<kProducts, 1, false>(a, products, kClusters, st);
         }
         if (e != cudaSuccess) return e;

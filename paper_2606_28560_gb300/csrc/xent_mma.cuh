@@ -30,11 +30,15 @@ struct Args {
     int tile_cols, out_cols;                       // columns of a tile, of the results (D)
     float* partials;                               // sums over a part of a tile's depth
     unsigned* counters;                            // parts of a tile that have arrived
-    int n_counters;
+    const float* scale;                            // g is divided by it, the products multiplied
     float* dx_acc;                                 // dx over the earlier pieces, fp32
     bool dx_add, dx_done;                          // there are earlier pieces; this is the last one
     void* dx;
     void* dw;
+    bool out_f32;
+    // operands of several planes: product i takes planes (combo_a >> 4 i) & 15 and (combo_b >> 4 i) & 15
+    int combos;
+    unsigned combo_a, combo_b;
 };
 
 struct Maps {
@@ -51,10 +55,11 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16);
 cudaError_t run_forward(const Problem& p, const FwdPlan& plan, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st);
 
 struct BwdPlan {
-    bool pack;
-    int planes, depth;
+    bool pack, wide;                               // wide: products of several planes
+    int planes, depth, g_planes;
+    int blocks;                                    // blocks of 256 columns of a products' tile
     int cols, ldg;                                 // columns of a piece; row length of g
-    size_t x, w, g, dx_acc, partials, counters, total;
+    size_t x, w, g, dx_acc, partials, counters, scale, total;
 };
 BwdPlan plan_backward(int N, int D, int V, bool bf16);
 cudaError_t run_backward(const Problem& p, const BwdPlan& plan, char* ws, bool bf16, const float* lse, const float* dloss,
