@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import operator
 import os
 import threading
 
@@ -449,6 +450,13 @@ def _grad_like(t, of):
     return t
 
 
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _on_device(tensors, index) -> bool:
+    return set(map(torch.Tensor.get_device, tensors)) == {index} and all(map(torch.Tensor.is_contiguous, tensors))
+
+
 _CLIP_CODE = {torch.float32: FIBATTN_F32, torch.bfloat16: FIBATTN_BF16}
 
 
@@ -467,23 +475,21 @@ def grad_norm(grads, *, norm=None, workspace=None, stream=None):
 
 
 def _clip(grads, max_norm, out, norm, workspace, stream, scale):
-    # (a model has hundreds of tensors: each is looked at with as few calls as will do)
+    # (a model has hundreds of tensors: each is looked at with few calls, made by map)
     n = len(grads)
     outs = grads if out is None else list(out)
     if len(outs) != n:
         raise ValueError("out must hold one tensor for each gradient")
     index = grads[0].get_device() if n else torch.cuda.current_device()
-    dtypes = [t.dtype for t in grads]
+    dtypes = list(map(_dtype_of, grads))
     if not _CLIP_CODE.keys() >= set(dtypes):
         raise TypeError("unsupported dtype: fp32 or bf16")
-    codes = [_CLIP_CODE[d] for d in dtypes]
-    sizes = [t.numel() for t in grads]
-    if index < 0 or n and {t.get_device() for t in grads} != {index} or not all([t.is_contiguous() for t in grads]):
+    sizes = list(map(torch.Tensor.numel, grads))
+    if index < 0 or n and not _on_device(grads, index):
         raise ValueError("gradients must be contiguous CUDA tensors on one device")
-    if out is not None and n:
-        if [t.dtype for t in outs] != dtypes or [t.numel() for t in outs] != sizes or \
-                {t.get_device() for t in outs} != {index} or not all([t.is_contiguous() for t in outs]):
-            raise ValueError("out must hold contiguous tensors like the gradients")
+    if out is not None and n and (list(map(_dtype_of, outs)) != dtypes or
+                                  list(map(torch.Tensor.numel, outs)) != sizes or not _on_device(outs, index)):
+        raise ValueError("out must hold contiguous tensors like the gradients")
     device = grads[0].device if n else torch.device("cuda", index)
     if norm is None:
         norm = torch.empty((), dtype=torch.float32, device=device)
@@ -492,9 +498,9 @@ def _clip(grads, max_norm, out, norm, workspace, stream, scale):
     L = lib()
     if workspace is None:
         workspace = torch.empty(L.fibattn_clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
-    arrays = [array.array("Q", [t.data_ptr() for t in grads]),
-              array.array("Q", [t.data_ptr() for t in outs]) if scale else None,
-              array.array("q", sizes), array.array("i", codes)]
+    ptrs = array.array("Q", map(torch.Tensor.data_ptr, grads))
+    optrs = (ptrs if out is None else array.array("Q", map(torch.Tensor.data_ptr, outs))) if scale else None
+    arrays = [ptrs, optrs, array.array("q", sizes), array.array("i", map(_CLIP_CODE.__getitem__, dtypes))]
     at = [a.buffer_info()[0] if a is not None else None for a in arrays]
     _check(L.fibattn_clip_grads(n, *at, max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                 _stream_of(stream, index)))

@@ -18,9 +18,10 @@ using namespace fibattn;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 16384;              // values of a chunk: 64 of each thread
-constexpr int kResident = 4;               // blocks of an SM
-constexpr int kBlocks = 152 * kResident;   // blocks of a launch, at most
+constexpr int kChunkBytes = 32768;         // bytes of a chunk: 128 of each thread
+__host__ __device__ constexpr int chunk_values(bool bf16) { return kChunkBytes / (bf16 ? 2 : 4); }
+constexpr int kNormResident = 4, kClipResident = 4;   // blocks of an SM
+constexpr int kBlocks = 152 * kNormResident;           // blocks (and partial sums) of a launch, at most
 constexpr int kTable = 512;                // tensors of a launch, at most
 constexpr int kShort = 48;                 // tensors of a short table (a launch carries its whole table)
 constexpr long long kMaxChunks = 1ll << 30;
@@ -80,18 +81,25 @@ template <typename T> __device__ __forceinline__ float sum_squares(const T* p, i
         s[1] = x * x;
     }
     const uint4* body = reinterpret_cast<const uint4*>(p + head);
-    for (int i = threadIdx.x; i < vectors; i += kNormBatch * kThreads) {
+    const auto add = [&](const V& v) {
+#pragma unroll
+        for (int j = 0; j < V::kValues; ++j) {
+            const float x = v.get(j);
+            s[j & 3] = fmaf(x, x, s[j & 3]);
+        }
+    };
+    int i = threadIdx.x;
+    for (; i + (kNormBatch - 1) * kThreads < vectors; i += kNormBatch * kThreads) {
         V v[kNormBatch];
 #pragma unroll
-        for (int k = 0; k < kNormBatch; ++k)
-            v[k].u = i + k * kThreads < vectors ? __ldg(body + i + k * kThreads) : make_uint4(0u, 0u, 0u, 0u);
+        for (int k = 0; k < kNormBatch; ++k) v[k].u = __ldg(body + i + k * kThreads);
 #pragma unroll
-        for (int k = 0; k < kNormBatch; ++k)
-#pragma unroll
-            for (int j = 0; j < V::kValues; ++j) {
-                const float x = v[k].get(j);
-                s[j & 3] = fmaf(x, x, s[j & 3]);
-            }
+        for (int k = 0; k < kNormBatch; ++k) add(v[k]);
+    }
+    for (; i < vectors; i += kThreads) {
+        V v;
+        v.u = __ldg(body + i);
+        add(v);
     }
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
@@ -109,14 +117,14 @@ __device__ double block_sum(double s, double* red) {
 
 // partial[b]: block b's sum of squares over its chunks b, b + gridDim, ...
 template <int N>
-__global__ void __launch_bounds__(kThreads, kResident) norm_kernel(const __grid_constant__ Table<N> t, double* partial) {
+__global__ void __launch_bounds__(kThreads, kNormResident) norm_kernel(const __grid_constant__ Table<N> t, double* partial) {
     __shared__ double red[kThreads / 32];
     grid_dependency_sync();
     double s = 0.0;
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const Entry& e = t.e[entry_of(t, c)];
-        const long long at = (long long)(c - e.first_chunk) * kChunk;
-        const int n = (int)min((long long)kChunk, e.n - at);
+        const long long at = (long long)(c - e.first_chunk) * chunk_values(e.bf16);
+        const int n = (int)min((long long)chunk_values(e.bf16), e.n - at);
         s += e.bf16 ? sum_squares(static_cast<const __nv_bfloat16*>(e.in) + at, n)
                     : sum_squares(static_cast<const float*>(e.in) + at, n);
     }
@@ -149,14 +157,18 @@ template <typename T> __device__ __forceinline__ void scale(const T* in, T* out,
     if ((int)threadIdx.x < head) put(out + threadIdx.x, to_f(in[threadIdx.x]) * c);
     const uint4* body = reinterpret_cast<const uint4*>(in + head);
     uint4* to = reinterpret_cast<uint4*>(out + head);
-    for (int i = threadIdx.x; i < vectors; i += kClipBatch * kThreads) {
+    int k0 = threadIdx.x;
+    for (; k0 + (kClipBatch - 1) * kThreads < vectors; k0 += kClipBatch * kThreads) {
         V v[kClipBatch];
 #pragma unroll
-        for (int k = 0; k < kClipBatch; ++k)
-            if (i + k * kThreads < vectors) v[k].u = __ldcs(body + i + k * kThreads);
+        for (int k = 0; k < kClipBatch; ++k) v[k].u = body[k0 + k * kThreads];
 #pragma unroll
-        for (int k = 0; k < kClipBatch; ++k)
-            if (i + k * kThreads < vectors) __stcs(to + i + k * kThreads, scaled(v[k], c));
+        for (int k = 0; k < kClipBatch; ++k) __stcs(to + k0 + k * kThreads, scaled(v[k], c));
+    }
+    for (; k0 < vectors; k0 += kThreads) {
+        V v;
+        v.u = body[k0];
+        __stcs(to + k0, scaled(v, c));
     }
     // the tail, or everything where in and out start at different offsets within 16 bytes
     for (int i = tail + threadIdx.x; i < n; i += kClipBatch * kThreads) {
@@ -171,7 +183,7 @@ template <typename T> __device__ __forceinline__ void scale(const T* in, T* out,
 
 // Every block adds up all partials, in the same order, and scales its chunks.
 template <int N>
-__global__ void __launch_bounds__(kThreads, kResident) clip_kernel(const __grid_constant__ Table<N> t, const double* partial,
+__global__ void __launch_bounds__(kThreads, kClipResident) clip_kernel(const __grid_constant__ Table<N> t, const double* partial,
                                                                    int partials, float max_norm, float* norm) {
     __shared__ double red[kThreads / 32];
     grid_dependency_sync();
@@ -185,12 +197,14 @@ __global__ void __launch_bounds__(kThreads, kResident) clip_kernel(const __grid_
     for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
         const Entry& e = t.e[entry_of(t, c)];
         if (e.out == e.in && coef == 1.f) continue;
-        const long long at = (long long)(c - e.first_chunk) * kChunk;
-        const int n = (int)min((long long)kChunk, e.n - at);
+        const long long at = (long long)(c - e.first_chunk) * chunk_values(e.bf16);
+        const int n = (int)min((long long)chunk_values(e.bf16), e.n - at);
         if (e.bf16) scale(static_cast<const __nv_bfloat16*>(e.in) + at, static_cast<__nv_bfloat16*>(e.out) + at, n, coef);
         else scale(static_cast<const float*>(e.in) + at, static_cast<float*>(e.out) + at, n, coef);
     }
 }
+
+long long chunks_of(long long n, bool bf16) { return (n + chunk_values(bf16) - 1) / chunk_values(bf16); }
 
 int tables_of(int n) { return n > kTable ? (n + kTable - 1) / kTable : 1; }
 
@@ -206,7 +220,7 @@ void fill(Table<N>* t, int first, int last, const void* const* grads, void* cons
         e.n = numels[i];
         e.bf16 = dtypes[i] == FIBATTN_BF16;
         e.first_chunk = (int)chunks;
-        chunks += (numels[i] + kChunk - 1) / kChunk;
+        chunks += chunks_of(numels[i], e.bf16);
     }
     t->chunks = (int)chunks;
 }
@@ -243,7 +257,7 @@ cudaError_t run(int n, const void* const* grads, void* const* outs, const long l
     for (int k = 0; k < (outs ? tables : 1) && e == cudaSuccess; ++k) {
         if (tables > 1) fill(&t, k * N, std::min(n, (k + 1) * N), grads, outs, numels, dtypes);
         if (!outs) t.chunks = 0;                 // the norm alone
-        const int grid = std::max(1, std::min(kBlocks, t.chunks));
+        const int grid = std::max(1, std::min(152 * kClipResident, t.chunks));
         ProfScope s("grad_clip", st);
         e = start(clip_kernel<N>, grid, st, t, static_cast<const double*>(partial), partials, max_norm,
                   k == 0 ? norm : static_cast<float*>(nullptr));
@@ -284,7 +298,7 @@ int fibattn_clip_grads(int n, const void* const* grads, void* const* outs, const
         const uintptr_t es = dtypes[i] == FIBATTN_BF16 ? 2 : 4;
         if (((uintptr_t)grads[i] | (outs ? (uintptr_t)outs[i] : 0)) & (es - 1))
             return set_errorf(FIBATTN_ERR_INVALID_ARG, "tensor %d: pointer not aligned to its element", i);
-        if (numels[i] > kMaxChunks * kChunk || (chunks += (numels[i] + kChunk - 1) / kChunk) > kMaxChunks)
+        if (numels[i] > kMaxChunks * chunk_values(false) || (chunks += chunks_of(numels[i], dtypes[i] == FIBATTN_BF16)) > kMaxChunks)
             return set_error(FIBATTN_ERR_INVALID_ARG, "too many values");
     }
     int rc = bind_device_context();

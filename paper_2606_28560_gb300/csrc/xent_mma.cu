@@ -54,6 +54,21 @@ struct Item {
     int tile_lo, tile_hi;                          // products: the tile's range of the iteration space
 };
 
+// Products: start of cluster c's range of the iteration space (all tiles'
+// chunks of depth one after another): equal shares of dx's part for the clusters
+// below first_dw, of dw's for the others.  A boundary within `snap` chunks of a
+// tile's end moves there: a sliver is not worth a tile of partial sums.
+__host__ __device__ inline int range_start(const Args& a, int c, int clusters) {
+    int b;
+    if (c < a.first_dw) b = (int)((long long)a.split * c / a.first_dw);
+    else b = a.split + (int)((long long)(a.total - a.split) * (c - a.first_dw) / (clusters - a.first_dw));
+    if (b <= 0 || b >= a.total) return b <= 0 ? 0 : a.total;
+    const int p = b < a.split ? 0 : 1, kc = a.prob[p].chunks, off = (b - (p ? a.split : 0)) % kc;
+    if (off <= a.snap[p]) return b - off;
+    if (kc - off <= a.snap[p]) return b - off + kc;
+    return b;
+}
+
 // The items of cluster c, in order.
 template <int MODE> struct Walk {
     const Args& a;
@@ -64,19 +79,7 @@ template <int MODE> struct Walk {
             end = bound(c + 1);
         }
     }
-    // Products: start of cluster c's range of the iteration space (all tiles'
-    // chunks of depth one after another).  Equal shares, but a boundary within
-    // `snap` chunks of a tile's end moves there: a sliver is not worth the
-    // exchange of a whole tile of partial sums.
-    __device__ int bound(int cluster) const {
-        const int b = (int)((long long)a.total * cluster / clusters);
-        if (b <= 0 || b >= a.total) return b <= 0 ? 0 : a.total;
-        const int p = b < a.split ? 0 : 1, base = p ? a.split : 0, kc = a.prob[p].chunks;
-        const int off = (b - base) % kc;
-        if (off <= a.snap) return b - off;
-        if (kc - off <= a.snap) return b - off + kc;
-        return b;
-    }
+    __device__ int bound(int cluster) const { return range_start(a, cluster, clusters); }
     __device__ bool next(Item& it) {
         if (MODE != kProducts) {
             if (at >= a.units) return false;
@@ -116,66 +119,66 @@ __device__ __forceinline__ int block_columns(const Args& a, const Item& it, int 
     return min(256, max(0, (a.out_cols - it.n0 - 256 * b + 31) & ~31));
 }
 
-// 128 columns of one output row from registers.  `aligned`: rows start on
+// COUNT columns of one output row from registers.  `aligned`: rows start on
 // 16-byte boundaries (then no group of 16 bytes straddles the end of a row).
-__device__ __forceinline__ void put_row(float* out, const float* v, int n, bool aligned) {
+template <int COUNT> __device__ __forceinline__ void put_row(float* out, const float* v, int n, bool aligned) {
     if (aligned) {
 #pragma unroll
-        for (int j = 0; j < 128; j += 4)
+        for (int j = 0; j < COUNT; j += 4)
             if (j < n) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     } else {
 #pragma unroll
-        for (int j = 0; j < 128; ++j)
+        for (int j = 0; j < COUNT; ++j)
             if (j < n) out[j] = v[j];
     }
 }
-__device__ __forceinline__ void put_row(__nv_bfloat16* out, const float* v, int n, bool aligned) {
+template <int COUNT> __device__ __forceinline__ void put_row(__nv_bfloat16* out, const float* v, int n, bool aligned) {
     if (aligned) {
 #pragma unroll
-        for (int j = 0; j < 128; j += 8)
+        for (int j = 0; j < COUNT; j += 8)
             if (j < n) Vec8<__nv_bfloat16>::store(out + j, v + j);
     } else {
 #pragma unroll
-        for (int j = 0; j < 128; ++j)
+        for (int j = 0; j < COUNT; ++j)
             if (j < n) out[j] = __float2bfloat16(v[j]);
     }
 }
 
 // Row `row`, columns from c0 of a finished product.  What g was divided by is
 // multiplied back here.
-template <bool WIDE>
+template <bool WIDE, int COUNT>
 __device__ __forceinline__ void write_product(const Args& a, int problem, int row, int c0, float scale, float* acc) {
     if (row >= a.prob[problem].rows) return;
     const int n = a.out_cols - c0;
     const size_t at = (size_t)row * a.out_cols + c0;
     const bool al4 = a.out_cols % 4 == 0;
 #pragma unroll
-    for (int j = 0; j < 128; ++j) acc[j] *= scale;
+    for (int j = 0; j < COUNT; ++j) acc[j] *= scale;
     if (problem == 0) {
         if (a.dx_add) {
             const float* p = a.dx_acc + at;
             if (al4) {
 #pragma unroll
-                for (int j = 0; j < 128; j += 4)
+                for (int j = 0; j < COUNT; j += 4)
                     if (j < n) {
                         const float4 v = *reinterpret_cast<const float4*>(p + j);
                         acc[j] += v.x; acc[j + 1] += v.y; acc[j + 2] += v.z; acc[j + 3] += v.w;
                     }
             } else {
 #pragma unroll
-                for (int j = 0; j < 128; ++j)
+                for (int j = 0; j < COUNT; ++j)
                     if (j < n) acc[j] += p[j];
             }
         }
         if (!a.dx_done) {
-            put_row(a.dx_acc + at, acc, n, al4);
+            put_row<COUNT>(a.dx_acc + at, acc, n, al4);
             return;
         }
     }
     void* out = problem == 0 ? a.dx : a.dw;
     const size_t to = problem == 0 ? at : at + (size_t)a.v0 * a.out_cols;
-    if (WIDE && a.out_f32) put_row(static_cast<float*>(out) + to, acc, n, al4);
-    else put_row(static_cast<__nv_bfloat16*>(out) + to, acc, n, a.out_cols % 8 == 0);
+    if (WIDE && a.out_f32) put_row<COUNT>(static_cast<float*>(out) + to, acc, n, al4);
+    else put_row<COUNT>(static_cast<__nv_bfloat16*>(out) + to, acc, n, a.out_cols % 8 == 0);
 }
 
 // Where cluster c keeps its sums over a part of the depth of a tile: one slot
@@ -185,40 +188,6 @@ __device__ __forceinline__ float* slot_of(const Args& a, const Walk<kProducts>& 
                                           int lane) {
     const size_t s = 2 * (size_t)c + (walk.bound(c) >= it.tile_lo ? 0 : 1);
     return a.partials + (((s * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + lane;
-}
-
-// The parts of a tile that several clusters share, once this cluster's are
-// stored: for each block of columns the warp that finds itself last adds the
-// parts up in the order of the depth, so the result does not depend on which
-// one is last, and writes the rows.
-template <int NB, bool WIDE>
-__device__ __forceinline__ void join_parts(const Args& a, const Walk<kProducts>& walk, const Item& it, int cluster, int rank, int ew,
-                                           int lane, int row, int half, float scale, float* acc) {
-    __threadfence();
-    __syncwarp();
-    int lo = cluster, hi = cluster, parts = 0;
-    while (walk.bound(lo) > it.tile_lo) --lo;
-    while (walk.bound(hi + 1) < it.tile_hi) ++hi;
-    for (int c = lo; c <= hi; ++c) parts += walk.bound(c + 1) > walk.bound(c);
-    unsigned before = 0;
-    if (lane < NB) before = atomicAdd(a.counters + ((lo * 2 + rank) * NB + lane) * kEpilogueWarps + ew, 1u);
-#pragma unroll 1
-    for (int b = 0; b < NB; ++b) {
-        const int c0 = it.n0 + 256 * b + 128 * half;
-        if ((int)__shfl_sync(0xffffffffu, before, b) != parts - 1) continue;
-        if (lane == b) a.counters[((lo * 2 + rank) * NB + b) * kEpilogueWarps + ew] = 0u;   // for the next piece
-        if (c0 >= a.out_cols) continue;
-        __threadfence();
-#pragma unroll
-        for (int j = 0; j < 128; ++j) acc[j] = 0.f;
-        for (int c = lo; c <= hi; ++c) {
-            if (walk.bound(c + 1) <= walk.bound(c)) continue;
-            const float* p = slot_of<NB>(a, walk, it, c, rank, b, ew, lane);
-#pragma unroll
-            for (int j = 0; j < 128; ++j) acc[j] += __ldcg(p + 32 * j);
-        }
-        write_product<WIDE>(a, it.problem, row, c0, scale, acc);
-    }
 }
 
 __device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
@@ -523,17 +492,16 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 } else if constexpr (MODE == kProducts) {
                     if (c0 >= a.out_cols) continue;          // (uniform over the warp)
                     if (it.whole) {
-                        write_product<WIDE>(a, it.problem, row, c0, out_scale, acc);
+                        write_product<WIDE, 128>(a, it.problem, row, c0, out_scale, acc);
                     } else {
                         float* mine = slot_of<NB>(a, walk, it, cluster, (int)rank, b, ew, lane);
+                        if (row < a.prob[it.problem].rows) {
 #pragma unroll
-                        for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
+                            for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
+                        }
                     }
                 }
             }
-            // (both blocks' accumulators are free by now: the next tile is under way)
-            if constexpr (MODE == kProducts)
-                if (!it.whole) join_parts<NB, WIDE>(a, walk, it, cluster, (int)rank, ew, lane, row, half, out_scale, acc);
         }
         if (MODE == kGradient && lane == 0) tc5::store_wait_all();
     }
@@ -548,11 +516,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
 // scale = the largest |dloss| of the rows with a target (1 if there is none or
 // it is not finite).  g is kept divided by it: with the mean's equal weights
 // the -1 of a target then is exact in bf16, where the weight itself would be
-// off by up to 2^-9 in every row alike.  Also clears the products' counters.
-__global__ void __launch_bounds__(1024) scale_kernel(Problem p, const float* dloss, float* scale, unsigned* counters, int n_counters) {
+// off by up to 2^-9 in every row alike.
+__global__ void __launch_bounds__(1024) scale_kernel(Problem p, const float* dloss, float* scale) {
     __shared__ float red[32];
     grid_dependency_sync();
-    for (int i = threadIdx.x; i < n_counters; i += 1024) counters[i] = 0u;
     float m = 0.f;
     for (int n = threadIdx.x; n < p.N; n += 1024) {
         const float d = fabsf(dloss[n]);
@@ -570,34 +537,108 @@ __global__ void __launch_bounds__(1024) scale_kernel(Problem p, const float* dlo
     }
 }
 
-// Rows of T as `planes` bf16 planes of row length `depth` (zeros past D): one
-// plane rounds nothing (bf16 rows of a length that TMA cannot address), three
-// hold an fp32 value to 24 bits.
-template <typename T> __global__ void __launch_bounds__(256) pack_kernel(const T* src, long long rows, int D, int depth, int planes,
-                                                                         __nv_bfloat16* dst) {
+// Rows of T as `planes` bf16 planes of row length `depth`, a multiple of eight
+// (zeros past D): one plane rounds nothing (bf16 rows of a length that TMA
+// cannot address), three hold an fp32 value to 24 bits.  A thread takes eight
+// values; two operands go in one launch.
+struct PackJob {
+    const void* src;
+    __nv_bfloat16* dst;
+    long long rows, groups;                        // groups of eight
+};
+template <typename T> __global__ void __launch_bounds__(256) pack_kernel(PackJob a, PackJob b, int D, int depth, int planes) {
     grid_dependency_sync();
-    const long long pairs = rows * (depth / 2);
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < pairs; i += gridDim.x * 256ll) {
-        const long long r = i / (depth / 2);
-        const int c = (int)(i % (depth / 2)) * 2;
-        float x0 = c < D ? to_f(src[r * D + c]) : 0.f, x1 = c + 1 < D ? to_f(src[r * D + c + 1]) : 0.f;
+    const int per_row = depth / 8;
+    const bool vectors = D % 8 == 0;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < a.groups + b.groups; i += gridDim.x * 256ll) {
+        const PackJob& job = i < a.groups ? a : b;
+        const long long g = i < a.groups ? i : i - a.groups, r = g / per_row;
+        const int c = (int)(g - r * per_row) * 8;
+        const T* src = static_cast<const T*>(job.src) + r * D + c;
+        float x[8];
+        if (vectors && c < D) {                   // (then the whole group is: D is a multiple of eight)
+            Vec8<T>::load(src, x);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = c + j < D ? to_f(src[j]) : 0.f;
+        }
         for (int p = 0; p < planes; ++p) {
-            const unsigned u = mma::pack_bf16(x0, x1);
-            reinterpret_cast<unsigned*>(dst)[p * pairs + i] = u;
-            x0 -= __uint_as_float(u << 16);
-            x1 -= __uint_as_float(u & 0xffff0000u);
+            unsigned u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u[j] = mma::pack_bf16(x[2 * j], x[2 * j + 1]);
+                x[2 * j] -= __uint_as_float(u[j] << 16);
+                x[2 * j + 1] -= __uint_as_float(u[j] & 0xffff0000u);
+            }
+            reinterpret_cast<uint4*>(job.dst)[p * job.groups + g] = make_uint4(u[0], u[1], u[2], u[3]);
         }
     }
 }
 
-cudaError_t pack(const void* src, long long rows, int D, int depth, int planes, void* dst, bool bf16, cudaStream_t st) {
-    const long long pairs = rows * (depth / 2);
-    const dim3 grid((unsigned)std::max(1ll, std::min(pairs / 256 + 1, 152ll * 8)));
-    if (bf16)
-        return launch_kernel(pack_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, static_cast<const __nv_bfloat16*>(src), rows, D,
-                             depth, planes, static_cast<__nv_bfloat16*>(dst));
-    return launch_kernel(pack_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(src), rows, D, depth, planes,
-                         static_cast<__nv_bfloat16*>(dst));
+// x and w as planes at x_to and w_to.
+cudaError_t pack(const Problem& p, int depth, int planes, void* x_to, void* w_to, bool bf16, cudaStream_t st) {
+    const PackJob x{p.x, static_cast<__nv_bfloat16*>(x_to), p.N, (long long)p.N * (depth / 8)};
+    const PackJob w{p.w, static_cast<__nv_bfloat16*>(w_to), p.V, (long long)p.V * (depth / 8)};
+    const dim3 grid((unsigned)std::max(1ll, std::min((x.groups + w.groups) / 256 + 1, 152ll * 8)));
+    return bf16 ? launch_kernel(pack_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, x, w, p.D, depth, planes)
+                : launch_kernel(pack_kernel<float>, grid, dim3(256), 0, st, x, w, p.D, depth, planes);
+}
+
+// The tiles that several clusters share: the sums of their parts, in the order
+// of the depth, by all SMs.  (A warp that finds itself the last of a tile's parts
+// could add them up inside the products; it then reads them through one SM: with
+// 64 rows, 512 wide, 32768 columns, where dx is one tile over 24 clusters, that
+// took 149 us of products against 26.5 and 8 for this kernel, and with 16384 rows,
+// two parts to a tile, the same time.)  Block (tile, group of 32 rows x 128
+// columns); a thread takes eight columns of a row.
+struct SplitTile {
+    int problem, m0, n0, first, parts;             // slots[first ..] hold its parts
+};
+struct SplitTiles {
+    int count;
+    SplitTile tile[kClusters];
+    short slots[2 * kClusters];
+};
+template <int NB, bool WIDE>
+__global__ void __launch_bounds__(512) join_products_kernel(const __grid_constant__ Args a, const __grid_constant__ SplitTiles s) {
+    grid_dependency_sync();
+    const SplitTile& t = s.tile[blockIdx.x];
+    const int ew = blockIdx.y % kEpilogueWarps, b = blockIdx.y / kEpilogueWarps % NB, rank = blockIdx.y / (kEpilogueWarps * NB);
+    const int lane = threadIdx.x & 31, j0 = (threadIdx.x >> 5) * 8;
+    const int row = t.m0 + 128 * rank + 32 * (ew & 3) + lane, c0 = t.n0 + 256 * b + 128 * (ew >> 2) + j0;
+    if (row >= a.prob[t.problem].rows || c0 >= a.out_cols) return;
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < t.parts; ++i) {
+        const float* p = a.partials + ((((size_t)s.slots[t.first + i] * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + 32 * j0 + lane;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] += __ldcg(p + 32 * j);
+    }
+    write_product<WIDE, 8>(a, t.problem, row, c0, *a.scale, acc);
+}
+
+// Which tiles the ranges of `clusters` clusters cut, and where their parts are.
+void find_splits(const Args& a, int clusters, SplitTiles* s) {
+    s->count = 0;
+    int used = 0, last = -1;
+    for (int c = 1; c < clusters; ++c) {
+        const int at = range_start(a, c, clusters);
+        if (at <= 0 || at >= a.total) continue;
+        const int p = at < a.split ? 0 : 1, kc = a.prob[p].chunks, base = p ? a.split : 0;
+        const int t = (at - base) / kc, lo = base + t * kc;
+        if (at == lo || lo == last) continue;      // a boundary between tiles, or a tile already listed
+        last = lo;
+        SplitTile& tile = s->tile[s->count++];
+        tile = SplitTile{p, t / a.prob[p].col_tiles * 256, t % a.prob[p].col_tiles * a.tile_cols, used, 0};
+        for (int k = c - 1; k < clusters && range_start(a, k, clusters) < lo + kc; ++k) {
+            const int from = range_start(a, k, clusters), to = range_start(a, k + 1, clusters);
+            if (to <= from || to <= lo) continue;
+            s->slots[used++] = (short)(2 * k + (from >= lo ? 0 : 1));
+            ++tile.parts;
+        }
+    }
 }
 
 bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, int planes, long long row_len, int box_cols,
@@ -638,11 +679,16 @@ template <int MODE, int NB, bool WIDE> cudaError_t launch(const Args& a, const M
 int tiles256(long long n) { return (int)((n + 255) / 256); }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Length, and need, of packed operand rows.
-void plan_operands(int D, bool bf16, bool* pack, int* planes, int* depth) {
-    *pack = !bf16 || D % 8 != 0;
+// Whether the operands are packed, into how many planes and rows of what
+// length.  bf16 rows are taken where they lie if TMA can address them (16-byte
+// rows); of those, rows that do not start on 32-byte boundaries cost the loads a
+// third of their rate, which from some 2500 rows on is more than the packing
+// takes (712 wide, 20000 columns, us forward in place / packed: 2048 rows 49.2 /
+// 50.4, 4096 rows 88.9 / 81.6, 8192 rows 165 / 147).
+void plan_operands(int N, int D, bool bf16, bool* pack, int* planes, int* depth) {
+    *pack = !bf16 || D % 8 != 0 || (D % 16 != 0 && N >= 2560);
     *planes = bf16 ? 1 : 3;
-    *depth = (D + 7) / 8 * 8;
+    *depth = *pack ? (D + 15) / 16 * 16 : D;
 }
 
 // The products of planes that make up one of values, the small ones first:
@@ -685,11 +731,22 @@ static int unit_tiles_of(int row_tiles, int col_tiles) {
     return unit;
 }
 
+//
+// A handful of rows goes as a stream over w instead (us on the GPU, stream /
+// tensor cores, depth 512, 32768 columns): bf16, which the tensor cores take as
+// it lies, 10.6 / 21.6 for one row, 16.6 / 26.2 for four, 28.6 / 24.9 for eight;
+// fp32, which has to be split into planes for them, 16 / 104 for one row, 56 / 91
+// for sixteen, 104 / 92 for thirty-two.
 FwdPlan plan_forward(int N, int D, int V, bool bf16) {
     FwdPlan f{};
-    plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
-    f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
-    f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
+    f.few_rows = N <= (bf16 ? 4 : 16);
+    if (f.few_rows) {
+        f.segments = few_rows_segments(N, V);
+    } else {
+        plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
+        f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
+        f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
+    }
     size_t off = 0;
     const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };
     f.x = take(f.pack ? (size_t)f.planes * N * f.depth * 2 : 0);
@@ -702,12 +759,21 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16) {
 }
 
 cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st) {
-    const void *x = p.x, *w = p.w;
+    const FwdParts parts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l), reinterpret_cast<float*>(ws + f.target)};
     cudaError_t e;
+    if (f.few_rows) {
+        {
+            ProfScope s("xent_few_rows", st);
+            e = launch_few_rows(p, parts, f.segments, bf16, st);
+        }
+        if (e != cudaSuccess) return e;
+        ProfScope s("xent_join", st);
+        return launch_join_rows(p, parts, f.segments, loss, lse, st);
+    }
+    const void *x = p.x, *w = p.w;
     if (f.pack) {
         ProfScope s("xent_pack", st);
-        if ((e = pack(p.x, p.N, p.D, f.depth, f.planes, ws + f.x, bf16, st)) != cudaSuccess) return e;
-        if ((e = pack(p.w, p.V, p.D, f.depth, f.planes, ws + f.w, bf16, st)) != cudaSuccess) return e;
+        if ((e = pack(p, f.depth, f.planes, ws + f.x, ws + f.w, bf16, st)) != cudaSuccess) return e;
         x = ws + f.x;
         w = ws + f.w;
     }
@@ -722,7 +788,7 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     a.col_tiles = tiles256(p.V);
     a.unit_tiles = f.unit_tiles;
     a.units = a.row_tiles * (f.segments / 2);
-    a.parts = FwdParts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l), reinterpret_cast<float*>(ws + f.target)};
+    a.parts = parts;
     const int clusters = std::min(kClusters, a.units);
     {
         ProfScope s("xent_fwd", st);
@@ -730,8 +796,26 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
         e = bf16 ? launch<kForward, 1, false>(a, maps, clusters, st) : launch<kForward, 1, true>(a, maps, clusters, st);
     }
     if (e != cudaSuccess) return e;
-    ProfScope s("xent_combine", st);
-    return launch_combine(p, a.parts, f.segments, loss, lse, st);
+    ProfScope s("xent_join", st);
+    return launch_join_segments(p, a.parts, f.segments, loss, lse, st);
+}
+
+// Divides the products' chunks among the clusters and returns how many take
+// part: dx and dw get clusters by their work, with a tile's own cost counted as
+// `tile` chunks, and no part of a tile is below `least` chunks.
+static int share_products(Args* a, int dx_tiles, int dw_tiles, bool wide) {
+    const int tile = wide ? 3 : 8, least = wide ? 4 : 12;
+    const int dx_chunks = a->prob[0].chunks, dw_chunks = a->prob[1].chunks;
+    const int dx = dx_tiles * dx_chunks, dw = dw_tiles * dw_chunks;
+    a->split = dx;
+    a->total = dx + dw;
+    const double cost_dx = dx + (double)tile * dx_tiles, cost_dw = dw + (double)tile * dw_tiles;
+    const int fair = std::max(1, std::min(kClusters - 1, (int)(kClusters * cost_dx / (cost_dx + cost_dw) + 0.5)));
+    a->first_dw = (int)std::min<long long>(fair, (long long)dx_tiles * std::max(1, dx_chunks / least));
+    const int for_dw = (int)std::min<long long>(kClusters - a->first_dw, (long long)dw_tiles * std::max(1, dw_chunks / least));
+    a->snap[0] = std::min(wide ? 4 : 16, dx / a->first_dw / 4);
+    a->snap[1] = std::min(wide ? 4 : 16, dw / for_dw / 4);
+    return a->first_dw + for_dw;
 }
 
 // g of a piece is held in memory for the two products: at most 512 MiB of it
@@ -742,7 +826,7 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
 // behind the launches.
 BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     BwdPlan f{};
-    plan_operands(D, bf16, &f.pack, &f.planes, &f.depth);
+    plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
     f.wide = !bf16 || (double)N * D * V <= (double)(1 << 26);
     f.g_planes = f.wide ? 3 : 1;
     f.blocks = !f.wide && D > 256 ? 2 : 1;
@@ -756,7 +840,6 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     f.g = take((size_t)f.g_planes * N * f.ldg * 2);
     f.dx_acc = take(f.cols < V ? (size_t)N * D * 4 : 0);
     f.partials = take((size_t)kClusters * 2 * f.blocks * 256 * 256 * 4);
-    f.counters = take((size_t)kClusters * 2 * f.blocks * kEpilogueWarps * 4);
     f.scale = take(4);
     f.total = off;
     return f;
@@ -768,8 +851,7 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     cudaError_t e;
     if (f.pack) {
         ProfScope s("xent_pack", st);
-        if ((e = pack(p.x, p.N, p.D, f.depth, f.planes, ws + f.x, bf16, st)) != cudaSuccess) return e;
-        if ((e = pack(p.w, p.V, p.D, f.depth, f.planes, ws + f.w, bf16, st)) != cudaSuccess) return e;
+        if ((e = pack(p, f.depth, f.planes, ws + f.x, ws + f.w, bf16, st)) != cudaSuccess) return e;
         x = ws + f.x;
         w = ws + f.w;
     }
@@ -785,10 +867,8 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     a.dloss = dloss;
     a.out_cols = p.D;
     a.tile_cols = 256 * f.blocks;
-    a.snap = f.wide ? 4 : 16;
     a.out_f32 = !bf16;
     a.partials = reinterpret_cast<float*>(ws + f.partials);
-    a.counters = reinterpret_cast<unsigned*>(ws + f.counters);
     float* scale = reinterpret_cast<float*>(ws + f.scale);
     a.scale = scale;
     a.dx_acc = reinterpret_cast<float*>(ws + f.dx_acc);
@@ -796,8 +876,7 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     a.dw = dw;
     {
         ProfScope s("xent_scale", st);
-        e = launch_kernel(scale_kernel, dim3(1), dim3(1024), 0, st, p, dloss, scale, a.counters,
-                          kClusters * 2 * f.blocks * kEpilogueWarps);
+        e = launch_kernel(scale_kernel, dim3(1), dim3(1024), 0, st, p, dloss, scale);
     }
     if (e != cudaSuccess) return e;
     for (int v0 = 0; v0 < p.V; v0 += f.cols) {
@@ -823,18 +902,27 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
         const int d_tiles = (p.D + a.tile_cols - 1) / a.tile_cols;
         a.prob[0] = Product{p.N, d_tiles, (cols + 63) / 64};
         a.prob[1] = Product{cols, d_tiles, (p.N + 63) / 64};
-        a.split = tiles256(p.N) * d_tiles * a.prob[0].chunks;
-        a.total = a.split + tiles256(cols) * d_tiles * a.prob[1].chunks;
+        const int workers = share_products(&a, tiles256(p.N) * d_tiles, tiles256(cols) * d_tiles, f.wide);
         a.dx_add = v0 > 0;
         a.dx_done = v0 + cols >= p.V;
         {
             ProfScope s("xent_products", st);
             set_combos(&a, f.g_planes, f.planes);
-            e = f.wide ? launch<kProducts, 1, true>(a, products, kClusters, st)
-                : f.blocks == 2 ? launch<kProducts, 2, false>(a, products, kClusters, st)
-                          : launch<kProducts, 1, false>(a, products, kClusters, st);
+            e = f.wide ? launch<kProducts, 1, true>(a, products, workers, st)
+                : f.blocks == 2 ? launch<kProducts, 2, false>(a, products, workers, st)
+                          : launch<kProducts, 1, false>(a, products, workers, st);
         }
         if (e != cudaSuccess) return e;
+        SplitTiles splits;
+        find_splits(a, workers, &splits);
+        if (splits.count > 0) {
+            ProfScope s("xent_join_products", st);
+            const dim3 grid(splits.count, 2 * f.blocks * kEpilogueWarps);
+            e = f.wide ? launch_kernel(join_products_kernel<1, true>, grid, dim3(512), 0, st, a, splits)
+                : f.blocks == 2 ? launch_kernel(join_products_kernel<2, false>, grid, dim3(512), 0, st, a, splits)
+                                : launch_kernel(join_products_kernel<1, false>, grid, dim3(512), 0, st, a, splits);
+            if (e != cudaSuccess) return e;
+        }
     }
     return cudaSuccess;
 }

@@ -24,12 +24,11 @@ struct Args {
     const float* dloss;
     int v0, cols;                                  // the piece of the vocabulary
     // products: the chunks of all tiles of prob[0] (dx), then of prob[1] (dw),
-    // one after another, make `total`; prob[1] starts at `split`
+    // one after another, make `total`; prob[1] starts at `split`, its clusters at first_dw
     Product prob[2];
-    int split, total, snap;
+    int split, total, first_dw, snap[2];
     int tile_cols, out_cols;                       // columns of a tile, of the results (D)
     float* partials;                               // sums over a part of a tile's depth
-    unsigned* counters;                            // parts of a tile that have arrived
     const float* scale;                            // g is divided by it, the products multiplied
     float* dx_acc;                                 // dx over the earlier pieces, fp32
     bool dx_add, dx_done;                          // there are earlier pieces; this is the last one
@@ -46,6 +45,7 @@ struct Maps {
 };
 
 struct FwdPlan {
+    bool few_rows;                                 // not on the tensor cores: one stream over w
     bool pack;
     int planes, depth;                             // of packed operands: planes, row length
     int unit_tiles, segments;                      // segments: entries of a row in FwdParts
@@ -59,7 +59,7 @@ struct BwdPlan {
     int planes, depth, g_planes;
     int blocks;                                    // blocks of 256 columns of a products' tile
     int cols, ldg;                                 // columns of a piece; row length of g
-    size_t x, w, g, dx_acc, partials, counters, scale, total;
+    size_t x, w, g, dx_acc, partials, scale, total;
 };
 BwdPlan plan_backward(int N, int D, int V, bool bf16);
 cudaError_t run_backward(const Problem& p, const BwdPlan& plan, char* ws, bool bf16, const float* lse, const float* dloss,
