@@ -116,8 +116,11 @@ template <int MODE> struct Walk {
 
 // Columns of block b of a product's tile that are multiplied: a multiple of 32.
 __device__ __forceinline__ int block_columns(const Args& a, const Item& it, int b) {
-    return min(256, max(0, (a.out_cols - it.n0 - 256 * b + 31) & ~31));
+    return min(256, max(0, (min(a.out_cols - it.n0, a.tile_cols) - 256 * b + 31) & ~31));
 }
+
+// Boxes of 64 columns that each CTA of the pair loads of them.
+__device__ __forceinline__ int block_boxes(const Args& a, const Item& it, int b) { return (block_columns(a, it, b) + 127) / 128; }
 
 // COUNT columns of one output row from registers.  `aligned`: rows start on
 // 16-byte boundaries (then no group of 16 bytes straddles the end of a row).
@@ -144,12 +147,11 @@ template <int COUNT> __device__ __forceinline__ void put_row(__nv_bfloat16* out,
     }
 }
 
-// Row `row`, columns from c0 of a finished product.  What g was divided by is
+// Row `row`, n columns (COUNT at most) from c0 of a finished product.  What g was divided by is
 // multiplied back here.
 template <bool WIDE, int COUNT>
-__device__ __forceinline__ void write_product(const Args& a, int problem, int row, int c0, float scale, float* acc) {
+__device__ __forceinline__ void write_product(const Args& a, int problem, int row, int c0, int n, float scale, float* acc) {
     if (row >= a.prob[problem].rows) return;
-    const int n = a.out_cols - c0;
     const size_t at = (size_t)row * a.out_cols + c0;
     const bool al4 = a.out_cols % 4 == 0;
 #pragma unroll
@@ -237,6 +239,11 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         if (warp == 0 && tc5::elect_one()) {
             // ---- loads: this CTA's operands; the even CTA's barrier counts both's bytes
             const unsigned full0 = tc5::map_to(full, 0);
+            // x and w are read by every cluster; g passes through once in each product (but
+            // its planes are read for several products of planes).  (Hints
+            // of 16384 rows, 512 wide, 32768 columns: gradient 360 -> 344 us, products 644 -> 614;
+            // a hint on g's stores changes neither.)
+            const unsigned long long keep = tc5::policy_keep(), pass = WIDE ? tc5::policy_normal() : tc5::policy_pass();
             Walk<MODE> walk(a, cluster, clusters);
             Item it;
             int stage = 0;
@@ -244,6 +251,12 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
             long long issued = 0;
             bool ok = true;
             while (ok && walk.next(it)) {
+                unsigned bytes = 2 * C::kStageBytes;       // of a stage, both CTAs
+                if (MODE == kProducts) {
+                    bytes = 2 * kOperandBytes;
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) bytes += 2 * 8192u * block_boxes(a, it, b);
+                }
                 for (int r0 = it.k0; ok && r0 < it.k1; r0 += min(kRun, it.k1 - r0)) {
                     const int len = min(kRun, it.k1 - r0);
                     for (int i = 0; i < combos * len; ++i) {
@@ -252,24 +265,24 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         const int pb = WIDE ? (a.combo_b >> (4 * (i / len))) & 15 : 0;
                         ok = tc5::wait_parity(empty + 8 * stage, phase ^ 1u);
                         if (!ok) break;
-                        if (rank == 0) tc5::expect_bytes(full + 8 * stage, 2 * C::kStageBytes);
+                        if (rank == 0) tc5::expect_bytes(full + 8 * stage, bytes);
                         const unsigned bar = full0 + 8 * stage, dst = smem0 + stage * C::kStageBytes;
                         if (MODE != kProducts) {
-                            tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar);
-                            tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar);
+                            tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
+                            tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
                         } else {
                             if (it.problem == 0) {
-                                tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar);
+                                tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, pass);
                             } else {
                                 for (int h = 0; h < 2; ++h)
-                                    tc5::load_box(dst + 8192 * h, &maps.m[2], it.m0 + 128 * rank + 64 * h, chunk * 64, pa, bar);
+                                    tc5::load_box(dst + 8192 * h, &maps.m[2], it.m0 + 128 * rank + 64 * h, chunk * 64, pa, bar, pass);
                             }
                             for (int b = 0; b < NB; ++b) {
                                 const int n = it.n0 + 256 * b + (int)rank * (block_columns(a, it, b) / 2);
                                 // the innermost coordinate starts on a 16-byte boundary: block_columns / 2 is a multiple of 16
-                                for (int h = 0; h < 2; ++h)
+                                for (int h = 0; h < block_boxes(a, it, b); ++h)
                                     tc5::load_box(dst + kOperandBytes * (1 + b) + 8192 * h, &maps.m[it.problem == 0 ? 1 : 3],
-                                                  n + 64 * h, (it.problem == 0 ? a.v0 : 0) + chunk * 64, pb, bar);
+                                                  n + 64 * h, (it.problem == 0 ? a.v0 : 0) + chunk * 64, pb, bar, keep);
                             }
                         }
                         ++issued;
@@ -303,6 +316,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     cols[b] = MODE == kProducts ? block_columns(a, it, b) : 256;
                     idesc[b] = tc5::instruction(cols[b], a_rows, b_rows);
                 }
+                const int depth = MODE != kProducts ? a.p.D : it.problem == 0 ? a.cols : a.p.N;
                 const unsigned a_step = a_rows ? 128u : 2u, b_step = b_rows ? 128u : 2u;   // 16 of depth, in 16 bytes
                 for (int r0 = it.k0; ok && r0 < it.k1; r0 += min(kRun, it.k1 - r0), ++run) {
                     const int len = min(kRun, it.k1 - r0);
@@ -315,6 +329,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         ok = tc5::wait_parity(full + 8 * stage, phase);
                         if (!ok) break;
                         tc5::fence_after();
+                        const int left = depth - 64 * (r0 + (WIDE ? i % len : i));   // what is past the depth is zeros
                         const unsigned src = smem0 + stage * C::kStageBytes;
                         const unsigned long long da = tc5::descriptor(src, a_rows ? 8192u : 16u);
 #pragma unroll
@@ -323,7 +338,8 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                             if (cols[b] > 0) {
 #pragma unroll
                                 for (unsigned k = 0; k < 4; ++k)
-                                    tc5::multiply(tmem + 256 * (buf + b), da + a_step * k, db + b_step * k, idesc[b], i > 0 || k > 0);
+                                    if ((int)(16 * k) < left)
+                                        tc5::multiply(tmem + 256 * (buf + b), da + a_step * k, db + b_step * k, idesc[b], i > 0 || k > 0);
                             }
                         }
                         tc5::commit_pair(empty + 8 * stage);
@@ -490,9 +506,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         }
                     }
                 } else if constexpr (MODE == kProducts) {
-                    if (c0 >= a.out_cols) continue;          // (uniform over the warp)
+                    const int end = min(a.out_cols, it.n0 + a.tile_cols);
+                    if (c0 >= end) continue;                 // (uniform over the warp)
                     if (it.whole) {
-                        write_product<WIDE, 128>(a, it.problem, row, c0, out_scale, acc);
+                        write_product<WIDE, 128>(a, it.problem, row, c0, end - c0, out_scale, acc);
                     } else {
                         float* mine = slot_of<NB>(a, walk, it, cluster, (int)rank, b, ew, lane);
                         if (row < a.prob[it.problem].rows) {
@@ -606,7 +623,8 @@ __global__ void __launch_bounds__(512) join_products_kernel(const __grid_constan
     const int ew = blockIdx.y % kEpilogueWarps, b = blockIdx.y / kEpilogueWarps % NB, rank = blockIdx.y / (kEpilogueWarps * NB);
     const int lane = threadIdx.x & 31, j0 = (threadIdx.x >> 5) * 8;
     const int row = t.m0 + 128 * rank + 32 * (ew & 3) + lane, c0 = t.n0 + 256 * b + 128 * (ew >> 2) + j0;
-    if (row >= a.prob[t.problem].rows || c0 >= a.out_cols) return;
+    const int end = min(a.out_cols, t.n0 + a.tile_cols);
+    if (row >= a.prob[t.problem].rows || c0 >= end) return;
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
@@ -616,7 +634,7 @@ __global__ void __launch_bounds__(512) join_products_kernel(const __grid_constan
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += __ldcg(p + 32 * j);
     }
-    write_product<WIDE, 8>(a, t.problem, row, c0, *a.scale, acc);
+    write_product<WIDE, 8>(a, t.problem, row, c0, end - c0, *a.scale, acc);
 }
 
 // Which tiles the ranges of `clusters` clusters cut, and where their parts are.
@@ -866,7 +884,9 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     a.lse = lse;
     a.dloss = dloss;
     a.out_cols = p.D;
-    a.tile_cols = 256 * f.blocks;
+    // equal tiles of at most 256 * blocks columns: 712 goes as 384 and 328, not as 512 and 200
+    const int d_tiles = (p.D + 256 * f.blocks - 1) / (256 * f.blocks);
+    a.tile_cols = ((p.D + d_tiles - 1) / d_tiles + 31) / 32 * 32;
     a.out_f32 = !bf16;
     a.partials = reinterpret_cast<float*>(ws + f.partials);
     float* scale = reinterpret_cast<float*>(ws + f.scale);
@@ -899,7 +919,6 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
             e = f.wide ? launch<kGradient, 1, true>(a, logits, clusters, st) : launch<kGradient, 1, false>(a, logits, clusters, st);
         }
         if (e != cudaSuccess) return e;
-        const int d_tiles = (p.D + a.tile_cols - 1) / a.tile_cols;
         a.prob[0] = Product{p.N, d_tiles, (cols + 63) / 64};
         a.prob[1] = Product{cols, d_tiles, (p.N + 63) / 64};
         const int workers = share_products(&a, tiles256(p.N) * d_tiles, tiles256(cols) * d_tiles, f.wide);
