@@ -36,9 +36,15 @@ struct FwdParts {
 // The tensor-core forward keeps them as [segment][row] ...
 cudaError_t launch_join_segments(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st);
 // ... the forward of few rows as [row][segment].
-int few_rows_segments(int N, int V);
+int few_rows_segments(int V);
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);
 cudaError_t launch_join_rows(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st);
+
+// The gradient of few rows: parts is [blocks][N][D] fp32 of scratch.
+int few_rows_at_most(int N, int D);                // rows that it can take, of N
+int few_rows_blocks(int V);
+cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts,
+                                     int blocks, bool bf16, cudaStream_t st);
 
 }  // namespace xent
 }  // namespace fibattn

@@ -47,7 +47,7 @@ template <int MODE, int NB> struct Config {
 // chunks of 64 from k0 to k1.
 struct Item {
     int m0, n0, k0, k1;
-    int problem;                                   // products: 0 dx, 1 dw
+    int problem = 0;                                 // products: 0 dx, 1 dw
     int unit;                                      // forward, gradient: segment of the columns
     bool first, last;                              // forward, gradient: tile of its unit
     bool whole;                                    // products: the whole depth
@@ -194,6 +194,36 @@ __device__ __forceinline__ float* slot_of(const Args& a, const Walk<kProducts>& 
 
 __device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
 
+// The largest of 256 threads' values (of 8 warps in a row, t counted from the
+// first); they meet at named barrier 1.
+__device__ __forceinline__ float block_max(float m, float* red, int t) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (t % 32 == 0) red[t / 32] = m;
+    asm volatile("bar.sync 1, 256;\n" ::: "memory");
+    m = red[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) m = fmaxf(m, red[w]);
+    return m;
+}
+
+// g is kept divided by the largest |dloss| of the rows with a target (by 1 if
+// there is none or it is not finite): with the mean's equal weights the -1 of a
+// target then is exact in bf16, where the weight itself would be off by up to
+// 2^-9 in every row alike.  Every block finds it for itself, from all rows or
+// from the maxima of another launch.
+__device__ __forceinline__ float find_scale(const Args& a, float* red, int t) {
+    float m = 0.f;
+    if (a.n_maxima > 0) {
+        for (int i = t; i < a.n_maxima; i += 256) m = fmaxf(m, a.maxima[i]);
+    } else {
+        for (int n = t; n < a.p.N; n += 256)
+            if (target_column(a.p, n) >= 0) m = fmaxf(m, fabsf(a.dloss[n]));
+    }
+    m = block_max(m, red, t);
+    return m > 0.f && m < INFINITY ? m : 1.f;
+}
+
 template <int MODE, int NB, bool WIDE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
@@ -201,6 +231,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     extern __shared__ unsigned char smem_raw[];
     __shared__ unsigned long long bars[2 * C::kStages + 4];
     __shared__ unsigned tmem_base_s;
+    __shared__ float red_s[MODE == kGradient ? kEpilogueWarps : 1];
     const unsigned smem0 = (tc5::smem_u32(smem_raw) + 1023u) & ~1023u;
     const unsigned full = tc5::smem_u32(bars), empty = full + 8 * C::kStages;
     const unsigned acc_full = empty + 8 * C::kStages, acc_empty = acc_full + 16;
@@ -251,9 +282,16 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
             long long issued = 0;
             bool ok = true;
             while (ok && walk.next(it)) {
-                unsigned bytes = 2 * C::kStageBytes;       // of a stage, both CTAs
-                if (MODE == kProducts) {
-                    bytes = 2 * kOperandBytes;
+                // Bytes of a stage, both CTAs.  Half tiles without a row or a column are not
+                // loaded: what a stale operand gives goes to rows and columns that nobody
+                // looks at, and boxes that lie outside their tensor are slow to fill.
+                const bool a_here = it.problem == 1 || it.m0 + 128 * (int)rank < a.p.N;
+                const bool b_here = MODE == kProducts || a.v0 + it.n0 + 128 * (int)rank < a.p.V;
+                unsigned bytes = MODE == kProducts && it.problem == 1 ? 2 * kOperandBytes
+                                                                      : a.row_box * 128u * (it.m0 + 128 < a.p.N ? 2 : 1);
+                if (MODE != kProducts) {
+                    bytes += kOperandBytes * (a.v0 + it.n0 + 128 < a.p.V ? 2 : 1);
+                } else {
 #pragma unroll
                     for (int b = 0; b < NB; ++b) bytes += 2 * 8192u * block_boxes(a, it, b);
                 }
@@ -268,11 +306,11 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         if (rank == 0) tc5::expect_bytes(full + 8 * stage, bytes);
                         const unsigned bar = full0 + 8 * stage, dst = smem0 + stage * C::kStageBytes;
                         if (MODE != kProducts) {
-                            tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
-                            tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
+                            if (a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
+                            if (b_here) tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
                         } else {
                             if (it.problem == 0) {
-                                tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, pass);
+                                if (a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, pass);
                             } else {
                                 for (int h = 0; h < 2; ++h)
                                     tc5::load_box(dst + 8192 * h, &maps.m[2], it.m0 + 128 * rank + 64 * h, chunk * 64, pa, bar, pass);
@@ -366,7 +404,13 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         bool ok = true;
         float m = -INFINITY, l = 0.f, z = 0.f, z2 = 0.f, dl = 0.f;
         int target = kIgnored;
-        const float out_scale = MODE == kForward ? 1.f : *a.scale;
+        float out_scale = 1.f;
+        if (MODE == kGradient) {
+            out_scale = find_scale(a, red_s, threadIdx.x - 128);
+            if (blockIdx.x == 0 && threadIdx.x == 128) *a.scale = out_scale;
+        } else if (MODE == kProducts) {
+            out_scale = *a.scale;
+        }
         while (walk.next(it)) {
             const int row = it.m0 + 128 * (int)rank + lane_row;
             if (MODE == kForward && it.first) {
@@ -530,28 +574,15 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
     if (warp == 2) tc5::tmem_free(tmem);
 }
 
-// scale = the largest |dloss| of the rows with a target (1 if there is none or
-// it is not finite).  g is kept divided by it: with the mean's equal weights
-// the -1 of a target then is exact in bf16, where the weight itself would be
-// off by up to 2^-9 in every row alike.
-__global__ void __launch_bounds__(1024) scale_kernel(Problem p, const float* dloss, float* scale) {
-    __shared__ float red[32];
+// maxima[block] = the largest |dloss| of the block's rows that have a target.
+__global__ void __launch_bounds__(256) maxima_kernel(Problem p, const float* dloss, float* maxima) {
+    __shared__ float red[8];
     grid_dependency_sync();
     float m = 0.f;
-    for (int n = threadIdx.x; n < p.N; n += 1024) {
-        const float d = fabsf(dloss[n]);
-        if (target_column(p, n) >= 0) m = fmaxf(m, d);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = m;
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        m = red[threadIdx.x];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (threadIdx.x == 0) *scale = m > 0.f && m < INFINITY ? m : 1.f;
-    }
+    for (int n = blockIdx.x * 256 + threadIdx.x; n < p.N; n += gridDim.x * 256)
+        if (target_column(p, n) >= 0) m = fmaxf(m, fabsf(dloss[n]));
+    m = block_max(m, red, threadIdx.x);
+    if (threadIdx.x == 0) maxima[blockIdx.x] = m;
 }
 
 // Rows of T as `planes` bf16 planes of row length `depth`, a multiple of eight
@@ -694,6 +725,9 @@ template <int MODE, int NB, bool WIDE> cudaError_t launch(const Args& a, const M
     return launch_kernel(kern, dim3(2 * clusters), dim3(kThreads), smem, st, a, maps);
 }
 
+// Rows of the boxes that x (and g, for dx) are loaded in: whole groups of eight.
+int row_box_of(int N) { return std::min(128, (N + 7) / 8 * 8); }
+
 int tiles256(long long n) { return (int)((n + 255) / 256); }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -749,19 +783,26 @@ static int unit_tiles_of(int row_tiles, int col_tiles) {
     return unit;
 }
 
-//
-// A handful of rows goes as a stream over w instead (us on the GPU, stream /
-// tensor cores, depth 512, 32768 columns): bf16, which the tensor cores take as
-// it lies, 10.6 / 21.6 for one row, 16.6 / 26.2 for four, 28.6 / 24.9 for eight;
-// fp32, which has to be split into planes for them, 16 / 104 for one row, 56 / 91
-// for sixteen, 104 / 92 for thirty-two.
+// Whether a handful of rows goes in one pass over w (xent_rows.cu) rather than to
+// the tensor cores.  Forward and backward go the same way: p = exp(logit - lse) is
+// good to the logits' own rounding only if both come from the same arithmetic.
+// Forward and backward together, us on the GPU, one pass / tensor cores:
+//   512 wide, 32768 columns: bf16 35 / 60 (one row), 48 / 60 (four), 80 / 58 (eight);
+//                            fp32 58 / 230 (one row), 93 / 220 (eight)
+//   512 wide, 4000 columns:  bf16 23 / 30 (eight);  64 wide, 257 columns: bf16 15 / 26 (eight)
+static bool stream_wins(int N, int D, int V, bool bf16) {
+    const int most = !bf16 || (long long)V * D <= (4 << 20) ? 8 : 4;
+    return N <= std::min(most, few_rows_at_most(N, D));
+}
+
 FwdPlan plan_forward(int N, int D, int V, bool bf16) {
     FwdPlan f{};
-    f.few_rows = N <= (bf16 ? 4 : 16);
+    plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
+    f.few_rows = stream_wins(N, D, V, bf16);
     if (f.few_rows) {
-        f.segments = few_rows_segments(N, V);
+        f.pack = false;
+        f.segments = few_rows_segments(V);
     } else {
-        plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
         f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
         f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
     }
@@ -796,11 +837,12 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
         w = ws + f.w;
     }
     Maps maps{};
-    if (!encode(&maps.m[0], x, f.depth, p.N, f.planes, f.depth, 64, 128) ||
+    if (!encode(&maps.m[0], x, f.depth, p.N, f.planes, f.depth, 64, row_box_of(p.N)) ||
         !encode(&maps.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 128))
         return cudaErrorInvalidValue;
     Args a{};
     a.p = p;
+    a.row_box = row_box_of(p.N);
     a.chunks = (p.D + 63) / 64;
     a.row_tiles = tiles256(p.N);
     a.col_tiles = tiles256(p.V);
@@ -840,12 +882,19 @@ static int share_products(Args* a, int dx_tiles, int dw_tiles, bool wide) {
 // (at least 256 columns; 16384 rows, 512 wide, 32768 columns: two products launches of
 // 339 us; pieces of 256 MiB 791 us together, one piece 650 us).  One bf16 plane rounds each g to 8 bits, which the
 // products average out over many; fp32 I/O keeps three planes (24 bits), and so
-// does bf16 I/O below 2^26 multiplications, where the further planes hide
-// behind the launches.
+// does bf16 I/O where whole tiles come to at most 2^26 multiplications: there the
+// sums are short and the further planes hide behind the launches (100 rows, 64
+// wide, 257 columns: 27 us either way).
 BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     BwdPlan f{};
+    f.few_rows = stream_wins(N, D, V, bf16);
+    if (f.few_rows) {
+        f.partials = 0;
+        f.total = up256((size_t)few_rows_blocks(V) * N * D * 4);
+        return f;
+    }
     plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
-    f.wide = !bf16 || (double)N * D * V <= (double)(1 << 26);
+    f.wide = !bf16 || 256.0 * tiles256(N) * 256.0 * tiles256(V) * D <= (double)(1 << 26);
     f.g_planes = f.wide ? 3 : 1;
     f.blocks = !f.wide && D > 256 ? 2 : 1;
     const long long fit = (512ll << 20) / (2ll * f.g_planes * std::max(N, 1)) / 256 * 256;
@@ -858,13 +907,16 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     f.g = take((size_t)f.g_planes * N * f.ldg * 2);
     f.dx_acc = take(f.cols < V ? (size_t)N * D * 4 : 0);
     f.partials = take((size_t)kClusters * 2 * f.blocks * 256 * 256 * 4);
-    f.scale = take(4);
+    f.maxima = N <= 4096 ? 0 : std::min(152, N / 2048);       // few rows: every block looks at all of them
+    f.scale = take((size_t)(1 + f.maxima) * 4);
     f.total = off;
     return f;
 }
 
 cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16, const float* lse, const float* dloss, void* dx,
                          void* dw, cudaStream_t st) {
+    if (f.few_rows)
+        return launch_few_rows_gradient(p, lse, dloss, dx, dw, reinterpret_cast<float*>(ws + f.partials), few_rows_blocks(p.V), bf16, st);
     const void *x = p.x, *w = p.w;
     cudaError_t e;
     if (f.pack) {
@@ -874,13 +926,14 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
         w = ws + f.w;
     }
     Maps logits{}, products{};
-    if (!encode(&logits.m[0], x, f.depth, p.N, f.planes, f.depth, 64, 128) ||
+    if (!encode(&logits.m[0], x, f.depth, p.N, f.planes, f.depth, 64, row_box_of(p.N)) ||
         !encode(&logits.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 128) ||
         !encode(&products.m[1], w, f.depth, p.V, f.planes, f.depth, 64, 64) ||
         !encode(&products.m[3], x, f.depth, p.N, f.planes, f.depth, 64, 64))
         return cudaErrorInvalidValue;
     Args a{};
     a.p = p;
+    a.row_box = row_box_of(p.N);
     a.lse = lse;
     a.dloss = dloss;
     a.out_cols = p.D;
@@ -889,20 +942,22 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     a.tile_cols = ((p.D + d_tiles - 1) / d_tiles + 31) / 32 * 32;
     a.out_f32 = !bf16;
     a.partials = reinterpret_cast<float*>(ws + f.partials);
-    float* scale = reinterpret_cast<float*>(ws + f.scale);
-    a.scale = scale;
+    a.scale = reinterpret_cast<float*>(ws + f.scale);
     a.dx_acc = reinterpret_cast<float*>(ws + f.dx_acc);
     a.dx = dx;
     a.dw = dw;
-    {
-        ProfScope s("xent_scale", st);
-        e = launch_kernel(scale_kernel, dim3(1), dim3(1024), 0, st, p, dloss, scale);
+    if (f.maxima > 0) {
+        ProfScope s("xent_maxima", st);
+        float* maxima = reinterpret_cast<float*>(ws + f.scale) + 1;
+        a.maxima = maxima;
+        a.n_maxima = f.maxima;
+        e = launch_kernel(maxima_kernel, dim3(f.maxima), dim3(256), 0, st, p, dloss, maxima);
+        if (e != cudaSuccess) return e;
     }
-    if (e != cudaSuccess) return e;
     for (int v0 = 0; v0 < p.V; v0 += f.cols) {
         const int cols = std::min(f.cols, p.V - v0);
         if (!encode(&logits.m[2], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 32) ||
-            !encode(&products.m[0], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 128) ||
+            !encode(&products.m[0], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, row_box_of(p.N)) ||
             !encode(&products.m[2], ws + f.g, cols, p.N, f.g_planes, f.ldg, 64, 64))
             return cudaErrorInvalidValue;
         a.v0 = v0;

@@ -29,7 +29,10 @@ struct Args {
     int split, total, first_dw, snap[2];
     int tile_cols, out_cols;                       // columns of a tile, of the results (D)
     float* partials;                               // sums over a part of a tile's depth
-    const float* scale;                            // g is divided by it, the products multiplied
+    float* scale;                                  // g is divided by it, the products multiplied
+    const float* maxima;                           // of |dloss|, over parts of the rows (n_maxima may be 0)
+    int n_maxima;
+    int row_box;                                   // rows of the boxes that x is loaded in
     float* dx_acc;                                 // dx over the earlier pieces, fp32
     bool dx_add, dx_done;                          // there are earlier pieces; this is the last one
     void* dx;
@@ -55,11 +58,13 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16);
 cudaError_t run_forward(const Problem& p, const FwdPlan& plan, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st);
 
 struct BwdPlan {
+    bool few_rows;                                 // not on the tensor cores: one pass over w
     bool pack, wide;                               // wide: products of several planes
     int planes, depth, g_planes;
     int blocks;                                    // blocks of 256 columns of a products' tile
     int cols, ldg;                                 // columns of a piece; row length of g
     size_t x, w, g, dx_acc, partials, scale, total;
+    int maxima;                                    // blocks that look for the largest |dloss|; 0: not apart
 };
 BwdPlan plan_backward(int N, int D, int V, bool bf16);
 cudaError_t run_backward(const Problem& p, const BwdPlan& plan, char* ws, bool bf16, const float* lse, const float* dloss,

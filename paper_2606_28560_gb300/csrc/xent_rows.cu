@@ -1,5 +1,5 @@
-// xent_rows.cu -- the cross entropy's forward for few rows (a decoding step's
-// tokens), and the join of per-row statistics.
+// xent_rows.cu -- the cross entropy for few rows (a decoding step's tokens), and
+// the join of per-row statistics.
 //
 // With few rows the work is one pass over w, so this kernel is built as a
 // stream: every warp takes a run of consecutive rows of w, four at a time, a
@@ -36,11 +36,38 @@ template <int K> __device__ __forceinline__ float sum_to_owner(float* s, int lan
     }
     float r = s[0];
 #pragma unroll
-    for (int o = 16 / K; o > 0; o /= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
+    for (int o = 1; o < 32 / K; o *= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
     return r;
 }
 
-// VECTORS: rows start on 16-byte boundaries.
+// Eight values at p, of which `n` are there (zeros, or no write, past them).
+// VECTORS: rows start on 16-byte boundaries and n is 0 or less, or 8 or more.
+template <typename T, bool VECTORS> __device__ __forceinline__ void load8(const T* p, int n, float* x) {
+    if (VECTORS && n > 0) {
+        Vec8<T>::load(p, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = !VECTORS && j < n ? to_f(p[j]) : 0.f;
+}
+__device__ __forceinline__ void put(float* p, float x) { *p = x; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16(x); }
+template <typename T, bool VECTORS> __device__ __forceinline__ void store8(T* p, int n, const float* x) {
+    if (VECTORS) {
+        if (n > 0) Vec8<T>::store(p, x);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < n) put(p + j, x[j]);
+}
+__device__ __forceinline__ float dot8(const float* a, const float4& q0, const float4& q1, float s) {
+    s = fmaf(a[0], q0.x, s); s = fmaf(a[1], q0.y, s); s = fmaf(a[2], q0.z, s); s = fmaf(a[3], q0.w, s);
+    s = fmaf(a[4], q1.x, s); s = fmaf(a[5], q1.y, s); s = fmaf(a[6], q1.z, s); return fmaf(a[7], q1.w, s);
+}
+// Value j of thread t in an array of eight for each of 256 threads.
+__device__ __forceinline__ float& red_at(float* s, int t, int j) { return s[j * 32 * kWarps + t]; }
+
 template <typename T, int NT, bool VECTORS>
 __global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts parts, int segments) {
     extern __shared__ float xs[];                  // [NT][steps * 256]
@@ -74,29 +101,13 @@ __global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts p
                 const int k = st * 256 + lane * 8;
                 float a[kGroup][8];
 #pragma unroll
-                for (int r = 0; r < kGroup; ++r) {
-                    if (k < p.D && v0 + r < hi) {
-                        Vec8<T>::load(w + (size_t)(v0 + r) * p.D + k, a[r]);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) a[r][j] = 0.f;
-                    }
-                }
+                for (int r = 0; r < kGroup; ++r) load8<T, true>(w + (size_t)(v0 + r) * p.D + k, v0 + r < hi ? p.D - k : 0, a[r]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float* q = xs + (n * steps + st) * 256 + lane * 4;
                     const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
 #pragma unroll
-                    for (int r = 0; r < kGroup; ++r) {
-                        s[n * kGroup + r] = fmaf(a[r][0], q0.x, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][1], q0.y, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][2], q0.z, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][3], q0.w, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][4], q1.x, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][5], q1.y, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][6], q1.z, s[n * kGroup + r]);
-                        s[n * kGroup + r] = fmaf(a[r][7], q1.w, s[n * kGroup + r]);
-                    }
+                    for (int r = 0; r < kGroup; ++r) s[n * kGroup + r] = dot8(a[r], q0, q1, s[n * kGroup + r]);
                 }
             }
         } else {
@@ -150,6 +161,124 @@ __device__ __forceinline__ void finish_row(const Problem& p, const FwdParts& par
     const int t = target_column(p, n);
     if (t == kBad) raise_status(p.status, kStatusTarget);
     loss[n] = t == kIgnored ? 0.f : t == kBad ? NAN : z - parts.target_logit[n];
+}
+
+// The gradient of few rows in one pass over w: a block forms the logits of a
+// batch of 32 rows of w as rows_kernel does, turns them into g in shared memory,
+// and then takes the batch again (from L1) with a thread for eight columns:
+//   dw[v] = sum_n g[n][v] x[n]   to memory,   dx[n] += g[n][v] w[v]   in registers.
+// parts[block][n][D]: dx over the block's rows of w.
+template <typename T, int NT, bool VECTORS>
+__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, T* dw, float* parts) {
+    extern __shared__ float xs[];                  // [NT][steps * 256], staged
+    constexpr int kValues = NT * kGroup, kBatch = kGroup * kWarps;
+    __shared__ float gs[kBatch][NT];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, steps = (p.D + 255) / 256;
+    grid_dependency_sync();
+    for (int i = threadIdx.x; i < NT * steps * 256; i += 32 * kWarps) {
+        const int n = i / (steps * 256), k = i % (steps * 256);
+        xs[n * steps * 256 + staged(k)] = n < p.N && k < p.D ? to_f(static_cast<const T*>(p.x)[(size_t)n * p.D + k]) : 0.f;
+    }
+    const int own = lane / (32 / kValues), own_n = own / kGroup, own_r = own % kGroup;
+    const bool writes = lane % (32 / kValues) == 0;
+    const int target = own_n < p.N ? target_column(p, own_n) : kIgnored;
+    const float z = target >= 0 ? lse[own_n] : 0.f, dl = target >= 0 ? dloss[own_n] : 0.f;
+    if (target == kBad && blockIdx.x == 0 && writes && own_r == 0) raise_status(p.status, kStatusTarget);
+    // columns 8 cg .. of the rows rg, rg + groups, ... of a batch
+    const int column_groups = (p.D + 7) / 8, groups = 32 * kWarps / column_groups;
+    const int cg = threadIdx.x % column_groups, rg = threadIdx.x / column_groups;
+    const bool takes = rg < groups;
+    const int at = (cg >> 5) * 256 + (cg & 31) * 4;           // staged(8 cg)
+    float dx[NT][8];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dx[n][j] = 0.f;
+    const int lo = (int)((long long)p.V * blockIdx.x / gridDim.x), hi = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
+    const T* w = static_cast<const T*>(p.w);
+    for (int b0 = lo; b0 < hi; b0 += kBatch) {
+        __syncthreads();                           // x is staged; the batch before has been read
+        const int v0 = b0 + warp * kGroup;
+        float s[kValues];
+#pragma unroll
+        for (int i = 0; i < kValues; ++i) s[i] = 0.f;
+        if (v0 < hi) {
+#pragma unroll 2
+            for (int st = 0; st < steps; ++st) {
+                const int k = st * 256 + lane * 8;
+                float a[kGroup][8];
+#pragma unroll
+                for (int r = 0; r < kGroup; ++r) load8<T, VECTORS>(w + (size_t)(v0 + r) * p.D + k, v0 + r < hi ? p.D - k : 0, a[r]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float* q = xs + (n * steps + st) * 256 + lane * 4;
+                    const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
+#pragma unroll
+                    for (int r = 0; r < kGroup; ++r) s[n * kGroup + r] = dot8(a[r], q0, q1, s[n * kGroup + r]);
+                }
+            }
+        }
+        const float mine = sum_to_owner<kValues>(s, lane);
+        if (writes) gs[warp * kGroup + own_r][own_n] = target < 0 ? 0.f : dl * (expf(mine - z) - (v0 + own_r == target ? 1.f : 0.f));
+        __syncthreads();
+        const int rows = min(kBatch, hi - b0);
+        if (takes) {
+            for (int r = rg; r < rows; r += groups) {
+                float a[8], o[8];
+                load8<T, VECTORS>(w + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, a);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = 0.f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float g = gs[r][n];
+                    const float* q = xs + n * steps * 256 + at;
+                    const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
+                    o[0] = fmaf(g, q0.x, o[0]); o[1] = fmaf(g, q0.y, o[1]); o[2] = fmaf(g, q0.z, o[2]); o[3] = fmaf(g, q0.w, o[3]);
+                    o[4] = fmaf(g, q1.x, o[4]); o[5] = fmaf(g, q1.y, o[5]); o[6] = fmaf(g, q1.z, o[6]); o[7] = fmaf(g, q1.w, o[7]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) dx[n][j] = fmaf(g, a[j], dx[n][j]);
+                }
+                store8<T, VECTORS>(dw + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, o);
+            }
+        }
+    }
+    // the groups' sums of a column, one row of x at a time, over the space of x
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        __syncthreads();
+        if (takes)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) red_at(xs, rg * column_groups + cg, j) = dx[n][j];
+        __syncthreads();
+        for (int o = threadIdx.x; n < p.N && o < 8 * column_groups; o += 32 * kWarps) {
+            const int c = o % column_groups, j = o / column_groups;
+            float sum = 0.f;
+            for (int i = 0; i < groups; ++i) sum += red_at(xs, i * column_groups + c, j);
+            if (8 * c + j < p.D) parts[((size_t)blockIdx.x * p.N + n) * p.D + 8 * c + j] = sum;
+        }
+    }
+}
+
+// dx[n][c] = sum over the blocks of parts[block][n][c]: 32 columns to a block of
+// 256 threads, every eighth part to a thread.
+template <typename T> __global__ void __launch_bounds__(256) join_dx_kernel(const float* parts, int blocks, long long values, T* dx) {
+    __shared__ float red[8][32];
+    grid_dependency_sync();
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const long long i = blockIdx.x * 32ll + lane;
+    float s = 0.f;
+    if (i < values) {
+#pragma unroll 8
+        for (int b = part; b < blocks; b += 8) s += parts[b * values + i];
+    }
+    red[part][lane] = s;
+    __syncthreads();
+    if (part == 0 && i < values) {
+        s = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += red[k][lane];
+        store8<T, false>(dx + i, 1, &s);
+    }
 }
 
 // Many rows: eight threads each, every eighth segment of [segment][row]; a
@@ -227,11 +356,15 @@ template <typename T, int NT> cudaError_t launch_rows(const Problem& p, const Fw
 }
 
 // Rows of x that a block takes: as many as there are, up to eight, and as fit
-// 47 KB of shared memory (w is read again, from L2, for each further group).
+// 47 KB of shared memory (the forward reads w again, from L2, for each further group).
+int rows_at_once(int N, int D) {
+    int nt = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
+    while (nt > 1 && nt * ((D + 255) / 256) > 47) nt /= 2;
+    return nt;
+}
+
 template <typename T> cudaError_t rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
-    int nt = p.N <= 1 ? 1 : p.N <= 2 ? 2 : p.N <= 4 ? 4 : 8;
-    while (nt > 1 && nt * ((p.D + 255) / 256) > 47) nt /= 2;
-    switch (nt) {
+    switch (rows_at_once(p.N, p.D)) {
     case 1: return launch_rows<T, 1>(p, parts, segments, st);
     case 2: return launch_rows<T, 2>(p, parts, segments, st);
     case 4: return launch_rows<T, 4>(p, parts, segments, st);
@@ -239,14 +372,55 @@ template <typename T> cudaError_t rows(const Problem& p, const FwdParts& parts, 
     }
 }
 
+template <typename T, int NT>
+cudaError_t launch_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dw, float* parts, int blocks,
+                                 cudaStream_t st) {
+    // x, and later eight values of each of the block's threads
+    const size_t smem = std::max((size_t)NT * ((p.D + 255) / 256) * 256 * 4, (size_t)32 * kWarps * 8 * 4);
+    if (p.D % 8 == 0)
+        return launch_kernel(rows_gradient_kernel<T, NT, true>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
+                             static_cast<T*>(dw), parts);
+    return launch_kernel(rows_gradient_kernel<T, NT, false>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
+                         static_cast<T*>(dw), parts);
+}
+template <typename T>
+cudaError_t rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts, int blocks,
+                          cudaStream_t st) {
+    cudaError_t e;
+    {
+        ProfScope s("xent_few_rows_grad", st);
+        switch (rows_at_once(p.N, p.D)) {
+        case 1: e = launch_rows_gradient<T, 1>(p, lse, dloss, dw, parts, blocks, st); break;
+        case 2: e = launch_rows_gradient<T, 2>(p, lse, dloss, dw, parts, blocks, st); break;
+        case 4: e = launch_rows_gradient<T, 4>(p, lse, dloss, dw, parts, blocks, st); break;
+        default: e = launch_rows_gradient<T, 8>(p, lse, dloss, dw, parts, blocks, st);
+        }
+    }
+    if (e != cudaSuccess) return e;
+    ProfScope s("xent_join_dx", st);
+    const long long values = (long long)p.N * p.D;
+    return launch_kernel(join_dx_kernel<T>, dim3((unsigned)((values + 31) / 32)), dim3(256), 0, st, parts, blocks, values,
+                         static_cast<T*>(dx));
+}
+
 }  // namespace
 
-int few_rows_segments(int N, int V) {
+int few_rows_segments(int V) {
     return std::max(1, std::min(152 * 4, (V + kGroup * kWarps - 1) / (kGroup * kWarps)));
 }
 
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st) {
     return bf16 ? rows<__nv_bfloat16>(p, parts, segments, st) : rows<float>(p, parts, segments, st);
+}
+
+int few_rows_at_most(int N, int D) { return D <= 2048 ? rows_at_once(N, D) : 0; }
+
+int few_rows_blocks(int V) { return std::max(1, std::min(152 * 2, (V + kGroup * kWarps - 1) / (kGroup * kWarps))); }
+
+cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts,
+                                     int blocks, bool bf16, cudaStream_t st) {
+    return bf16 ? rows_gradient<__nv_bfloat16>(p, lse, dloss, dx, dw, parts, blocks, st)
+                : rows_gradient<float>(p, lse, dloss, dx, dw, parts, blocks, st);
 }
 
 cudaError_t launch_join_segments(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st) {
