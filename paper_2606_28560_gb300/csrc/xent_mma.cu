@@ -36,11 +36,15 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 enum Mode { kForward, kGradient, kProducts };
 
-template <int MODE, int NB> struct Config {
-    static constexpr unsigned kStageBytes = kOperandBytes * (1 + NB);
-    static constexpr int kStages = NB == 2 ? 4 : MODE == kGradient ? 6 : 7;
+// RESIDENT: the tile's rows of A stay in shared memory for a unit of tiles (up
+// to kResidentChunks chunks of depth), and only B goes through the stages.
+constexpr int kResidentChunks = 8;
+template <int MODE, int NB, bool RESIDENT> struct Config {
+    static constexpr unsigned kResidentBytes = RESIDENT ? kResidentChunks * kOperandBytes : 0;
+    static constexpr unsigned kStageBytes = kOperandBytes * ((RESIDENT ? 0 : 1) + NB);
+    static constexpr int kStages = RESIDENT ? (MODE == kGradient ? 4 : 6) : NB == 2 ? 4 : MODE == kGradient ? 6 : 7;
     static constexpr unsigned kStoreBytes = MODE == kGradient ? kEpilogueWarps * 4096 : 0;   // a 32 x 64 box a warp
-    static constexpr unsigned kSmem = kStages * kStageBytes + kStoreBytes + 1024;
+    static constexpr unsigned kSmem = kResidentBytes + kStages * kStageBytes + kStoreBytes + 1024;
 };
 
 // One tile (or a part of its depth): rows from m0, columns from n0, depth in
@@ -224,17 +228,19 @@ __device__ __forceinline__ float find_scale(const Args& a, float* red, int t) {
     return m > 0.f && m < INFINITY ? m : 1.f;
 }
 
-template <int MODE, int NB, bool WIDE>
+template <int MODE, int NB, bool WIDE, bool RESIDENT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
-    using C = Config<MODE, NB>;
+    using C = Config<MODE, NB, RESIDENT>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ unsigned long long bars[2 * C::kStages + 4];
+    __shared__ unsigned long long bars[2 * C::kStages + 4 + (RESIDENT ? 2 * kResidentChunks : 0)];
     __shared__ unsigned tmem_base_s;
     __shared__ float red_s[MODE == kGradient ? kEpilogueWarps : 1];
     const unsigned smem0 = (tc5::smem_u32(smem_raw) + 1023u) & ~1023u;
     const unsigned full = tc5::smem_u32(bars), empty = full + 8 * C::kStages;
     const unsigned acc_full = empty + 8 * C::kStages, acc_empty = acc_full + 16;
+    const unsigned a_full = acc_empty + 16, a_empty = a_full + 8 * kResidentChunks;   // (resident chunks of A)
+    const unsigned stages0 = smem0 + C::kResidentBytes;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned rank = tc5::cluster_rank();
     const int cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
@@ -243,6 +249,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         for (int s = 0; s < C::kStages; ++s) {
             tc5::init_barrier(full + 8 * s, 1);
             tc5::init_barrier(empty + 8 * s, 1);
+        }
+        for (int k = 0; RESIDENT && k < kResidentChunks; ++k) {
+            tc5::init_barrier(a_full + 8 * k, 1);
+            tc5::init_barrier(a_empty + 8 * k, 1);
         }
         for (int b = 0; b < 2; ++b) {
             tc5::init_barrier(acc_full + 8 * b, 1);
@@ -277,8 +287,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
             const unsigned long long keep = tc5::policy_keep(), pass = WIDE ? tc5::policy_normal() : tc5::policy_pass();
             Walk<MODE> walk(a, cluster, clusters);
             Item it;
+            const unsigned a_full0 = tc5::map_to(a_full, 0);
             int stage = 0;
-            unsigned phase = 0;
+            unsigned phase = 0, unit = 0;
+            int a_upto = 0;                                // chunks of the current unit's rows that are issued
             long long issued = 0;
             bool ok = true;
             while (ok && walk.next(it)) {
@@ -287,8 +299,9 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 // looks at, and boxes that lie outside their tensor are slow to fill.
                 const bool a_here = it.problem == 1 || it.m0 + 128 * (int)rank < a.p.N;
                 const bool b_here = MODE == kProducts || a.v0 + it.n0 + 128 * (int)rank < a.p.V;
-                unsigned bytes = MODE == kProducts && it.problem == 1 ? 2 * kOperandBytes
-                                                                      : a.row_box * 128u * (it.m0 + 128 < a.p.N ? 2 : 1);
+                const unsigned a_bytes = MODE == kProducts && it.problem == 1 ? 2 * kOperandBytes
+                                                                              : a.row_box * 128u * (it.m0 + 128 < a.p.N ? 2 : 1);
+                unsigned bytes = RESIDENT ? 0 : a_bytes;
                 if (MODE != kProducts) {
                     bytes += kOperandBytes * (a.v0 + it.n0 + 128 < a.p.V ? 2 : 1);
                 } else {
@@ -301,13 +314,23 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         const int chunk = r0 + (WIDE ? i % len : i);
                         const int pa = WIDE ? (a.combo_a >> (4 * (i / len))) & 15 : 0;
                         const int pb = WIDE ? (a.combo_b >> (4 * (i / len))) & 15 : 0;
+                        if (RESIDENT && it.first) {        // the unit's rows, as the last unit's are done with
+                            a_upto = chunk;
+                            ok = tc5::wait_parity(a_empty + 8 * chunk, (unit & 1u) ^ 1u);
+                            if (!ok) break;
+                            if (rank == 0) tc5::expect_bytes(a_full + 8 * chunk, a_bytes);
+                            if (a_here)
+                                tc5::load_box(smem0 + chunk * kOperandBytes, &maps.m[0], chunk * 64, it.m0 + 128 * rank, 0,
+                                              a_full0 + 8 * chunk, keep);
+                            a_upto = chunk + 1;
+                        }
                         ok = tc5::wait_parity(empty + 8 * stage, phase ^ 1u);
                         if (!ok) break;
                         if (rank == 0) tc5::expect_bytes(full + 8 * stage, bytes);
-                        const unsigned bar = full0 + 8 * stage, dst = smem0 + stage * C::kStageBytes;
+                        const unsigned bar = full0 + 8 * stage, dst = stages0 + stage * C::kStageBytes;
                         if (MODE != kProducts) {
-                            if (a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
-                            if (b_here) tc5::load_box(dst + kOperandBytes, &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
+                            if (!RESIDENT && a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
+                            if (b_here) tc5::load_box(dst + (RESIDENT ? 0 : kOperandBytes), &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
                         } else {
                             if (it.problem == 0) {
                                 if (a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, pass);
@@ -327,11 +350,18 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
                     }
                 }
+                if (RESIDENT && it.last) {
+                    ++unit;
+                    a_upto = 0;
+                }
             }
             if (!ok) {
                 // Copies may still be under way into this pair's shared memory: wait
                 // for the stages issued last (bounded as every wait is).
                 raise_status(a.p.status, kStatusWaitTimeout);
+                if (RESIDENT && rank == 0)
+                    for (int k = 0; k < a.chunks; ++k)
+                        if (k < a_upto || unit > 0) tc5::wait_parity(a_full + 8 * k, k < a_upto ? unit & 1u : (unit - 1) & 1u);
                 if (rank == 0)
                     for (int s = 0; s < C::kStages && s < issued; ++s) {
                         const int st = (stage + C::kStages - 1 - s) % C::kStages;
@@ -343,7 +373,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
             Walk<MODE> walk(a, cluster, clusters);
             Item it;
             int stage = 0;
-            unsigned phase = 0, run = 0;
+            unsigned phase = 0, run = 0, unit = 0;
             bool ok = true;
             while (ok && walk.next(it)) {
                 const bool a_rows = MODE == kProducts && it.problem == 1, b_rows = MODE == kProducts;
@@ -364,15 +394,19 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     if (!ok) break;
                     tc5::fence_after();
                     for (int i = 0; i < combos * len; ++i) {
+                        if (RESIDENT && it.first) {
+                            ok = tc5::wait_parity(a_full + 8 * i, unit & 1u);
+                            if (!ok) break;
+                        }
                         ok = tc5::wait_parity(full + 8 * stage, phase);
                         if (!ok) break;
                         tc5::fence_after();
                         const int left = depth - 64 * (r0 + (WIDE ? i % len : i));   // what is past the depth is zeros
-                        const unsigned src = smem0 + stage * C::kStageBytes;
-                        const unsigned long long da = tc5::descriptor(src, a_rows ? 8192u : 16u);
+                        const unsigned src = stages0 + stage * C::kStageBytes;
+                        const unsigned long long da = tc5::descriptor(RESIDENT ? smem0 + i * kOperandBytes : src, a_rows ? 8192u : 16u);
 #pragma unroll
                         for (int b = 0; b < NB; ++b) {
-                            const unsigned long long db = tc5::descriptor(src + kOperandBytes * (1 + b), b_rows ? 8192u : 16u);
+                            const unsigned long long db = tc5::descriptor(src + kOperandBytes * ((RESIDENT ? 0 : 1) + b), b_rows ? 8192u : 16u);
                             if (cols[b] > 0) {
 #pragma unroll
                                 for (unsigned k = 0; k < 4; ++k)
@@ -381,12 +415,14 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                             }
                         }
                         tc5::commit_pair(empty + 8 * stage);
+                        if (RESIDENT && it.last) tc5::commit_pair(a_empty + 8 * i);
                         if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) break;
 #pragma unroll
                     for (int b = 0; b < NB; ++b) tc5::commit_pair(acc_full + 8 * (buf + b));
                 }
+                if (RESIDENT && it.last) ++unit;
             }
             if (!ok) raise_status(a.p.status, kStatusWaitTimeout);
         }
@@ -397,7 +433,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         const int lane_row = (warp & 3) * 32 + lane;
         const unsigned t_lane = tmem + ((unsigned)(warp & 3) << 21) + 128u * half;
         const unsigned acc_empty0 = tc5::map_to(acc_empty, 0);
-        const unsigned stage_out = smem0 + C::kStages * C::kStageBytes + ew * 4096u;
+        const unsigned stage_out = stages0 + C::kStages * C::kStageBytes + ew * 4096u;
         Walk<MODE> walk(a, cluster, clusters);
         Item it;
         unsigned run = 0;
@@ -703,8 +739,8 @@ bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int NB, bool WIDE> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
-    auto kern = xent_kernel<MODE, NB, WIDE>;
+template <int MODE, int NB, bool WIDE, bool RESIDENT> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
+    auto kern = xent_kernel<MODE, NB, WIDE, RESIDENT>;
     // The register split of the two halves of a block draws on what the block
     // was launched with: refuse to launch a build that was given less.
     static const int registers = [&] {
@@ -712,7 +748,7 @@ template <int MODE, int NB, bool WIDE> cudaError_t launch(const Args& a, const M
         return cudaFuncGetAttributes(&at, kern) == cudaSuccess ? at.numRegs : 0;
     }();
     if (registers * kThreads < 56 * 128 + 224 * 256) return cudaErrorInvalidDeviceFunction;
-    constexpr unsigned smem = Config<MODE, NB>::kSmem;
+    constexpr unsigned smem = Config<MODE, NB, RESIDENT>::kSmem;
     static std::atomic<unsigned long long> set{0};          // devices (of the first 64) where the limit is raised already
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -730,6 +766,14 @@ int row_box_of(int N) { return std::min(128, (N + 7) / 8 * 8); }
 
 int tiles256(long long n) { return (int)((n + 255) / 256); }
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Whether the rows of a tile stay in shared memory over the tiles of a unit,
+// which halves what the forward and the gradient pass load.  16384 rows, 512 wide,
+// 32768 columns: the forward 273 -> 261 us; the gradient pass, whose stages then
+// are four instead of six, 340 -> 365 us by itself, but the card runs at its power
+// limit after some tens of milliseconds and then the step takes 1440 -> 1409 us
+// with both, 1420 us with the forward alone.
+bool resident(const Args& a) { return a.chunks <= kResidentChunks && a.unit_tiles > 1; }
 
 // Whether the operands are packed, into how many planes and rows of what
 // length.  bf16 rows are taken where they lie if TMA can address them (16-byte
@@ -853,7 +897,9 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     {
         ProfScope s("xent_fwd", st);
         set_combos(&a, f.planes, f.planes);
-        e = bf16 ? launch<kForward, 1, false>(a, maps, clusters, st) : launch<kForward, 1, true>(a, maps, clusters, st);
+        e = !bf16 ? launch<kForward, 1, true, false>(a, maps, clusters, st)
+            : resident(a) ? launch<kForward, 1, false, true>(a, maps, clusters, st)
+                          : launch<kForward, 1, false, false>(a, maps, clusters, st);
     }
     if (e != cudaSuccess) return e;
     ProfScope s("xent_join", st);
@@ -971,7 +1017,9 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
             ProfScope s("xent_grad", st);
             const int clusters = std::min(kClusters, a.units);
             set_combos(&a, f.planes, f.planes);
-            e = f.wide ? launch<kGradient, 1, true>(a, logits, clusters, st) : launch<kGradient, 1, false>(a, logits, clusters, st);
+            e = f.wide ? launch<kGradient, 1, true, false>(a, logits, clusters, st)
+                : resident(a) ? launch<kGradient, 1, false, true>(a, logits, clusters, st)
+                              : launch<kGradient, 1, false, false>(a, logits, clusters, st);
         }
         if (e != cudaSuccess) return e;
         a.prob[0] = Product{p.N, d_tiles, (cols + 63) / 64};
@@ -982,9 +1030,9 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
         {
             ProfScope s("xent_products", st);
             set_combos(&a, f.g_planes, f.planes);
-            e = f.wide ? launch<kProducts, 1, true>(a, products, workers, st)
-                : f.blocks == 2 ? launch<kProducts, 2, false>(a, products, workers, st)
-                          : launch<kProducts, 1, false>(a, products, workers, st);
+            e = f.wide ? launch<kProducts, 1, true, false>(a, products, workers, st)
+                : f.blocks == 2 ? launch<kProducts, 2, false, false>(a, products, workers, st)
+                          : launch<kProducts, 1, false, false>(a, products, workers, st);
         }
         if (e != cudaSuccess) return e;
         SplitTiles splits;
