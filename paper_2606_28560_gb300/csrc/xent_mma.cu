@@ -55,35 +55,53 @@ struct Item {
     int unit;                                      // forward, gradient: segment of the columns
     bool first, last;                              // forward, gradient: tile of its unit
     bool whole;                                    // products: the whole depth
-    int tile_lo, tile_hi;                          // products: the tile's range of the iteration space
+    bool begins;                                   // products: the cluster's range begins in this tile
 };
 
-// Products: start of cluster c's range of the iteration space (all tiles'
-// chunks of depth one after another): equal shares of dx's part for the clusters
-// below first_dw, of dw's for the others.  A boundary within `snap` chunks of a
-// tile's end moves there: a sliver is not worth a tile of partial sums.
-__host__ __device__ inline int range_start(const Args& a, int c, int clusters) {
-    int b;
-    if (c < a.first_dw) b = (int)((long long)a.split * c / a.first_dw);
-    else b = a.split + (int)((long long)(a.total - a.split) * (c - a.first_dw) / (clusters - a.first_dw));
-    if (b <= 0 || b >= a.total) return b <= 0 ? 0 : a.total;
-    const int p = b < a.split ? 0 : 1, kc = a.prob[p].chunks, off = (b - (p ? a.split : 0)) % kc;
-    if (off <= a.snap[p]) return b - off;
-    if (kc - off <= a.snap[p]) return b - off + kc;
+// Products: the range of cluster c.  The clusters below first_dw work on dx, the
+// others on dw.  Of each product, `siblings` neighbouring clusters take the same
+// rows and depth at the same time for different columns, so that what they read
+// of g is read from memory once; a sibling's tiles' chunks, one tile after
+// another, are cut into equal shares for the groups of siblings.  A boundary
+// within `snap` chunks of a tile's end moves there: a sliver is not worth a tile
+// of partial sums.
+struct Range {
+    int problem, sibling, lo, hi;                  // chunks of the sibling's tiles
+};
+__host__ __device__ inline int share_start(const Product& p, int snap, int group, int groups) {
+    const int b = (int)((long long)p.tiles * p.chunks * group / groups), off = b % p.chunks;
+    if (off <= snap) return b - off;
+    if (p.chunks - off <= snap) return b - off + p.chunks;
     return b;
+}
+__host__ __device__ inline Range range_of(const Args& a, int c, int clusters) {
+    Range r;
+    r.problem = c < a.first_dw ? 0 : 1;
+    const Product& p = a.prob[r.problem];
+    const int local = r.problem ? c - a.first_dw : c, groups = (r.problem ? clusters - a.first_dw : a.first_dw) / p.siblings;
+    const int group = local / p.siblings;
+    r.sibling = local % p.siblings;
+    r.lo = share_start(p, a.snap[r.problem], group, groups);
+    r.hi = share_start(p, a.snap[r.problem], group + 1, groups);
+    return r;
+}
+// Tile t of a sibling: its first row and column.
+__host__ __device__ inline int tile_row(const Product& p, int t) { return t / (p.col_tiles / p.siblings) * 256; }
+__host__ __device__ inline int tile_col(const Args& a, const Product& p, int t, int sibling) {
+    return (t % (p.col_tiles / p.siblings) * p.siblings + sibling) * a.tile_cols;
 }
 
 // The items of cluster c, in order.
 template <int MODE> struct Walk {
     const Args& a;
-    int c, clusters, at, sub, end;
-    __device__ Walk(const Args& args, int cluster, int n) : a(args), c(cluster), clusters(n), at(cluster), sub(0), end(0) {
+    int clusters, at, sub;
+    Range range;
+    __device__ Walk(const Args& args, int cluster, int n) : a(args), clusters(n), at(cluster), sub(0) {
         if (MODE == kProducts) {
-            at = bound(c);
-            end = bound(c + 1);
+            range = range_of(a, cluster, n);
+            at = range.lo;
         }
     }
-    __device__ int bound(int cluster) const { return range_start(a, cluster, clusters); }
     __device__ bool next(Item& it) {
         if (MODE != kProducts) {
             if (at >= a.units) return false;
@@ -100,18 +118,17 @@ template <int MODE> struct Walk {
             else ++sub;
             return true;
         } else {
-            if (at >= end) return false;
-            it.problem = at < a.split ? 0 : 1;
+            if (at >= range.hi) return false;
+            it.problem = range.problem;
             const Product& p = a.prob[it.problem];
-            const int base = it.problem ? a.split : 0, t = (at - base) / p.chunks;
-            it.tile_lo = base + t * p.chunks;
-            it.tile_hi = it.tile_lo + p.chunks;
-            const int stop = min(end, it.tile_hi);
-            it.m0 = (t / p.col_tiles) * 256;
-            it.n0 = (t % p.col_tiles) * a.tile_cols;
-            it.k0 = at - it.tile_lo;
-            it.k1 = stop - it.tile_lo;
+            const int t = at / p.chunks, first = t * p.chunks;
+            const int stop = min(range.hi, first + p.chunks);
+            it.m0 = tile_row(p, t);
+            it.n0 = tile_col(a, p, t, range.sibling);
+            it.k0 = at - first;
+            it.k1 = stop - first;
             it.whole = it.k0 == 0 && it.k1 == p.chunks;
+            it.begins = range.lo >= first;
             at = stop;
             return true;
         }
@@ -187,13 +204,10 @@ __device__ __forceinline__ void write_product(const Args& a, int problem, int ro
     else put_row<COUNT>(static_cast<__nv_bfloat16*>(out) + to, acc, n, a.out_cols % 8 == 0);
 }
 
-// Where cluster c keeps its sums over a part of the depth of a tile: one slot
-// for the tile that its range begins in, one for the tile that it ends in.
-template <int NB>
-__device__ __forceinline__ float* slot_of(const Args& a, const Walk<kProducts>& walk, const Item& it, int c, int rank, int b, int ew,
-                                          int lane) {
-    const size_t s = 2 * (size_t)c + (walk.bound(c) >= it.tile_lo ? 0 : 1);
-    return a.partials + (((s * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + lane;
+// Where a cluster keeps its sums over a part of the depth of a tile: slot 2 c for
+// the tile that its range begins in, 2 c + 1 for the one that it ends in.
+template <int NB> __device__ __forceinline__ float* slot_at(const Args& a, int slot, int rank, int b, int ew) {
+    return a.partials + ((((size_t)slot * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096;
 }
 
 __device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
@@ -591,7 +605,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                     if (it.whole) {
                         write_product<WIDE, 128>(a, it.problem, row, c0, end - c0, out_scale, acc);
                     } else {
-                        float* mine = slot_of<NB>(a, walk, it, cluster, (int)rank, b, ew, lane);
+                        float* mine = slot_at<NB>(a, 2 * cluster + (it.begins ? 0 : 1), (int)rank, b, ew) + lane;
                         if (row < a.prob[it.problem].rows) {
 #pragma unroll
                             for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
@@ -697,7 +711,7 @@ __global__ void __launch_bounds__(512) join_products_kernel(const __grid_constan
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
 #pragma unroll 4
     for (int i = 0; i < t.parts; ++i) {
-        const float* p = a.partials + ((((size_t)s.slots[t.first + i] * 2 + rank) * NB + b) * kEpilogueWarps + ew) * 4096 + 32 * j0 + lane;
+        const float* p = slot_at<NB>(a, s.slots[t.first + i], rank, b, ew) + 32 * j0 + lane;
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j] += __ldcg(p + 32 * j);
     }
@@ -707,22 +721,27 @@ __global__ void __launch_bounds__(512) join_products_kernel(const __grid_constan
 // Which tiles the ranges of `clusters` clusters cut, and where their parts are.
 void find_splits(const Args& a, int clusters, SplitTiles* s) {
     s->count = 0;
-    int used = 0, last = -1;
-    for (int c = 1; c < clusters; ++c) {
-        const int at = range_start(a, c, clusters);
-        if (at <= 0 || at >= a.total) continue;
-        const int p = at < a.split ? 0 : 1, kc = a.prob[p].chunks, base = p ? a.split : 0;
-        const int t = (at - base) / kc, lo = base + t * kc;
-        if (at == lo || lo == last) continue;      // a boundary between tiles, or a tile already listed
-        last = lo;
-        SplitTile& tile = s->tile[s->count++];
-        tile = SplitTile{p, t / a.prob[p].col_tiles * 256, t % a.prob[p].col_tiles * a.tile_cols, used, 0};
-        for (int k = c - 1; k < clusters && range_start(a, k, clusters) < lo + kc; ++k) {
-            const int from = range_start(a, k, clusters), to = range_start(a, k + 1, clusters);
-            if (to <= from || to <= lo) continue;
-            s->slots[used++] = (short)(2 * k + (from >= lo ? 0 : 1));
-            ++tile.parts;
+    int used = 0;
+    for (int first = 0; first < clusters; ) {      // the first cluster of a group of siblings
+        const Range r = range_of(a, first, clusters);
+        const Product& p = a.prob[r.problem];
+        const int past = r.problem ? clusters : a.first_dw;
+        const int t = r.hi / p.chunks, lo = t * p.chunks;
+        if (r.lo <= lo && lo < r.hi) {             // the range holds the first part of tile t, not the last
+
+            for (int sib = 0; sib < p.siblings; ++sib) {
+                SplitTile& tile = s->tile[s->count++];
+                tile = SplitTile{r.problem, tile_row(p, t), tile_col(a, p, t, sib), used, 0};
+                for (int c = first + sib; c < past; c += p.siblings) {
+                    const Range part = range_of(a, c, clusters);
+                    if (part.lo >= lo + p.chunks) break;
+                    if (part.hi <= part.lo || part.hi <= lo) continue;
+                    s->slots[used++] = (short)(2 * c + (part.lo >= lo ? 0 : 1));
+                    ++tile.parts;
+                }
+            }
         }
+        first += p.siblings;
     }
 }
 
@@ -909,19 +928,25 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
 // Divides the products' chunks among the clusters and returns how many take
 // part: dx and dw get clusters by their work, with a tile's own cost counted as
 // `tile` chunks, and no part of a tile is below `least` chunks.
-static int share_products(Args* a, int dx_tiles, int dw_tiles, bool wide) {
+static int share_products(Args* a, int dx_rows, int dw_rows, int col_tiles, int dx_chunks, int dw_chunks, bool wide) {
     const int tile = wide ? 3 : 8, least = wide ? 4 : 12;
-    const int dx_chunks = a->prob[0].chunks, dw_chunks = a->prob[1].chunks;
-    const int dx = dx_tiles * dx_chunks, dw = dw_tiles * dw_chunks;
-    a->split = dx;
-    a->total = dx + dw;
-    const double cost_dx = dx + (double)tile * dx_tiles, cost_dw = dw + (double)tile * dw_tiles;
-    const int fair = std::max(1, std::min(kClusters - 1, (int)(kClusters * cost_dx / (cost_dx + cost_dw) + 0.5)));
-    a->first_dw = (int)std::min<long long>(fair, (long long)dx_tiles * std::max(1, dx_chunks / least));
-    const int for_dw = (int)std::min<long long>(kClusters - a->first_dw, (long long)dw_tiles * std::max(1, dw_chunks / least));
-    a->snap[0] = std::min(wide ? 4 : 16, dx / a->first_dw / 4);
-    a->snap[1] = std::min(wide ? 4 : 16, dw / for_dw / 4);
-    return a->first_dw + for_dw;
+    const double cost_dx = (double)dx_rows * (dx_chunks + tile), cost_dw = (double)dw_rows * (dw_chunks + tile);
+    int clusters[2];
+    clusters[0] = std::max(1, std::min(kClusters - 1, (int)(kClusters * cost_dx / (cost_dx + cost_dw) + 0.5)));
+    clusters[1] = kClusters - clusters[0];
+    for (int p = 0; p < 2; ++p) {
+        const int rows = p ? dw_rows : dx_rows, chunks = p ? dw_chunks : dx_chunks;
+        const int by_two = col_tiles % 2 == 0 ? 2 : col_tiles % 3 == 0 ? 3 : 1;
+        const int siblings = clusters[p] >= by_two ? by_two : 1;
+        const int tiles = rows * (col_tiles / siblings);
+        int groups = clusters[p] / siblings;
+        groups = (int)std::min<long long>(groups, (long long)tiles * std::max(1, chunks / least));
+        a->prob[p] = Product{p ? a->cols : a->p.N, col_tiles, chunks, tiles, siblings};
+        a->snap[p] = (int)std::min<long long>(wide ? 4 : 16, (long long)tiles * chunks / groups / 4);
+        clusters[p] = groups * siblings;
+    }
+    a->first_dw = clusters[0];
+    return clusters[0] + clusters[1];
 }
 
 // g of a piece is held in memory for the two products: at most 512 MiB of it
@@ -1022,9 +1047,7 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
                               : launch<kGradient, 1, false, false>(a, logits, clusters, st);
         }
         if (e != cudaSuccess) return e;
-        a.prob[0] = Product{p.N, d_tiles, (cols + 63) / 64};
-        a.prob[1] = Product{cols, d_tiles, (p.N + 63) / 64};
-        const int workers = share_products(&a, tiles256(p.N) * d_tiles, tiles256(cols) * d_tiles, f.wide);
+        const int workers = share_products(&a, tiles256(p.N), tiles256(cols), d_tiles, (cols + 63) / 64, (p.N + 63) / 64, f.wide);
         a.dx_add = v0 > 0;
         a.dx_done = v0 + cols >= p.V;
         {

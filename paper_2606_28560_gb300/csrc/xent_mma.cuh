@@ -9,9 +9,10 @@ namespace xent {
 
 constexpr int kClusters = 76;                      // CTA pairs of a GB300 (152 SMs)
 
-// One product of the backward: rows x (the tile's) columns, depth in chunks of 64.
+// One product of the backward: rows x (tiles of) columns, depth in chunks of 64;
+// `siblings` clusters at a time share the column tiles, each has `tiles` tiles.
 struct Product {
-    int rows, col_tiles, chunks;
+    int rows, col_tiles, chunks, tiles, siblings;
 };
 
 struct Args {
@@ -23,10 +24,8 @@ struct Args {
     const float* lse;
     const float* dloss;
     int v0, cols;                                  // the piece of the vocabulary
-    // products: the chunks of all tiles of prob[0] (dx), then of prob[1] (dw),
-    // one after another, make `total`; prob[1] starts at `split`, its clusters at first_dw
-    Product prob[2];
-    int split, total, first_dw, snap[2];
+    Product prob[2];                               // products: dx, dw
+    int first_dw, snap[2];                         // the first cluster of dw's
     int tile_cols, out_cols;                       // columns of a tile, of the results (D)
     float* partials;                               // sums over a part of a tile's depth
     float* scale;                                  // g is divided by it, the products multiplied
