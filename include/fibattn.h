@@ -289,7 +289,11 @@ int fibattn_fwd_noalloc(const void* q, const void* k, const void* v, void* out, 
  * loss is NaN, it adds nothing to the gradients, and status bit 2 is set
  * (fibattn_check_status).  Limits: 0 <= N <= 2^24, 1 <= D <= 8192,
  * 1 <= V <= 2^24.  N == 0 launches nothing but the zeroing of dw.
- * Every product is accumulated in fp32; results do not depend on timing.
+ * Every product is accumulated in fp32; results do not depend on timing.  fp32
+ * operands keep their 24 bits (on the tensor cores as sums of three bf16 values);
+ * with bf16 I/O g is rounded to bf16 between the two products of the gradient
+ * (relative to the largest |dloss|, so that equal weights round nothing), as a
+ * bf16 tensor between two library calls would be.
  * As in any matrix product, an ignored row of x that holds an infinity or NaN
  * still reaches dw as 0 * NaN.
  * ------------------------------------------------------------------------- */
@@ -305,8 +309,9 @@ int fibattn_linear_xent_fwd(const void* x, const void* w, const long long* targe
  *   g[n][v] = dloss[n] (exp(s[n][v] - lse[n]) - [v == targets[n]]), 0 for ignored rows;
  *   dx = g w [N][D],  dw = g^T x [V][D], in `dtype`, overwritten.
  * The logits are formed again, a piece of the vocabulary at a time; g of one
- * piece is held in the workspace (bf16 for bf16 I/O).  dx and dw may not alias
- * each other, an input or the workspace. */
+ * piece is held in the workspace (at most 512 MiB of it).  dx or dw may be NULL
+ * when only the other is wanted (a frozen head; a probe on frozen states).  They
+ * may not alias each other, an input or the workspace. */
 size_t fibattn_linear_xent_bwd_workspace_bytes(int N, int D, int V, int dtype);
 
 int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targets,
@@ -327,8 +332,8 @@ int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targe
  * clipping).  norm: device, 1 float.  A norm that is not finite passes into
  * the outputs by the formula above (NaN, or 0 with NaN where the infinities
  * were); the caller that wants to skip such a step looks at norm.  Squares
- * are summed in fp32 within a run of at most 256 values of one thread and in
- * fp64 beyond; the result does not depend on timing. */
+ * are summed in fp32 in runs of at most 128 values and in fp64 beyond; the
+ * result does not depend on timing. */
 size_t fibattn_clip_grads_workspace_bytes(int n);
 
 int fibattn_clip_grads(int n, const void* const* grads, void* const* outs,

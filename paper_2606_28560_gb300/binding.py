@@ -424,23 +424,27 @@ def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=N
     return loss, lse
 
 
-def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=None, dw=None, workspace=None,
-                    stream=None):
+def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=None, dw=None, want_dx: bool = True,
+                    want_dw: bool = True, workspace=None, stream=None):
     """Gradients of ``sum(dloss * loss)`` by x and w (fibattn_linear_xent_bwd).
     lse [N] from ``linear_xent_fwd`` of the same inputs; dloss [N] fp32.
-    Returns (dx [N, D], dw [V, D]) in x's dtype."""
+    Returns (dx [N, D], dw [V, D]) in x's dtype; without ``want_dx`` or
+    ``want_dw`` that product is not computed and None is returned for it."""
     N, D, V, code, index = _check_xent(x, w, targets)
     _f32_row(lse, N, index, "lse")
     _f32_row(dloss, N, index, "dloss")
-    dx = torch.empty_like(x) if dx is None else _grad_like(dx, x)
-    dw = torch.empty_like(w) if dw is None else _grad_like(dw, w)
+    if not (want_dx or want_dw):
+        raise ValueError("neither dx nor dw is wanted")
+    dx = None if not want_dx else torch.empty_like(x) if dx is None else _grad_like(dx, x)
+    dw = None if not want_dw else torch.empty_like(w) if dw is None else _grad_like(dw, w)
     L = lib()
     if workspace is None:
         need = L.fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
         workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
     _check(L.fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
-                                     dx.data_ptr(), dw.data_ptr(), N, D, V, ignore_index, code, workspace.data_ptr(),
-                                     workspace.numel(), _stream_of(stream, index)))
+                                     dx.data_ptr() if want_dx else None, dw.data_ptr() if want_dw else None, N, D, V,
+                                     ignore_index, code, workspace.data_ptr(), workspace.numel(),
+                                     _stream_of(stream, index)))
     return dx, dw
 
 

@@ -66,7 +66,7 @@ int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targe
                             void* workspace, size_t workspace_bytes, void* stream) {
     int rc = check_sizes(N, D, V, dtype);
     if (rc) return rc;
-    if (!dw || (N > 0 && (!x || !w || !targets || !lse || !dloss || !dx || !workspace)))
+    if (N > 0 && ((!dx && !dw) || !x || !w || !targets || !lse || !dloss || !workspace))
         return set_error(FIBATTN_ERR_INVALID_ARG, "NULL tensor or workspace pointer");
     if (misaligned16(x) || misaligned16(w) || misaligned16(lse) || misaligned16(dloss) || misaligned16(dx) ||
         misaligned16(dw) || misaligned16(workspace) || ((uintptr_t)targets & 7u))
@@ -81,7 +81,7 @@ int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targe
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (N == 0) {                                // no rows: the head's gradient is zero
-        e = cudaMemsetAsync(dw, 0, (size_t)V * D * (bf16 ? 2 : 4), st);
+        e = dw ? cudaMemsetAsync(dw, 0, (size_t)V * D * (bf16 ? 2 : 4), st) : cudaSuccess;
         return e == cudaSuccess ? FIBATTN_OK : launch_failed(e, "zero gradients of an empty batch");
     }
     e = xent::run_backward(p, plan, static_cast<char*>(workspace), bf16, lse, dloss, dx, dw, st);

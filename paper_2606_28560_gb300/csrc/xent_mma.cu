@@ -933,8 +933,11 @@ static int share_products(Args* a, int dx_rows, int dw_rows, int col_tiles, int 
     const double cost_dx = (double)dx_rows * (dx_chunks + tile), cost_dw = (double)dw_rows * (dw_chunks + tile);
     int clusters[2];
     clusters[0] = std::max(1, std::min(kClusters - 1, (int)(kClusters * cost_dx / (cost_dx + cost_dw) + 0.5)));
+    if (!a->dx) clusters[0] = 0;
+    if (!a->dw) clusters[0] = kClusters;
     clusters[1] = kClusters - clusters[0];
     for (int p = 0; p < 2; ++p) {
+        if (clusters[p] == 0) continue;            // not asked for
         const int rows = p ? dw_rows : dx_rows, chunks = p ? dw_chunks : dx_chunks;
         const int by_two = col_tiles % 2 == 0 ? 2 : col_tiles % 3 == 0 ? 3 : 1;
         const int siblings = clusters[p] >= by_two ? by_two : 1;

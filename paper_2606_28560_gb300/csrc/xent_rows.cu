@@ -169,7 +169,8 @@ __device__ __forceinline__ void finish_row(const Problem& p, const FwdParts& par
 //   dw[v] = sum_n g[n][v] x[n]   to memory,   dx[n] += g[n][v] w[v]   in registers.
 // parts[block][n][D]: dx over the block's rows of w.
 template <typename T, int NT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, T* dw, float* parts) {
+__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, T* dw, float* parts,
+                                                                    bool want_dx) {
     extern __shared__ float xs[];                  // [NT][steps * 256], staged
     constexpr int kValues = NT * kGroup, kBatch = kGroup * kWarps;
     __shared__ float gs[kBatch][NT];
@@ -238,10 +239,11 @@ __global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, c
 #pragma unroll
                     for (int j = 0; j < 8; ++j) dx[n][j] = fmaf(g, a[j], dx[n][j]);
                 }
-                store8<T, VECTORS>(dw + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, o);
+                if (dw) store8<T, VECTORS>(dw + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, o);
             }
         }
     }
+    if (!want_dx) return;
     // the groups' sums of a column, one row of x at a time, over the space of x
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -373,15 +375,15 @@ template <typename T> cudaError_t rows(const Problem& p, const FwdParts& parts, 
 }
 
 template <typename T, int NT>
-cudaError_t launch_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dw, float* parts, int blocks,
-                                 cudaStream_t st) {
+cudaError_t launch_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dw, float* parts, bool want_dx,
+                                 int blocks, cudaStream_t st) {
     // x, and later eight values of each of the block's threads
     const size_t smem = std::max((size_t)NT * ((p.D + 255) / 256) * 256 * 4, (size_t)32 * kWarps * 8 * 4);
     if (p.D % 8 == 0)
         return launch_kernel(rows_gradient_kernel<T, NT, true>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
-                             static_cast<T*>(dw), parts);
+                             static_cast<T*>(dw), parts, want_dx);
     return launch_kernel(rows_gradient_kernel<T, NT, false>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
-                         static_cast<T*>(dw), parts);
+                         static_cast<T*>(dw), parts, want_dx);
 }
 template <typename T>
 cudaError_t rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts, int blocks,
@@ -390,13 +392,13 @@ cudaError_t rows_gradient(const Problem& p, const float* lse, const float* dloss
     {
         ProfScope s("xent_few_rows_grad", st);
         switch (rows_at_once(p.N, p.D)) {
-        case 1: e = launch_rows_gradient<T, 1>(p, lse, dloss, dw, parts, blocks, st); break;
-        case 2: e = launch_rows_gradient<T, 2>(p, lse, dloss, dw, parts, blocks, st); break;
-        case 4: e = launch_rows_gradient<T, 4>(p, lse, dloss, dw, parts, blocks, st); break;
-        default: e = launch_rows_gradient<T, 8>(p, lse, dloss, dw, parts, blocks, st);
+        case 1: e = launch_rows_gradient<T, 1>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
+        case 2: e = launch_rows_gradient<T, 2>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
+        case 4: e = launch_rows_gradient<T, 4>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
+        default: e = launch_rows_gradient<T, 8>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st);
         }
     }
-    if (e != cudaSuccess) return e;
+    if (e != cudaSuccess || !dx) return e;
     ProfScope s("xent_join_dx", st);
     const long long values = (long long)p.N * p.D;
     return launch_kernel(join_dx_kernel<T>, dim3((unsigned)((values + 31) / 32)), dim3(256), 0, st, parts, blocks, values,

@@ -24,7 +24,9 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dloss):
         x, w, targets, lse = ctx.saved_tensors
-        dx, dw = B.linear_xent_bwd(x, w, targets, lse, dloss.contiguous(), ignore_index=ctx.ignore_index)
+        want_dx, want_dw = ctx.needs_input_grad[:2]
+        dx, dw = B.linear_xent_bwd(x, w, targets, lse, dloss.contiguous(), ignore_index=ctx.ignore_index,
+                                   want_dx=want_dx, want_dw=want_dw)
         return dx, dw, None, None
 
 

@@ -238,6 +238,27 @@ def test_writes_only_its_outputs(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [0, 3, 700])
+def test_one_gradient_alone(N, dtype):
+    x, w, t, dl = make(N, 520, 1500, TYPES[dtype], 18)
+    _, lse = fa.linear_xent_fwd(x, w, t)
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    a, none = fa.linear_xent_bwd(x, w, t, lse, dl, want_dw=False)
+    none2, b = fa.linear_xent_bwd(x, w, t, lse, dl, want_dx=False)
+    assert none is None and none2 is None
+    # the depth may be cut elsewhere: the sums' roundings, and bf16's own
+    for got, want in ((a, dx), (b, dw)):
+        if want.numel():
+            tol = (2.0 ** -8 if dtype == "bf16" else 4e-6) * max(1e-30, float(want.double().norm()))
+            assert float((got.double() - want.double()).norm()) <= tol
+    x.requires_grad_(True)                        # a frozen head
+    if N:
+        fa.linear_cross_entropy(x, w, t).backward()
+        assert x.grad is not None and w.grad is None
+
+
+@pytest.mark.gpu
 def test_gradient_against_differences():
     """Central differences of the library's own loss; a loss is within some 1e-6 in
     fp32, so a quotient over 2 h = 0.04 is within 1e-4, plus h^2 of the third derivative."""
@@ -314,8 +335,9 @@ def test_refused_before_any_launch(call, bad):
 
 def test_refused_outputs():
     assert _fwd(loss=0) == 1 and _fwd(loss=264) == 1
+    assert _bwd(dl=0) == 1 and _bwd(dx=0, dw=0) == 1
     for name in ("dl", "dx", "dw"):
-        assert _bwd(**{name: 0}) == 1 and _bwd(**{name: 264}) == 1
+        assert _bwd(**{name: 264}) == 1
 
 
 def test_no_rows_need_no_pointers():
