@@ -15,7 +15,8 @@
 // The tensor core truncates as it accumulates (some 2e-8 of the running sum
 // for each 16 of depth), so a long depth is cut into runs whose sums are added
 // in registers: 512 deep for bf16 logits, whose loss and lse are fp32 results.
-// The products of bf16 gradients, rounded to 8 bits at the end, are not cut.
+// The products of bf16 gradients, rounded to 8 bits at the end, are cut only
+// where their depth passes 2^17.
 // fp32 operands are sums of three bf16 planes ("wide" below: several planes,
 // runs of 128, CUDA's expf).
 #include <algorithm>
@@ -51,7 +52,7 @@ template <int MODE, int NB, bool RESIDENT> struct Config {
 // chunks of 64 from k0 to k1.
 struct Item {
     int m0, n0, k0, k1;
-    int problem = 0;                                 // products: 0 dx, 1 dw
+    int problem = 0;                               // products: 0 dx, 1 dw
     int unit;                                      // forward, gradient: segment of the columns
     bool first, last;                              // forward, gradient: tile of its unit
     bool whole;                                    // products: the whole depth
@@ -168,8 +169,8 @@ template <int COUNT> __device__ __forceinline__ void put_row(__nv_bfloat16* out,
     }
 }
 
-// Row `row`, n columns (COUNT at most) from c0 of a finished product.  What g was divided by is
-// multiplied back here.
+// Row `row`, n columns (COUNT at most) from c0 of a finished product.  What g was
+// divided by is multiplied back here.
 template <bool WIDE, int COUNT>
 __device__ __forceinline__ void write_product(const Args& a, int problem, int row, int c0, int n, float scale, float* acc) {
     if (row >= a.prob[problem].rows) return;
@@ -287,17 +288,16 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
 
     const int combos = WIDE ? a.combos : 1;        // products of planes for one of values
     // Depth of a run (chunks of 64) whose sums stay in the tensor core.
-    constexpr int kRun = WIDE ? 2 : MODE == kProducts ? (1 << 30) : 8;
+    constexpr int kRun = WIDE ? 2 : MODE != kProducts ? 8 : NB == 1 ? 2048 : 1 << 30;
 
     if (warp < 4) {
         tc5::registers_down<56>();
         if (warp == 0 && tc5::elect_one()) {
             // ---- loads: this CTA's operands; the even CTA's barrier counts both's bytes
             const unsigned full0 = tc5::map_to(full, 0);
-            // x and w are read by every cluster; g passes through once in each product (but
-            // its planes are read for several products of planes).  (Hints
-            // of 16384 rows, 512 wide, 32768 columns: gradient 360 -> 344 us, products 644 -> 614;
-            // a hint on g's stores changes neither.)
+            // x and w are read by every cluster; g passes through once in each product (its
+            // planes, where it has several, are read again).  With these hints and 16384
+            // rows, 512 wide, 32768 columns: gradient 360 -> 344 us, products 644 -> 614.
             const unsigned long long keep = tc5::policy_keep(), pass = WIDE ? tc5::policy_normal() : tc5::policy_pass();
             Walk<MODE> walk(a, cluster, clusters);
             Item it;
@@ -344,7 +344,9 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         const unsigned bar = full0 + 8 * stage, dst = stages0 + stage * C::kStageBytes;
                         if (MODE != kProducts) {
                             if (!RESIDENT && a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, keep);
-                            if (b_here) tc5::load_box(dst + (RESIDENT ? 0 : kOperandBytes), &maps.m[1], chunk * 64, a.v0 + it.n0 + 128 * rank, pb, bar, keep);
+                            if (b_here)
+                                tc5::load_box(dst + (RESIDENT ? 0 : kOperandBytes), &maps.m[1], chunk * 64,
+                                              a.v0 + it.n0 + 128 * rank, pb, bar, keep);
                         } else {
                             if (it.problem == 0) {
                                 if (a_here) tc5::load_box(dst, &maps.m[0], chunk * 64, it.m0 + 128 * rank, pa, bar, pass);
@@ -420,7 +422,8 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         const unsigned long long da = tc5::descriptor(RESIDENT ? smem0 + i * kOperandBytes : src, a_rows ? 8192u : 16u);
 #pragma unroll
                         for (int b = 0; b < NB; ++b) {
-                            const unsigned long long db = tc5::descriptor(src + kOperandBytes * ((RESIDENT ? 0 : 1) + b), b_rows ? 8192u : 16u);
+                            const unsigned long long db =
+                                tc5::descriptor(src + kOperandBytes * ((RESIDENT ? 0 : 1) + b), b_rows ? 8192u : 16u);
                             if (cols[b] > 0) {
 #pragma unroll
                                 for (unsigned k = 0; k < 4; ++k)
@@ -758,7 +761,8 @@ bool encode(CUtensorMap* map, const void* base, long long cols, long long rows, 
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int MODE, int NB, bool WIDE, bool RESIDENT> cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
+template <int MODE, int NB, bool WIDE, bool RESIDENT>
+cudaError_t launch(const Args& a, const Maps& maps, int clusters, cudaStream_t st) {
     auto kern = xent_kernel<MODE, NB, WIDE, RESIDENT>;
     // The register split of the two halves of a block draws on what the block
     // was launched with: refuse to launch a build that was given less.
@@ -846,6 +850,15 @@ static int unit_tiles_of(int row_tiles, int col_tiles) {
     return unit;
 }
 
+// Whether products are made of several products of planes.  One bf16 plane rounds
+// each g to 8 bits, which the sums of dx and dw average out over many; fp32 I/O
+// keeps three planes (24 bits), and so does bf16 I/O where whole tiles come to at
+// most 2^26 multiplications: there the sums are short and the further planes hide
+// behind the launches (100 rows, 64 wide, 257 columns: 27 us either way).
+static bool several_planes(int N, int D, int V, bool bf16) {
+    return !bf16 || 256.0 * tiles256(N) * 256.0 * tiles256(V) * D <= (double)(1 << 26);
+}
+
 // Whether a handful of rows goes in one pass over w (xent_rows.cu) rather than to
 // the tensor cores.  Forward and backward go the same way: p = exp(logit - lse) is
 // good to the logits' own rounding only if both come from the same arithmetic.
@@ -866,6 +879,7 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16) {
         f.pack = false;
         f.segments = few_rows_segments(V);
     } else {
+        f.wide = several_planes(N, D, V, bf16);
         f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
         f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
     }
@@ -881,7 +895,8 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16) {
 }
 
 cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st) {
-    const FwdParts parts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l), reinterpret_cast<float*>(ws + f.target)};
+    const FwdParts parts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l),
+                         reinterpret_cast<float*>(ws + f.target)};
     cudaError_t e;
     if (f.few_rows) {
         {
@@ -916,7 +931,7 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     {
         ProfScope s("xent_fwd", st);
         set_combos(&a, f.planes, f.planes);
-        e = !bf16 ? launch<kForward, 1, true, false>(a, maps, clusters, st)
+        e = f.wide ? launch<kForward, 1, true, false>(a, maps, clusters, st)
             : resident(a) ? launch<kForward, 1, false, true>(a, maps, clusters, st)
                           : launch<kForward, 1, false, false>(a, maps, clusters, st);
     }
@@ -952,13 +967,9 @@ static int share_products(Args* a, int dx_rows, int dw_rows, int col_tiles, int 
     return clusters[0] + clusters[1];
 }
 
-// g of a piece is held in memory for the two products: at most 512 MiB of it
-// (at least 256 columns; 16384 rows, 512 wide, 32768 columns: two products launches of
-// 339 us; pieces of 256 MiB 791 us together, one piece 650 us).  One bf16 plane rounds each g to 8 bits, which the
-// products average out over many; fp32 I/O keeps three planes (24 bits), and so
-// does bf16 I/O where whole tiles come to at most 2^26 multiplications: there the
-// sums are short and the further planes hide behind the launches (100 rows, 64
-// wide, 257 columns: 27 us either way).
+// g of a piece is held in memory for the two products: at most 512 MiB of it, at
+// least 256 columns (16384 rows, 512 wide, 32768 columns: products of 678 us in all;
+// 791 us with pieces of 256 MiB, 650 us with one piece of 1 GiB).
 BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     BwdPlan f{};
     f.few_rows = stream_wins(N, D, V, bf16);
@@ -968,9 +979,10 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
         return f;
     }
     plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
-    f.wide = !bf16 || 256.0 * tiles256(N) * 256.0 * tiles256(V) * D <= (double)(1 << 26);
+    f.wide = several_planes(N, D, V, bf16);
     f.g_planes = f.wide ? 3 : 1;
-    f.blocks = !f.wide && D > 256 ? 2 : 1;
+    // (a tile of two blocks keeps its sums in the tensor core over its whole depth)
+    f.blocks = !f.wide && D > 256 && std::max(N, V) <= (1 << 18) ? 2 : 1;
     const long long fit = (512ll << 20) / (2ll * f.g_planes * std::max(N, 1)) / 256 * 256;
     f.cols = (int)std::min<long long>(V, std::max(256ll, fit));
     f.ldg = (f.cols + 7) / 8 * 8;
@@ -990,7 +1002,8 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
 cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16, const float* lse, const float* dloss, void* dx,
                          void* dw, cudaStream_t st) {
     if (f.few_rows)
-        return launch_few_rows_gradient(p, lse, dloss, dx, dw, reinterpret_cast<float*>(ws + f.partials), few_rows_blocks(p.V), bf16, st);
+        return launch_few_rows_gradient(p, lse, dloss, dx, dw, reinterpret_cast<float*>(ws + f.partials), few_rows_blocks(p.V),
+                                        bf16, st);
     const void *x = p.x, *w = p.w;
     cudaError_t e;
     if (f.pack) {
@@ -1050,7 +1063,8 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
                               : launch<kGradient, 1, false, false>(a, logits, clusters, st);
         }
         if (e != cudaSuccess) return e;
-        const int workers = share_products(&a, tiles256(p.N), tiles256(cols), d_tiles, (cols + 63) / 64, (p.N + 63) / 64, f.wide);
+        const int workers =
+            share_products(&a, tiles256(p.N), tiles256(cols), d_tiles, (cols + 63) / 64, (p.N + 63) / 64, f.wide);
         a.dx_add = v0 > 0;
         a.dx_done = v0 + cols >= p.V;
         {

@@ -48,7 +48,7 @@ struct Maps {
 
 struct FwdPlan {
     bool few_rows;                                 // not on the tensor cores: one stream over w
-    bool pack;
+    bool pack, wide;                               // wide: logits of several planes, or in short runs
     int planes, depth;                             // of packed operands: planes, row length
     int unit_tiles, segments;                      // segments: entries of a row in FwdParts
     size_t x, w, m, l, target, total;              // workspace offsets
