@@ -100,10 +100,13 @@ template <typename T> __device__ __forceinline__ float sum_squares(const T* p, i
 #pragma unroll
         for (int k = 0; k < kNormBatch; ++k) add(v[k]);
     }
-    for (; i < vectors; i += kThreads) {
-        V v;
-        v.u = __ldg(body + i);
-        add(v);
+    if (i < vectors) {                     // fewer than a batch are left
+        V v[kNormBatch];
+#pragma unroll
+        for (int k = 0; k < kNormBatch; ++k)
+            v[k].u = i + k * kThreads < vectors ? __ldg(body + i + k * kThreads) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < kNormBatch; ++k) add(v[k]);
     }
     return (s[0] + s[1]) + (s[2] + s[3]);
 }
@@ -169,10 +172,14 @@ template <typename T> __device__ __forceinline__ void scale(const T* in, T* out,
 #pragma unroll
         for (int k = 0; k < kClipBatch; ++k) __stcs(to + k0 + k * kThreads, scaled(v[k], c));
     }
-    for (; k0 < vectors; k0 += kThreads) {
-        V v;
-        v.u = body[k0];
-        __stcs(to + k0, scaled(v, c));
+    if (k0 < vectors) {                    // fewer than a batch are left
+        V v[kClipBatch];
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k)
+            if (k0 + k * kThreads < vectors) v[k].u = body[k0 + k * kThreads];
+#pragma unroll
+        for (int k = 0; k < kClipBatch; ++k)
+            if (k0 + k * kThreads < vectors) __stcs(to + k0 + k * kThreads, scaled(v[k], c));
     }
     // the tail, or everything where in and out start at different offsets within 16 bytes
     for (int i = tail + threadIdx.x; i < n; i += kClipBatch * kThreads) {
