@@ -212,6 +212,35 @@ template <int NB> __device__ __forceinline__ float* slot_at(const Args& a, int s
 }
 
 __device__ __forceinline__ float ex2(float x) { return mma::ex2(x); }
+// Two fp32 operations at a time, each rounded as its scalar form.
+__device__ __forceinline__ unsigned long long pair(float x, float y) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long p, float& x, float& y) {
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(x), "=f"(y) : "l"(p));
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long add2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 // The largest of 256 threads' values (of 8 warps in a row, t counted from the
 // first); they meet at named barrier 1.
@@ -528,10 +557,10 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         for (int j = 0; j < 128; ++j) s = c0 + j == target ? acc[j] : s;
                         a.parts.target_logit[row] = s;
                     }
-                    float mx[4] = {acc[0], acc[1], acc[2], acc[3]};
+                    float mx[4] = {m, acc[0], acc[1], acc[2]};
 #pragma unroll
-                    for (int j = 4; j < 128; ++j) mx[j & 3] = fmaxf(mx[j & 3], acc[j]);
-                    const float top = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
+                    for (int j = 3; j < 127; j += 2) mx[j / 2 & 3] = max3(mx[j / 2 & 3], acc[j], acc[j + 1]);
+                    const float top = max3(max3(mx[0], mx[1], mx[2]), mx[3], acc[127]);
                     const float ms = top == -INFINITY ? 0.f : top;
                     float s[4] = {0.f, 0.f, 0.f, 0.f};
                     if (WIDE) {
@@ -540,8 +569,16 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         l = l * expf(m - ms);
                     } else {
                         const float off = -ms * kLog2e;
+                        const unsigned long long scale2 = pair(kLog2e, kLog2e), off2 = pair(off, off);
+                        unsigned long long s2[2] = {0ull, 0ull};
 #pragma unroll
-                        for (int j = 0; j < 128; ++j) s[j & 3] += ex2(fmaf(acc[j], kLog2e, off));
+                        for (int j = 0; j < 128; j += 2) {
+                            float u, v;
+                            unpair(fma2(pair(acc[j], acc[j + 1]), scale2, off2), u, v);
+                            s2[j / 2 & 1] = add2(s2[j / 2 & 1], pair(ex2(u), ex2(v)));
+                        }
+                        unpair(s2[0], s[0], s[1]);
+                        unpair(s2[1], s[2], s[3]);
                         l = l * ex2(fmaf(m, kLog2e, off));
                     }
                     l += (s[0] + s[1]) + (s[2] + s[3]);
@@ -557,9 +594,18 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
 #pragma unroll
                         for (int j = 0; j < 128; ++j) acc[j] = ok ? 0.f : NAN;
                     } else {
+                        if (WIDE) {
 #pragma unroll
-                        for (int j = 0; j < 128; ++j)
-                            acc[j] = dl * (WIDE ? expf(acc[j] - z) : ex2(fmaf(acc[j], kLog2e, -z2)));
+                            for (int j = 0; j < 128; ++j) acc[j] = dl * expf(acc[j] - z);
+                        } else {
+                            const unsigned long long scale2 = pair(kLog2e, kLog2e), off2 = pair(-z2, -z2), dl2 = pair(dl, dl);
+#pragma unroll
+                            for (int j = 0; j < 128; j += 2) {
+                                float u, v;
+                                unpair(fma2(pair(acc[j], acc[j + 1]), scale2, off2), u, v);
+                                unpair(mul2(pair(ex2(u), ex2(v)), dl2), acc[j], acc[j + 1]);
+                            }
+                        }
                         const int local = target - a.v0 - c0;
                         if ((unsigned)local < 128u) {
 #pragma unroll

@@ -143,6 +143,24 @@ def test_same_result_every_time_and_on_another_stream():
 
 
 @pytest.mark.gpu
+def test_in_a_captured_graph():
+    grads, _ = tensors(SPECS["small mix"] + SPECS["around a chunk"], 5, 1)
+    outs, _ = tensors(SPECS["small mix"] + SPECS["around a chunk"], 6, 3)
+    fa.clip_grads(grads, 1.0, out=outs)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        norm = fa.clip_grads(grads, 1.0, out=outs)
+    for t in grads:
+        t.mul_(2)
+    g.replay()
+    torch.cuda.synchronize()
+    want, coef = truth(grads, 1.0)
+    assert abs(float(norm) - want) <= NORM_TOL * want
+    close(outs, grads, coef)
+
+
+@pytest.mark.gpu
 def test_parameters():
     m = torch.nn.Sequential(torch.nn.Linear(33, 65), torch.nn.Linear(65, 9), torch.nn.Linear(9, 1)).cuda()
     m[2].weight.requires_grad_(False)             # a parameter without a gradient

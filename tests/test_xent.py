@@ -206,6 +206,49 @@ def test_same_result_every_time_and_on_another_stream(dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [2, 300])
+def test_in_a_captured_graph(N, dtype):
+    """Replays on changed inputs give what direct calls give."""
+    x, w, t, dl = make(N, 136, 2000, TYPES[dtype], 19)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):                    # warm up off the capture
+        loss, lse = fa.linear_xent_fwd(x, w, t)
+        fa.linear_xent_bwd(x, w, t, lse, dl)
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        loss, lse = fa.linear_xent_fwd(x, w, t)
+        dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    x2, w2, t2, dl2 = make(N, 136, 2000, TYPES[dtype], 20)
+    for a, b in ((x, x2), (w, w2), (t, t2), (dl, dl2)):
+        a.copy_(b)
+    for _ in range(2):
+        g.replay()
+    torch.cuda.synchronize()
+    want = fa.linear_xent_fwd(x2, w2, t2)
+    want += fa.linear_xent_bwd(x2, w2, t2, want[1], dl2)
+    assert all(torch.equal(a, b) for a, b in zip((loss, lse, dx, dw), want))
+
+
+@pytest.mark.gpu
+def test_depth_beyond_a_run_of_the_tensor_core():
+    """Positive operands, whose truncated sums would drift if a deep logit were
+    summed by the tensor core alone (128 steps of 16 at some 2e-8 each: 3e-6 of a
+    sum of some hundreds, 1e-3).  Runs of 512 keep the drift below 32 steps'."""
+    g = torch.Generator().manual_seed(21)
+    x, w = (torch.rand(n, 2048, generator=g).bfloat16().cuda() for n in (300, 700))
+    w /= 8
+    t = torch.randint(0, 700, (300,), generator=g).cuda()
+    s = x.double() @ w.double().t()
+    lse = fa.linear_xent_fwd(x, w, t)[1]
+    off = (lse.double() - torch.logsumexp(s, 1)).abs().max()
+    # 32 steps of 2^-24 to 2^-23 of a run's sum (a quarter of s), four runs, their fp32 sums, lse's own rounding
+    assert float(off) <= float(s.abs().max()) * (32 * 2.0 ** -23 + 8 * 2.0 ** -24)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
 def test_writes_only_its_outputs(dtype):
     """Outputs and workspace lie between guards of a known pattern."""
     N, D, V = 130, 72, 515
