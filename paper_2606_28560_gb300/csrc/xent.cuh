@@ -33,18 +33,30 @@ struct FwdParts {
     float* target_logit;
 };
 
-// The tensor-core forward keeps them as [segment][row] ...
+// The fifth-generation tensor cores keep them as [segment][row] ...
 cudaError_t launch_join_segments(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st);
-// ... the forward of few rows as [row][segment].
+// ... and the passes of few rows as [row][segment].
+cudaError_t launch_join_rows(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st);
+// dx from parts [ranges][N][D].
+cudaError_t launch_join_dx(const Problem& p, const float* parts, int ranges, void* dx, bool bf16, cudaStream_t st);
+
+// One to four rows (xent_stream.cu).  Scratch of the gradient: parts [blocks][N][D].
+bool stream_applies(int N, int D);
+int stream_segments(int V);
+cudaError_t launch_stream(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);
+int stream_blocks(int V);
+cudaError_t launch_stream_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts, int blocks,
+                                   bool bf16, cudaStream_t st);
+
+// Few rows (xent_rows.cu).  Scratch of the gradient: gradient [V][tokens], parts
+// [ranges][N][D]; all fp32.
+bool few_rows_applies(int N, int D);
+int few_rows_tokens(int N);                        // N rounded up to 8, 16 or 32
 int few_rows_segments(int V);
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);
-cudaError_t launch_join_rows(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st);
-
-// The gradient of few rows: parts is [blocks][N][D] fp32 of scratch.
-int few_rows_at_most(int N, int D);                // rows that it can take, of N
-int few_rows_blocks(int V);
-cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts,
-                                     int blocks, bool bf16, cudaStream_t st);
+int few_rows_ranges(int N, int D, int V, bool bf16);
+cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* gradient,
+                                     float* parts, int ranges, bool bf16, cudaStream_t st);
 
 }  // namespace xent
 }  // namespace fibattn

@@ -905,26 +905,31 @@ static bool several_planes(int N, int D, int V, bool bf16) {
     return !bf16 || 256.0 * tiles256(N) * 256.0 * tiles256(V) * D <= (double)(1 << 26);
 }
 
-// Whether a handful of rows goes in one pass over w (xent_rows.cu) rather than to
-// the tensor cores.  Forward and backward go the same way: p = exp(logit - lse) is
-// good to the logits' own rounding only if both come from the same arithmetic.
-// Forward and backward together, us on the GPU, one pass / tensor cores:
-//   512 wide, 32768 columns: bf16 35 / 60 (one row), 48 / 60 (four), 80 / 58 (eight);
-//                            fp32 58 / 230 (one row), 93 / 220 (eight)
-//   512 wide, 4000 columns:  bf16 23 / 30 (eight);  64 wide, 257 columns: bf16 15 / 26 (eight)
-static bool stream_wins(int N, int D, int V, bool bf16) {
-    const int most = !bf16 || (long long)V * D <= (4 << 20) ? 8 : 4;
-    return N <= std::min(most, few_rows_at_most(N, D));
+// Forward and backward go the same way: p = exp(logit - lse) is good to the
+// logits' own rounding only if both come from the same arithmetic.  Forward and
+// backward together, us on the GPU, stream / few rows / tiles:
+//   512 wide, 32768 columns: bf16 35 / 48 / 67 (one row), 80 / 48 / 67 (eight),
+//                            - / 62 / 67 (sixteen), - / 109 / 65 (thirty-two)
+//                            fp32 58 / 79 / 211 (one row), 93 / 81 / 205 (eight),
+//                            - / 177 / 203 (thirty-two)
+//   2048 wide, 131072 columns: bf16 395 / 530 / 498 (one row), - / 770 / 500 (sixteen)
+//                            fp32 746 / 850 / 2640 (one row), - / 1290 / 2660 (sixteen)
+//   64 wide, 257 columns:    bf16 9 / 12 / 27 (one row), - / 18 / 30 (thirty-two)
+static Way way_of(int N, int D, int V, bool bf16) {
+    if (stream_applies(N, D)) return Way::kStream;
+    const int most = !bf16 || (long long)V * D <= (1 << 20) ? 32 : D <= 512 ? 16 : 0;
+    return N <= most && few_rows_applies(N, D) ? Way::kFewRows : Way::kTiles;
 }
 
 FwdPlan plan_forward(int N, int D, int V, bool bf16) {
     FwdPlan f{};
-    plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
-    f.few_rows = stream_wins(N, D, V, bf16);
-    if (f.few_rows) {
-        f.pack = false;
+    f.way = way_of(N, D, V, bf16);
+    if (f.way == Way::kStream) {
+        f.segments = stream_segments(V);
+    } else if (f.way == Way::kFewRows) {
         f.segments = few_rows_segments(V);
     } else {
+        plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
         f.wide = several_planes(N, D, V, bf16);
         f.unit_tiles = unit_tiles_of(tiles256(N), tiles256(V));
         f.segments = 2 * ((tiles256(V) + f.unit_tiles - 1) / f.unit_tiles);
@@ -944,10 +949,10 @@ cudaError_t run_forward(const Problem& p, const FwdPlan& f, char* ws, bool bf16,
     const FwdParts parts{reinterpret_cast<float*>(ws + f.m), reinterpret_cast<float*>(ws + f.l),
                          reinterpret_cast<float*>(ws + f.target)};
     cudaError_t e;
-    if (f.few_rows) {
+    if (f.way != Way::kTiles) {
         {
-            ProfScope s("xent_few_rows", st);
-            e = launch_few_rows(p, parts, f.segments, bf16, st);
+            ProfScope s(f.way == Way::kStream ? "xent_stream" : "xent_few_rows", st);
+            e = f.way == Way::kStream ? launch_stream(p, parts, f.segments, bf16, st) : launch_few_rows(p, parts, f.segments, bf16, st);
         }
         if (e != cudaSuccess) return e;
         ProfScope s("xent_join", st);
@@ -1018,10 +1023,15 @@ static int share_products(Args* a, int dx_rows, int dw_rows, int col_tiles, int 
 // 791 us with pieces of 256 MiB, 650 us with one piece of 1 GiB).
 BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     BwdPlan f{};
-    f.few_rows = stream_wins(N, D, V, bf16);
-    if (f.few_rows) {
-        f.partials = 0;
-        f.total = up256((size_t)few_rows_blocks(V) * N * D * 4);
+    f.way = way_of(N, D, V, bf16);
+    if (f.way == Way::kStream) {
+        f.ranges = stream_blocks(V);
+    } else if (f.way == Way::kFewRows) {
+        f.ranges = few_rows_ranges(N, D, V, bf16);
+        f.partials = up256((size_t)few_rows_tokens(N) * V * 4);     // after g
+    }
+    if (f.way != Way::kTiles) {
+        f.total = f.partials + up256((size_t)f.ranges * N * D * 4);
         return f;
     }
     plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
@@ -1047,9 +1057,9 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
 
 cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16, const float* lse, const float* dloss, void* dx,
                          void* dw, cudaStream_t st) {
-    if (f.few_rows)
-        return launch_few_rows_gradient(p, lse, dloss, dx, dw, reinterpret_cast<float*>(ws + f.partials), few_rows_blocks(p.V),
-                                        bf16, st);
+    float *g = reinterpret_cast<float*>(ws + f.g), *parts = reinterpret_cast<float*>(ws + f.partials);
+    if (f.way == Way::kStream) return launch_stream_gradient(p, lse, dloss, dx, dw, parts, f.ranges, bf16, st);
+    if (f.way == Way::kFewRows) return launch_few_rows_gradient(p, lse, dloss, dx, dw, g, parts, f.ranges, bf16, st);
     const void *x = p.x, *w = p.w;
     cudaError_t e;
     if (f.pack) {
@@ -1074,7 +1084,7 @@ cudaError_t run_backward(const Problem& p, const BwdPlan& f, char* ws, bool bf16
     const int d_tiles = (p.D + 256 * f.blocks - 1) / (256 * f.blocks);
     a.tile_cols = ((p.D + d_tiles - 1) / d_tiles + 31) / 32 * 32;
     a.out_f32 = !bf16;
-    a.partials = reinterpret_cast<float*>(ws + f.partials);
+    a.partials = parts;
     a.scale = reinterpret_cast<float*>(ws + f.scale);
     a.dx_acc = reinterpret_cast<float*>(ws + f.dx_acc);
     a.dx = dx;

@@ -46,8 +46,11 @@ struct Maps {
     CUtensorMap m[4];
 };
 
+// Where a call goes: one to four rows, few rows, or tiles on the fifth-generation cores.
+enum class Way { kStream, kFewRows, kTiles };
+
 struct FwdPlan {
-    bool few_rows;                                 // not on the tensor cores: one stream over w
+    Way way;
     bool pack, wide;                               // wide: logits of several planes, or in short runs
     int planes, depth;                             // of packed operands: planes, row length
     int unit_tiles, segments;                      // segments: entries of a row in FwdParts
@@ -57,10 +60,11 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16);
 cudaError_t run_forward(const Problem& p, const FwdPlan& plan, char* ws, bool bf16, float* loss, float* lse, cudaStream_t st);
 
 struct BwdPlan {
-    bool few_rows;                                 // not on the tensor cores: one pass over w
+    Way way;
     bool pack, wide;                               // wide: products of several planes
     int planes, depth, g_planes;
     int blocks;                                    // blocks of 256 columns of a products' tile
+    int ranges;                                    // parts of dx (not for tiles)
     int cols, ldg;                                 // columns of a piece; row length of g
     size_t x, w, g, dx_acc, partials, scale, total;
     int maxima;                                    // blocks that look for the largest |dloss|; 0: not apart

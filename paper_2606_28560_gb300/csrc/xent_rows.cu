@@ -1,10 +1,19 @@
-// xent_rows.cu -- the cross entropy for few rows (a decoding step's tokens), and
-// the join of per-row statistics.
+// xent_rows.cu -- the cross entropy for five to 32 rows (a small batch over a large
+// head), and the joins of per-row statistics and of dx's parts.
 //
-// With few rows the work is one pass over w, so this kernel is built as a
-// stream: every warp takes a run of consecutive rows of w, four at a time, a
-// lane 16 bytes of each per step, against x in shared memory (fp32).  Products
-// and sums are fp32 FMAs for either type.  Bound by memory.
+// With few rows the work is w read once per pass, and fp32 cannot afford to be
+// split into planes in memory for the fifth-generation cores.  These kernels are
+// streams over w: every warp takes sixteen rows of w at a time straight from memory into
+// the operand registers of mma.sync (tf32, 16 x 8 x 8), against up to 32 rows of x
+// in shared memory.  fp32 values go as two tf32 values, x = hi + lo, three products
+// of the four (the fourth is below 2^-22); bf16 values are exact.  The large
+// products are summed 64 deep before they are added in fp32, because the tensor
+// core truncates.  Bound by memory up to some 16 rows, by the tensor rate
+// (150 T multiplications a second, a third of it in fp32) beyond.
+//
+// A sum does not care for the order of its terms, so lanes take them as memory
+// gives them: in the logits a lane's depth values are consecutive; in the
+// products a lane's four columns are, and its tokens.
 #include <algorithm>
 
 #include "xent.cuh"
@@ -14,146 +23,458 @@ namespace xent {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kGroup = 4;                          // rows of w that a warp has under way
+constexpr int kTileRows = 16;                      // rows of w in a warp's hands
 
-// x of one step of a row (256 values: 8 per lane) is laid out as the lanes'
-// first four values, then their last four, so that a warp's 16-byte reads touch
-// every bank once.
-__device__ __forceinline__ int staged(int k) { return (k & ~255) + ((k >> 2) & 1) * 128 + ((k >> 3) & 31) * 4 + (k & 3); }
+template <typename T> struct Lane { static constexpr int kValues = 16 / sizeof(T); };   // of 16 bytes
 
-// s[i] summed over the warp, one value to each lane: returns the sum of value
-// owner(lane) = lane / (32 / K).  Halving exchanges: K - 1 shuffles and one for
-// each bit that is left, where a butterfly for every value would take 5 K.
-template <int K> __device__ __forceinline__ float sum_to_owner(float* s, int lane) {
+// The 16 bytes at p, n values of them (zeros past them).  VECTORS: 16-byte
+// boundaries, and n is 0 or less or all or more.
+template <typename T, bool VECTORS> __device__ __forceinline__ uint4 fetch16(const T* p, int n) {
+    if constexpr (VECTORS) {
+        return n > 0 ? __ldg(reinterpret_cast<const uint4*>(p)) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        unsigned w[4];
 #pragma unroll
-    for (int h = K / 2, o = 16; h > 0; h /= 2, o /= 2) {
-        const bool up = lane & o;
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                w[i] = i < n ? __float_as_uint(p[i]) : 0u;
+            } else {
+                const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
+                w[i] = (2 * i < n ? (unsigned)q[2 * i] : 0u) | (2 * i + 1 < n ? (unsigned)q[2 * i + 1] << 16 : 0u);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+template <typename T> __device__ __forceinline__ void unfold(const uint4& u, float* x) {
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < h; ++i) {
-            const float give = up ? s[i] : s[i + h], keep = up ? s[i + h] : s[i];
-            s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            x[i] = __uint_as_float(w[i]);
+        } else {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
     }
-    float r = s[0];
-#pragma unroll
-    for (int o = 1; o < 32 / K; o *= 2) r += __shfl_xor_sync(0xffffffffu, r, o);
-    return r;
 }
-
-// Eight values at p, of which `n` are there (zeros, or no write, past them).
-// VECTORS: rows start on 16-byte boundaries and n is 0 or less, or 8 or more.
-template <typename T, bool VECTORS> __device__ __forceinline__ void load8(const T* p, int n, float* x) {
+// Four values at p, of which n are there.  VECTORS: all or none, aligned to them.
+template <typename T, bool VECTORS> __device__ __forceinline__ void load4(const T* p, int n, float* x) {
     if (VECTORS && n > 0) {
-        Vec8<T>::load(p, x);
+        if constexpr (sizeof(T) == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(p);
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            x[0] = __uint_as_float(u.x << 16); x[1] = __uint_as_float(u.x & 0xffff0000u);
+            x[2] = __uint_as_float(u.y << 16); x[3] = __uint_as_float(u.y & 0xffff0000u);
+        }
         return;
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = !VECTORS && j < n ? to_f(p[j]) : 0.f;
+    for (int j = 0; j < 4; ++j) x[j] = !VECTORS && j < n ? to_f(p[j]) : 0.f;
 }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float x) { *p = __float2bfloat16(x); }
-template <typename T, bool VECTORS> __device__ __forceinline__ void store8(T* p, int n, const float* x) {
-    if (VECTORS) {
-        if (n > 0) Vec8<T>::store(p, x);
-        return;
+template <typename T, bool VECTORS> __device__ __forceinline__ void store4(T* p, int n, const float* x) {
+    if constexpr (!VECTORS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) put(p + j, x[j]);
+    } else if (n > 0) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+        } else {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+            *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const unsigned*>(&a), *reinterpret_cast<const unsigned*>(&b));
+        }
+    }
+}
+
+// N consecutive fp32 values, aligned to all of them (to 16 bytes at most), or zeros.
+template <int N> __device__ __forceinline__ void load_together(const float* p, bool there, float* x) {
+#pragma unroll
+    for (int i = 0; i < N; i += N < 4 ? N : 4) {
+        if constexpr (N == 1) {
+            x[i] = there ? __ldcg(p) : 0.f;
+        } else if constexpr (N == 2) {
+            const float2 v = there ? __ldcg(reinterpret_cast<const float2*>(p)) : make_float2(0.f, 0.f);
+            x[i] = v.x; x[i + 1] = v.y;
+        } else {
+            const float4 v = there ? __ldcg(reinterpret_cast<const float4*>(p + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
+        }
+    }
+}
+
+// The tf32 value next to x (11 bits), as the tensor core takes it.
+__device__ __forceinline__ unsigned high(float x) {
+    unsigned r;
+    asm("cvt.rna.tf32.f32 %0, %1;\n" : "=r"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ unsigned low(float x, unsigned hi) { return __float_as_uint(x - __uint_as_float(hi)); }
+
+__device__ __forceinline__ void mma(float* c, const unsigned* a, unsigned b0, unsigned b1) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Where value j of lane l's 16 bytes of block b of octet o's rows of x lies.
+template <typename T, int OCT> __device__ __forceinline__ int staged(int b, int o, int l, int j) {
+    return (((b * OCT + o) * (Lane<T>::kValues / 4) + j / 4) * 32 + l) * 4 + j % 4;
+}
+
+// Logits of 16 rows of w (from v0) and OCT x 8 rows of x (xs):
+// s[o][0..3] = rows g, g, g + 8, g + 8 and tokens 2 t, 2 t + 1, 2 t, 2 t + 1 of
+// octet o, lane = 4 g + t.
+template <typename T, int OCT, bool VECTORS>
+__device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, const float* xs, int lane, float (*s)[4]) {
+    constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal, kAhead = 4;   // blocks of depth under way
+    constexpr bool kExact = sizeof(T) == 2;
+    const int g = lane >> 2, t = lane & 3, blocks = (D + kBlock - 1) / kBlock;
+    const T* r0 = w + (size_t)(v0 + g) * D + t * kVal;
+    const T* r1 = r0 + (size_t)8 * D;
+    const bool in0 = v0 + g < V, in1 = v0 + g + 8 < V;
+    float small[OCT][4];
+#pragma unroll
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[o][j] = small[o][j] = 0.f;
+    uint4 n0[kAhead], n1[kAhead];                  // the next blocks, as they come
+    const auto fetch = [&](int b0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = (b0 + u) * kBlock, left = D - k - t * kVal;
+            n0[u] = fetch16<T, VECTORS>(r0 + k, in0 ? left : 0);
+            n1[u] = fetch16<T, VECTORS>(r1 + k, in1 ? left : 0);
+        }
+    };
+    fetch(0);
+    for (int b0 = 0; b0 < blocks; b0 += kAhead) {
+        float a0[kAhead][kVal], a1[kAhead][kVal];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            unfold<T>(n0[u], a0[u]);
+            unfold<T>(n1[u], a1[u]);
+        }
+        if (b0 + kAhead < blocks) fetch(b0 + kAhead);
+        float big[OCT][4];                         // 64 (fp32) or 128 (bf16) deep
+#pragma unroll
+        for (int o = 0; o < OCT; ++o)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) big[o][j] = 0.f;
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (b0 + u < blocks) {
+#pragma unroll
+                for (int q = 0; q < kVal / 4; ++q) {
+                    unsigned ah[2][4], al[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {  // two steps of eight: values 4 q + 2 h, 4 q + 2 h + 1
+                        const float e[4] = {a0[u][4 * q + 2 * h], a1[u][4 * q + 2 * h], a0[u][4 * q + 2 * h + 1],
+                                            a1[u][4 * q + 2 * h + 1]};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            ah[h][j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
+                            al[h][j] = kExact ? 0u : low(e[j], ah[h][j]);
+                        }
+                    }
+#pragma unroll
+                    for (int o = 0; o < OCT; ++o) {
+                        const float4 x = *reinterpret_cast<const float4*>(xs + staged<T, OCT>(b0 + u, o, lane, 4 * q));
+                        const float e[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const unsigned b0h = kExact ? __float_as_uint(e[2 * h]) : high(e[2 * h]);
+                            const unsigned b1h = kExact ? __float_as_uint(e[2 * h + 1]) : high(e[2 * h + 1]);
+                            if (!kExact) {
+                                mma(small[o], al[h], b0h, b1h);
+                                mma(small[o], ah[h], low(e[2 * h], b0h), low(e[2 * h + 1], b1h));
+                            }
+                            mma(big[o], ah[h], b0h, b1h);
+                        }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 0; o < OCT; ++o)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[o][j] += big[o][j];
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < n) put(p + j, x[j]);
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[o][j] += small[o][j];
 }
-__device__ __forceinline__ float dot8(const float* a, const float4& q0, const float4& q1, float s) {
-    s = fmaf(a[0], q0.x, s); s = fmaf(a[1], q0.y, s); s = fmaf(a[2], q0.z, s); s = fmaf(a[3], q0.w, s);
-    s = fmaf(a[4], q1.x, s); s = fmaf(a[5], q1.y, s); s = fmaf(a[6], q1.z, s); return fmaf(a[7], q1.w, s);
-}
-// Value j of thread t in an array of eight for each of 256 threads.
-__device__ __forceinline__ float& red_at(float* s, int t, int j) { return s[j * 32 * kWarps + t]; }
 
-template <typename T, int NT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts parts, int segments) {
-    extern __shared__ float xs[];                  // [NT][steps * 256]
-    __shared__ float red_m[kWarps][NT], red_l[kWarps][NT];
-    constexpr int kValues = NT * kGroup;           // logits of a group of rows of w, value n * kGroup + r
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int n0 = blockIdx.y * NT, steps = (p.D + 255) / 256;
-    grid_dependency_sync();
-    for (int i = threadIdx.x; i < NT * steps * 256; i += 32 * kWarps) {
-        const int n = i / (steps * 256), k = i % (steps * 256);
+// x's rows from n0 (8 OCT of them, zeros past N) into shared memory, as tile_logits reads them.
+template <typename T, int OCT> __device__ __forceinline__ void stage_x(const Problem& p, int n0, float* xs) {
+    constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal;
+    const int blocks = (p.D + kBlock - 1) / kBlock;
+    for (int i = threadIdx.x; i < OCT * 8 * blocks * kBlock; i += 32 * kWarps) {
+        const int n = i / (blocks * kBlock), k = i % (blocks * kBlock);
         const bool in = n0 + n < p.N && k < p.D;
-        xs[n * steps * 256 + (VECTORS ? staged(k) : k)] =
+        xs[staged<T, OCT>(k / kBlock, n / 8, (n % 8) * 4 + k % kBlock / kVal, k % kVal)] =
             in ? to_f(static_cast<const T*>(p.x)[(size_t)(n0 + n) * p.D + k]) : 0.f;
     }
-    // a lane keeps the statistics of the logits that the reduction leaves with it: row n0 + n, every kGroup-th column
-    const int own = lane / (32 / kValues), own_n = own / kGroup, own_r = own % kGroup;
-    const bool writes = lane % (32 / kValues) == 0;
-    const int target = n0 + own_n < p.N ? target_column(p, n0 + own_n) : kIgnored;
-    float m = -INFINITY, l = 0.f;
+}
+
+__device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
+    const float top = fmaxf(m, m2), ms = top == -INFINITY ? 0.f : top;
+    l = l * expf(m - ms) + l2 * expf(m2 - ms);
+    m = top;
+}
+
+// Block: a segment of w (for `groups` > 1 as many groups of 8 OCT rows of x, whose
+// blocks follow one another so that they read w together).  Statistics
+// [row][segment].
+template <typename T, int OCT, bool VECTORS>
+__global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts parts, int segments, int groups) {
+    extern __shared__ __align__(16) float xs[];
+    __shared__ float red[2][kWarps][8 * OCT];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int seg = blockIdx.x / groups, n0 = blockIdx.x % groups * 8 * OCT;
+    grid_dependency_sync();
+    stage_x<T, OCT>(p, n0, xs);
+    float m[OCT][2], l[OCT][2];
+    int target[OCT][2];
+#pragma unroll
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int n = n0 + 8 * o + 2 * t + j;
+            target[o][j] = n < p.N ? target_column(p, n) : kIgnored;
+            m[o][j] = -INFINITY;
+            l[o][j] = 0.f;
+        }
     __syncthreads();
-    const int worker = blockIdx.x * kWarps + warp, workers = gridDim.x * kWarps;
-    const int lo = (int)((long long)p.V * worker / workers), hi = (int)((long long)p.V * (worker + 1) / workers);
-    const T* w = static_cast<const T*>(p.w);
-    for (int v0 = lo; v0 < hi; v0 += kGroup) {
-        float s[kValues];
+    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * kWarps + warp, workers = segments * kWarps;
+    for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
+        float s[OCT][4];
+        tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
+        const int v = i * kTileRows + g;
 #pragma unroll
-        for (int i = 0; i < kValues; ++i) s[i] = 0.f;
-        if (VECTORS) {
-#pragma unroll 2
-            for (int st = 0; st < steps; ++st) {
-                const int k = st * 256 + lane * 8;
-                float a[kGroup][8];
+        for (int o = 0; o < OCT; ++o)
 #pragma unroll
-                for (int r = 0; r < kGroup; ++r) load8<T, true>(w + (size_t)(v0 + r) * p.D + k, v0 + r < hi ? p.D - k : 0, a[r]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float* q = xs + (n * steps + st) * 256 + lane * 4;
-                    const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
-#pragma unroll
-                    for (int r = 0; r < kGroup; ++r) s[n * kGroup + r] = dot8(a[r], q0, q1, s[n * kGroup + r]);
-                }
+            for (int j = 0; j < 2; ++j) {
+                if (v == target[o][j]) parts.target_logit[n0 + 8 * o + 2 * t + j] = s[o][j];
+                if (v + 8 == target[o][j]) parts.target_logit[n0 + 8 * o + 2 * t + j] = s[o][2 + j];
+                const float a = v < p.V ? s[o][j] : -INFINITY, b = v + 8 < p.V ? s[o][2 + j] : -INFINITY;
+                const float top = fmaxf(m[o][j], fmaxf(a, b)), ms = top == -INFINITY ? 0.f : top;
+                l[o][j] = l[o][j] * expf(m[o][j] - ms) + (expf(a - ms) + expf(b - ms));
+                m[o][j] = top;
             }
-        } else {
-#pragma unroll 2
-            for (int k = lane; k < p.D; k += 32) {
-                float a[kGroup];
+    }
 #pragma unroll
-                for (int r = 0; r < kGroup; ++r) a[r] = v0 + r < hi ? to_f(w[(size_t)(v0 + r) * p.D + k]) : 0.f;
+    for (int o = 0; o < OCT; ++o)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float q = xs[n * steps * 256 + k];
+        for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                    for (int r = 0; r < kGroup; ++r) s[n * kGroup + r] = fmaf(a[r], q, s[n * kGroup + r]);
-                }
+            for (int d = 4; d < 32; d *= 2)
+                merge(m[o][j], l[o][j], __shfl_xor_sync(0xffffffffu, m[o][j], d), __shfl_xor_sync(0xffffffffu, l[o][j], d));
+            if (g == 0) {
+                red[0][warp][8 * o + 2 * t + j] = m[o][j];
+                red[1][warp][8 * o + 2 * t + j] = l[o][j];
             }
         }
-        const float mine = sum_to_owner<kValues>(s, lane);
-        if (v0 + own_r < hi) {
-            if (v0 + own_r == target && writes) parts.target_logit[n0 + own_n] = mine;
-            const float top = fmaxf(m, mine), ms = top == -INFINITY ? 0.f : top;
-            l = l * expf(m - ms) + expf(mine - ms);
-            m = top;
-        }
-    }
-    // the kGroup owners of a row of x: neighbours of 32 / kValues lanes each
-#pragma unroll
-    for (int o = 32 / kValues; o < 32 / NT; o *= 2) {
-        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-        const float top = fmaxf(m, m2), ms = top == -INFINITY ? 0.f : top;
-        l = l * expf(m - ms) + l2 * expf(m2 - ms);
-        m = top;
-    }
-    if (writes && own_r == 0) {
-        red_m[warp][own_n] = m;
-        red_l[warp][own_n] = l;
-    }
     __syncthreads();
-    if (threadIdx.x < NT && n0 + (int)threadIdx.x < p.N) {
-        const int n = threadIdx.x;
+    if ((int)threadIdx.x < 8 * OCT && n0 + (int)threadIdx.x < p.N) {
         float top = -INFINITY, sum = 0.f;
-        for (int w8 = 0; w8 < kWarps; ++w8) top = fmaxf(top, red_m[w8][n]);
-        const float ms = top == -INFINITY ? 0.f : top;
-        for (int w8 = 0; w8 < kWarps; ++w8) sum += red_l[w8][n] * expf(red_m[w8][n] - ms);
-        parts.m[(size_t)(n0 + n) * segments + blockIdx.x] = top;
-        parts.l[(size_t)(n0 + n) * segments + blockIdx.x] = sum;
+#pragma unroll
+        for (int w8 = 0; w8 < kWarps; ++w8) merge(top, sum, red[0][w8][threadIdx.x], red[1][w8][threadIdx.x]);
+        parts.m[(size_t)(n0 + threadIdx.x) * segments + seg] = top;
+        parts.l[(size_t)(n0 + threadIdx.x) * segments + seg] = sum;
     }
+}
+
+// The same logits, as g[v][token] (row length `tokens`; zeros for tokens past N).
+template <typename T, int OCT, bool VECTORS>
+__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient,
+                                                                      int tokens, int groups) {
+    extern __shared__ __align__(16) float xs[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int seg = blockIdx.x / groups, n0 = blockIdx.x % groups * 8 * OCT;
+    grid_dependency_sync();
+    stage_x<T, OCT>(p, n0, xs);
+    int target[OCT][2];
+    float z[OCT][2], dl[OCT][2];
+#pragma unroll
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int n = n0 + 8 * o + 2 * t + j;
+            target[o][j] = n < p.N ? target_column(p, n) : kIgnored;
+            z[o][j] = target[o][j] >= 0 ? lse[n] : 0.f;
+            dl[o][j] = target[o][j] >= 0 ? dloss[n] : 0.f;
+            if (target[o][j] == kBad && seg == 0 && warp == 0 && g == 0) raise_status(p.status, kStatusTarget);
+        }
+    __syncthreads();
+    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * kWarps + warp, workers = gridDim.x / groups * kWarps;
+    for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
+        float s[OCT][4];
+        tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
+#pragma unroll
+        for (int o = 0; o < OCT; ++o)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int v = i * kTileRows + g + 8 * h;
+                float2 out;
+                float* e = &out.x;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    e[j] = target[o][j] < 0 ? 0.f : dl[o][j] * (expf(s[o][2 * h + j] - z[o][j]) - (v == target[o][j] ? 1.f : 0.f));
+                if (v < p.V) *reinterpret_cast<float2*>(gradient + (size_t)v * tokens + n0 + 8 * o + 2 * t) = out;
+            }
+    }
+}
+
+// dw[v] = sum_n g[v][n] x[n] and dx[n] = sum_v g[v][n] w[v].  A warp takes 32
+// columns (lane 4 g' + t' ... four consecutive columns 4 g .. 4 g + 3, as rows g and
+// g + 8 of two 16-row operands) of a range of rows of w, sixteen at a time:
+//   dx^T (columns x tokens) += w^T (columns x 8 rows of w) g (8 rows x tokens)
+//   dw^T (columns x 8 rows of w) = x^T (columns x tokens) g^T (tokens x 8 rows)
+// In the first, token 4-or-fewer g + o is column g of octet o; in the second,
+// tokens 2 OCT t + 2 o and + 1 are depth t and t + 4 of octet o.
+// parts[range][n][D]: dx over the range.
+template <typename T, int OCT, bool VECTORS>
+__global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int ranges) {
+    constexpr bool kExact = sizeof(T) == 2;
+    constexpr int kTokens = 8 * OCT;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int unit = blockIdx.x * kWarps + (threadIdx.x >> 5), column_groups = (p.D + 31) / 32;
+    grid_dependency_sync();
+    if (unit >= column_groups * ranges) return;
+    // neighbouring warps: the column groups of the same rows
+    const int c = unit % column_groups * 32 + 4 * g, range = unit / column_groups;
+    const int left = p.D - c;
+    float x[OCT][2][4];
+#pragma unroll
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = 2 * OCT * t + 2 * o + h;
+            load4<T, VECTORS>(static_cast<const T*>(p.x) + (size_t)n * p.D + c, n < p.N ? left : 0, x[o][h]);
+        }
+    float dx[2][OCT][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int o = 0; o < OCT; ++o)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dx[i][o][j] = 0.f;
+    const T* w = static_cast<const T*>(p.w);
+    const int tiles = (p.V + kTileRows - 1) / kTileRows;
+    const int lo = (int)((long long)tiles * range / ranges), hi = (int)((long long)tiles * (range + 1) / ranges);
+    float next[4][4];                              // the next tile's rows of w
+    const auto fetch = [&](int v0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {              // rows v0 + 4 u + t
+            const int v = v0 + 4 * u + t;
+            load4<T, VECTORS>(w + (size_t)v * p.D + c, v < p.V ? left : 0, next[u]);
+        }
+    };
+    if (lo < hi) fetch(lo * kTileRows);
+    for (int i0 = lo; i0 < hi; ++i0) {
+        const int v0 = i0 * kTileRows;
+        float a[4][4], gv[4][OCT], gt[2][2 * OCT];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[u][j] = next[u][j];
+        if (i0 + 1 < hi) fetch(v0 + kTileRows);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int v = v0 + 4 * u + t;
+            const float* q = gradient + (size_t)v * kTokens + OCT * g;
+            load_together<OCT>(q, v < p.V, gv[u]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {              // row v0 + 8 h + g, this lane's tokens
+            const int v = v0 + 8 * h + g;
+            const float* q = gradient + (size_t)v * kTokens + 2 * OCT * t;
+            load_together<2 * OCT>(q, v < p.V, gt[h]);
+        }
+        if (parts) {
+            float sum[2][OCT][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int o = 0; o < OCT; ++o)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[i][o][j] = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {          // eight rows of w: 4 u + t with u = 2 h, 2 h + 1
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float e[4] = {a[2 * h][2 * i], a[2 * h][2 * i + 1], a[2 * h + 1][2 * i], a[2 * h + 1][2 * i + 1]};
+                    unsigned ah[4], al[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        ah[j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
+                        al[j] = kExact ? 0u : low(e[j], ah[j]);
+                    }
+#pragma unroll
+                    for (int o = 0; o < OCT; ++o) {
+                        const unsigned b0 = high(gv[2 * h][o]), b1 = high(gv[2 * h + 1][o]);
+                        mma(sum[i][o], ah, low(gv[2 * h][o], b0), low(gv[2 * h + 1][o], b1));
+                        if (!kExact) mma(sum[i][o], al, b0, b1);
+                        mma(sum[i][o], ah, b0, b1);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int o = 0; o < OCT; ++o)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) dx[i][o][j] += sum[i][o][j];
+        }
+        if (dw) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {          // rows v0 + 8 h ..
+                float out[2][4];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) out[i][j] = 0.f;
+#pragma unroll
+                    for (int o = 0; o < OCT; ++o) {
+                        const float e[4] = {x[o][0][2 * i], x[o][0][2 * i + 1], x[o][1][2 * i], x[o][1][2 * i + 1]};
+                        unsigned ah[4], al[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            ah[j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
+                            al[j] = kExact ? 0u : low(e[j], ah[j]);
+                        }
+                        const unsigned b0 = high(gt[h][2 * o]), b1 = high(gt[h][2 * o + 1]);
+                        mma(out[i], ah, low(gt[h][2 * o], b0), low(gt[h][2 * o + 1], b1));
+                        if (!kExact) mma(out[i], al, b0, b1);
+                        mma(out[i], ah, b0, b1);
+                    }
+                }
+                // columns 4 g .. 4 g + 3 of rows 2 t and 2 t + 1
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int v = v0 + 8 * h + 2 * t + j;
+                    const float r[4] = {out[0][j], out[0][2 + j], out[1][j], out[1][2 + j]};
+                    if (v < p.V) store4<T, VECTORS>(dw + (size_t)v * p.D + c, left, r);
+                }
+            }
+        }
+    }
+    if (!parts) return;
+    // dx^T: columns 4 g + 2 i, 4 g + 2 i + 1; tokens OCT (2 t + j) + o
+#pragma unroll
+    for (int o = 0; o < OCT; ++o)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int n = OCT * (2 * t + j) + o;
+            const float r[4] = {dx[0][o][j], dx[0][o][2 + j], dx[1][o][j], dx[1][o][2 + j]};
+            if (n < p.N) store4<float, VECTORS>(parts + ((size_t)range * p.N + n) * p.D + c, left, r);
+        }
 }
 
 __device__ __forceinline__ void finish_row(const Problem& p, const FwdParts& parts, int n, float z, float* loss, float* lse) {
@@ -163,107 +484,9 @@ __device__ __forceinline__ void finish_row(const Problem& p, const FwdParts& par
     loss[n] = t == kIgnored ? 0.f : t == kBad ? NAN : z - parts.target_logit[n];
 }
 
-// The gradient of few rows in one pass over w: a block forms the logits of a
-// batch of 32 rows of w as rows_kernel does, turns them into g in shared memory,
-// and then takes the batch again (from L1) with a thread for eight columns:
-//   dw[v] = sum_n g[n][v] x[n]   to memory,   dx[n] += g[n][v] w[v]   in registers.
-// parts[block][n][D]: dx over the block's rows of w.
-template <typename T, int NT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, T* dw, float* parts,
-                                                                    bool want_dx) {
-    extern __shared__ float xs[];                  // [NT][steps * 256], staged
-    constexpr int kValues = NT * kGroup, kBatch = kGroup * kWarps;
-    __shared__ float gs[kBatch][NT];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, steps = (p.D + 255) / 256;
-    grid_dependency_sync();
-    for (int i = threadIdx.x; i < NT * steps * 256; i += 32 * kWarps) {
-        const int n = i / (steps * 256), k = i % (steps * 256);
-        xs[n * steps * 256 + staged(k)] = n < p.N && k < p.D ? to_f(static_cast<const T*>(p.x)[(size_t)n * p.D + k]) : 0.f;
-    }
-    const int own = lane / (32 / kValues), own_n = own / kGroup, own_r = own % kGroup;
-    const bool writes = lane % (32 / kValues) == 0;
-    const int target = own_n < p.N ? target_column(p, own_n) : kIgnored;
-    const float z = target >= 0 ? lse[own_n] : 0.f, dl = target >= 0 ? dloss[own_n] : 0.f;
-    if (target == kBad && blockIdx.x == 0 && writes && own_r == 0) raise_status(p.status, kStatusTarget);
-    // columns 8 cg .. of the rows rg, rg + groups, ... of a batch
-    const int column_groups = (p.D + 7) / 8, groups = 32 * kWarps / column_groups;
-    const int cg = threadIdx.x % column_groups, rg = threadIdx.x / column_groups;
-    const bool takes = rg < groups;
-    const int at = (cg >> 5) * 256 + (cg & 31) * 4;           // staged(8 cg)
-    float dx[NT][8];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) dx[n][j] = 0.f;
-    const int lo = (int)((long long)p.V * blockIdx.x / gridDim.x), hi = (int)((long long)p.V * (blockIdx.x + 1) / gridDim.x);
-    const T* w = static_cast<const T*>(p.w);
-    for (int b0 = lo; b0 < hi; b0 += kBatch) {
-        __syncthreads();                           // x is staged; the batch before has been read
-        const int v0 = b0 + warp * kGroup;
-        float s[kValues];
-#pragma unroll
-        for (int i = 0; i < kValues; ++i) s[i] = 0.f;
-        if (v0 < hi) {
-#pragma unroll 2
-            for (int st = 0; st < steps; ++st) {
-                const int k = st * 256 + lane * 8;
-                float a[kGroup][8];
-#pragma unroll
-                for (int r = 0; r < kGroup; ++r) load8<T, VECTORS>(w + (size_t)(v0 + r) * p.D + k, v0 + r < hi ? p.D - k : 0, a[r]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float* q = xs + (n * steps + st) * 256 + lane * 4;
-                    const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
-#pragma unroll
-                    for (int r = 0; r < kGroup; ++r) s[n * kGroup + r] = dot8(a[r], q0, q1, s[n * kGroup + r]);
-                }
-            }
-        }
-        const float mine = sum_to_owner<kValues>(s, lane);
-        if (writes) gs[warp * kGroup + own_r][own_n] = target < 0 ? 0.f : dl * (expf(mine - z) - (v0 + own_r == target ? 1.f : 0.f));
-        __syncthreads();
-        const int rows = min(kBatch, hi - b0);
-        if (takes) {
-            for (int r = rg; r < rows; r += groups) {
-                float a[8], o[8];
-                load8<T, VECTORS>(w + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, a);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = 0.f;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float g = gs[r][n];
-                    const float* q = xs + n * steps * 256 + at;
-                    const float4 q0 = *reinterpret_cast<const float4*>(q), q1 = *reinterpret_cast<const float4*>(q + 128);
-                    o[0] = fmaf(g, q0.x, o[0]); o[1] = fmaf(g, q0.y, o[1]); o[2] = fmaf(g, q0.z, o[2]); o[3] = fmaf(g, q0.w, o[3]);
-                    o[4] = fmaf(g, q1.x, o[4]); o[5] = fmaf(g, q1.y, o[5]); o[6] = fmaf(g, q1.z, o[6]); o[7] = fmaf(g, q1.w, o[7]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) dx[n][j] = fmaf(g, a[j], dx[n][j]);
-                }
-                if (dw) store8<T, VECTORS>(dw + (size_t)(b0 + r) * p.D + 8 * cg, p.D - 8 * cg, o);
-            }
-        }
-    }
-    if (!want_dx) return;
-    // the groups' sums of a column, one row of x at a time, over the space of x
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        __syncthreads();
-        if (takes)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) red_at(xs, rg * column_groups + cg, j) = dx[n][j];
-        __syncthreads();
-        for (int o = threadIdx.x; n < p.N && o < 8 * column_groups; o += 32 * kWarps) {
-            const int c = o % column_groups, j = o / column_groups;
-            float sum = 0.f;
-            for (int i = 0; i < groups; ++i) sum += red_at(xs, i * column_groups + c, j);
-            if (8 * c + j < p.D) parts[((size_t)blockIdx.x * p.N + n) * p.D + 8 * c + j] = sum;
-        }
-    }
-}
-
-// dx[n][c] = sum over the blocks of parts[block][n][c]: 32 columns to a block of
+// dx[n][c] = sum over the ranges of parts[range][n][c]: 32 columns to a block of
 // 256 threads, every eighth part to a thread.
-template <typename T> __global__ void __launch_bounds__(256) join_dx_kernel(const float* parts, int blocks, long long values, T* dx) {
+template <typename T> __global__ void __launch_bounds__(256) join_dx_kernel(const float* parts, int ranges, long long values, T* dx) {
     __shared__ float red[8][32];
     grid_dependency_sync();
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
@@ -271,7 +494,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_dx_kernel(cons
     float s = 0.f;
     if (i < values) {
 #pragma unroll 8
-        for (int b = part; b < blocks; b += 8) s += parts[b * values + i];
+        for (int b = part; b < ranges; b += 8) s += parts[b * values + i];
     }
     red[part][lane] = s;
     __syncthreads();
@@ -279,7 +502,7 @@ template <typename T> __global__ void __launch_bounds__(256) join_dx_kernel(cons
         s = 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k) s += red[k][lane];
-        store8<T, false>(dx + i, 1, &s);
+        put(dx + i, s);
     }
 }
 
@@ -349,80 +572,112 @@ __global__ void __launch_bounds__(256) join_rows_kernel(Problem p, FwdParts part
     }
 }
 
-template <typename T, int NT> cudaError_t launch_rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
-    const size_t smem = (size_t)NT * ((p.D + 255) / 256) * 256 * 4;
-    const dim3 grid(segments, (p.N + NT - 1) / NT);
-    if (p.D % (16 / sizeof(T)) == 0 && p.D % 8 == 0)
-        return launch_kernel(rows_kernel<T, NT, true>, grid, dim3(32 * kWarps), smem, st, p, parts, segments);
-    return launch_kernel(rows_kernel<T, NT, false>, grid, dim3(32 * kWarps), smem, st, p, parts, segments);
+constexpr size_t kMostSmem = 200 * 1024;
+
+template <typename K> cudaError_t allow_smem(K kern) {
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
 }
 
-// Rows of x that a block takes: as many as there are, up to eight, and as fit
-// 47 KB of shared memory (the forward reads w again, from L2, for each further group).
-int rows_at_once(int N, int D) {
-    int nt = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
-    while (nt > 1 && nt * ((D + 255) / 256) > 47) nt /= 2;
-    return nt;
+size_t smem_of(int oct, int D) { return (size_t)oct * 8 * ((D + 31) / 32 * 32) * 4; }
+
+// Octets of rows of x: 1, 2 or 4, as many as there are; and how many of them fit a
+// block's shared memory at a time (0: not one).
+int octets(int N) { return N <= 8 ? 1 : N <= 16 ? 2 : 4; }
+int octets_at_once(int N, int D) {
+    int oct = octets(N);
+    while (oct > 0 && smem_of(oct, D) > kMostSmem) oct /= 2;
+    return oct;
 }
 
-template <typename T> cudaError_t rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
-    switch (rows_at_once(p.N, p.D)) {
-    case 1: return launch_rows<T, 1>(p, parts, segments, st);
-    case 2: return launch_rows<T, 2>(p, parts, segments, st);
-    case 4: return launch_rows<T, 4>(p, parts, segments, st);
-    default: return launch_rows<T, 8>(p, parts, segments, st);
+template <typename T, int OCT, bool VECTORS>
+cudaError_t launch_rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
+    const cudaError_t e = allow_smem(rows_kernel<T, OCT, VECTORS>);
+    if (e != cudaSuccess) return e;
+    const int groups = octets(p.N) / OCT;
+    return launch_kernel(rows_kernel<T, OCT, VECTORS>, dim3((unsigned)(segments * groups)), dim3(32 * kWarps), smem_of(OCT, p.D), st,
+                         p, parts, segments, groups);
+}
+template <typename T, bool VECTORS>
+cudaError_t rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
+    switch (octets_at_once(p.N, p.D)) {
+    case 1: return launch_rows<T, 1, VECTORS>(p, parts, segments, st);
+    case 2: return launch_rows<T, 2, VECTORS>(p, parts, segments, st);
+    default: return launch_rows<T, 4, VECTORS>(p, parts, segments, st);
     }
 }
 
-template <typename T, int NT>
-cudaError_t launch_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dw, float* parts, bool want_dx,
-                                 int blocks, cudaStream_t st) {
-    // x, and later eight values of each of the block's threads
-    const size_t smem = std::max((size_t)NT * ((p.D + 255) / 256) * 256 * 4, (size_t)32 * kWarps * 8 * 4);
-    if (p.D % 8 == 0)
-        return launch_kernel(rows_gradient_kernel<T, NT, true>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
-                             static_cast<T*>(dw), parts, want_dx);
-    return launch_kernel(rows_gradient_kernel<T, NT, false>, dim3(blocks), dim3(32 * kWarps), smem, st, p, lse, dloss,
-                         static_cast<T*>(dw), parts, want_dx);
+template <typename T, int OCT, bool VECTORS>
+cudaError_t launch_gradient(const Problem& p, const float* lse, const float* dloss, float* gradient, cudaStream_t st) {
+    const cudaError_t e = allow_smem(rows_gradient_kernel<T, OCT, VECTORS>);
+    if (e != cudaSuccess) return e;
+    const int groups = octets(p.N) / OCT;
+    ProfScope s("xent_few_rows_grad", st);
+    return launch_kernel(rows_gradient_kernel<T, OCT, VECTORS>, dim3((unsigned)(few_rows_segments(p.V) * groups)), dim3(32 * kWarps),
+                         smem_of(OCT, p.D), st, p, lse, dloss, gradient, 8 * octets(p.N), groups);
 }
-template <typename T>
-cudaError_t rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts, int blocks,
-                          cudaStream_t st) {
-    cudaError_t e;
-    {
-        ProfScope s("xent_few_rows_grad", st);
-        switch (rows_at_once(p.N, p.D)) {
-        case 1: e = launch_rows_gradient<T, 1>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
-        case 2: e = launch_rows_gradient<T, 2>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
-        case 4: e = launch_rows_gradient<T, 4>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st); break;
-        default: e = launch_rows_gradient<T, 8>(p, lse, dloss, dw, parts, dx != nullptr, blocks, st);
-        }
-    }
-    if (e != cudaSuccess || !dx) return e;
-    ProfScope s("xent_join_dx", st);
-    const long long values = (long long)p.N * p.D;
-    return launch_kernel(join_dx_kernel<T>, dim3((unsigned)((values + 31) / 32)), dim3(256), 0, st, parts, blocks, values,
-                         static_cast<T*>(dx));
+template <typename T, int OCT, bool VECTORS>
+cudaError_t launch_products(const Problem& p, const float* gradient, T* dw, float* parts, int ranges, cudaStream_t st) {
+    const int units = (p.D + 31) / 32 * ranges;
+    ProfScope s("xent_few_rows_products", st);
+    return launch_kernel(rows_products_kernel<T, OCT, VECTORS>, dim3((unsigned)((units + kWarps - 1) / kWarps)), dim3(32 * kWarps), 0,
+                         st, p, gradient, dw, parts, ranges);
+}
+template <typename T, bool VECTORS>
+cudaError_t gradient_of(const Problem& p, const float* lse, const float* dloss, T* dx, T* dw, float* gradient, float* parts, int ranges,
+                        cudaStream_t st) {
+    const int once = octets_at_once(p.N, p.D);
+    cudaError_t e = once == 1   ? launch_gradient<T, 1, VECTORS>(p, lse, dloss, gradient, st)
+                    : once == 2 ? launch_gradient<T, 2, VECTORS>(p, lse, dloss, gradient, st)
+                                : launch_gradient<T, 4, VECTORS>(p, lse, dloss, gradient, st);
+    if (e != cudaSuccess) return e;
+    float* to = dx ? parts : nullptr;
+    const int oct = octets(p.N);
+    e = oct == 1   ? launch_products<T, 1, VECTORS>(p, gradient, dw, to, ranges, st)
+        : oct == 2 ? launch_products<T, 2, VECTORS>(p, gradient, dw, to, ranges, st)
+                   : launch_products<T, 4, VECTORS>(p, gradient, dw, to, ranges, st);
+    return e != cudaSuccess || !dx ? e : launch_join_dx(p, parts, ranges, dx, sizeof(T) == 2, st);
 }
 
 }  // namespace
 
-int few_rows_segments(int V) {
-    return std::max(1, std::min(152 * 4, (V + kGroup * kWarps - 1) / (kGroup * kWarps)));
+bool few_rows_applies(int N, int D) { return N <= 32 && octets_at_once(N, D) > 0; }
+
+int few_rows_tokens(int N) { return 8 * octets(N); }
+
+// Segments of w: two blocks of warps to an SM, a tile to a warp at least.
+int few_rows_segments(int V) { return std::max(1, std::min(152 * 2, (V + kTileRows * kWarps - 1) / (kTileRows * kWarps))); }
+
+// Ranges of rows of w in the products: as many blocks of warps as an SM holds over
+// all groups of 32 columns, a tile to a warp at least.
+int few_rows_ranges(int N, int D, int V, bool bf16) {
+    const int groups = (D + 31) / 32, resident = bf16 && N <= 8 ? 3 : 2;
+    return std::max(1, std::min(152 * resident * kWarps / groups, (V + kTileRows - 1) / kTileRows));
 }
 
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st) {
-    return bf16 ? rows<__nv_bfloat16>(p, parts, segments, st) : rows<float>(p, parts, segments, st);
+    if (bf16) return p.D % 8 == 0 ? rows<__nv_bfloat16, true>(p, parts, segments, st) : rows<__nv_bfloat16, false>(p, parts, segments, st);
+    return p.D % 4 == 0 ? rows<float, true>(p, parts, segments, st) : rows<float, false>(p, parts, segments, st);
 }
 
-int few_rows_at_most(int N, int D) { return D <= 2048 ? rows_at_once(N, D) : 0; }
+cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* gradient,
+                                     float* parts, int ranges, bool bf16, cudaStream_t st) {
+    if (bf16) {
+        auto *x = static_cast<__nv_bfloat16*>(dx), *w = static_cast<__nv_bfloat16*>(dw);
+        return p.D % 8 == 0 ? gradient_of<__nv_bfloat16, true>(p, lse, dloss, x, w, gradient, parts, ranges, st)
+                            : gradient_of<__nv_bfloat16, false>(p, lse, dloss, x, w, gradient, parts, ranges, st);
+    }
+    auto *x = static_cast<float*>(dx), *w = static_cast<float*>(dw);
+    return p.D % 4 == 0 ? gradient_of<float, true>(p, lse, dloss, x, w, gradient, parts, ranges, st)
+                        : gradient_of<float, false>(p, lse, dloss, x, w, gradient, parts, ranges, st);
+}
 
-int few_rows_blocks(int V) { return std::max(1, std::min(152 * 2, (V + kGroup * kWarps - 1) / (kGroup * kWarps))); }
-
-cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* parts,
-                                     int blocks, bool bf16, cudaStream_t st) {
-    return bf16 ? rows_gradient<__nv_bfloat16>(p, lse, dloss, dx, dw, parts, blocks, st)
-                : rows_gradient<float>(p, lse, dloss, dx, dw, parts, blocks, st);
+cudaError_t launch_join_dx(const Problem& p, const float* parts, int ranges, void* dx, bool bf16, cudaStream_t st) {
+    ProfScope s("xent_join_dx", st);
+    const long long values = (long long)p.N * p.D;
+    const dim3 grid((unsigned)((values + 31) / 32));
+    return bf16 ? launch_kernel(join_dx_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, parts, ranges, values,
+                                static_cast<__nv_bfloat16*>(dx))
+                : launch_kernel(join_dx_kernel<float>, grid, dim3(256), 0, st, parts, ranges, values, static_cast<float*>(dx));
 }
 
 cudaError_t launch_join_segments(const Problem& p, const FwdParts& parts, int segments, float* loss, float* lse, cudaStream_t st) {

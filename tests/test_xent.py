@@ -81,7 +81,10 @@ def check(x, w, t, dl, tag=""):
 
 SIZES = [(1, 1, 1), (1, 64, 257), (3, 7, 5), (2, 512, 4096), (100, 64, 257), (129, 100, 1000), (257, 72, 513),
          (256, 64, 256), (255, 128, 255), (1001, 100, 5003), (300, 520, 20011), (64, 2048, 3001), (513, 1030, 700),
-         (1024, 512, 2048), (7, 1536, 30000), (2049, 8, 31), (128, 333, 128)]
+         (1024, 512, 2048), (7, 1536, 30000), (2049, 8, 31), (128, 333, 128),
+         # one to four rows, few rows, tiles: each border, odd widths, a vocabulary that ends inside a tile
+         (4, 2048, 501), (4, 2056, 501), (5, 33, 17), (8, 136, 4099), (9, 512, 1003), (16, 1000, 2001), (17, 130, 999),
+         (32, 260, 1234), (33, 260, 1234), (32, 1604, 300), (16, 3205, 70), (8, 6404, 40), (31, 3, 1025)]
 
 
 @pytest.mark.gpu
