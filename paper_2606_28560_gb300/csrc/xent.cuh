@@ -52,7 +52,7 @@ cudaError_t launch_stream_gradient(const Problem& p, const float* lse, const flo
 // [ranges][N][D]; all fp32.
 bool few_rows_applies(int N, int D);
 int few_rows_tokens(int N);                        // N rounded up to 8, 16 or 32
-int few_rows_segments(int V);
+int few_rows_segments(int N, int D, int V);
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);
 int few_rows_ranges(int N, int D, int V, bool bf16);
 cudaError_t launch_few_rows_gradient(const Problem& p, const float* lse, const float* dloss, void* dx, void* dw, float* gradient,

@@ -927,7 +927,7 @@ FwdPlan plan_forward(int N, int D, int V, bool bf16) {
     if (f.way == Way::kStream) {
         f.segments = stream_segments(V);
     } else if (f.way == Way::kFewRows) {
-        f.segments = few_rows_segments(V);
+        f.segments = few_rows_segments(N, D, V);
     } else {
         plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
         f.wide = several_planes(N, D, V, bf16);

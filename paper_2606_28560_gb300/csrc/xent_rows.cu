@@ -8,8 +8,13 @@
 // in shared memory.  fp32 values go as two tf32 values, x = hi + lo, three products
 // of the four (the fourth is below 2^-22); bf16 values are exact.  The large
 // products are summed 64 deep before they are added in fp32, because the tensor
-// core truncates.  Bound by memory up to some 16 rows, by the tensor rate
-// (150 T multiplications a second, a third of it in fp32) beyond.
+// core truncates.
+//
+// Bound by memory in bf16 and up to 16 rows in fp32: 16 x 2048 x 131072 in fp32 takes
+// 191 us forward (5.6 TB/s) and 631 backward (2 x 1.07 GB read, 1.07 written).
+// With 32 rows, 354 and 1003, it is halfway between memory (159 and 476) and the
+// tensor rate (150 T multiplications a second, three for one in fp32): what is
+// issued beside them, the splitting in two and the loads of x, is the rest.
 //
 // A sum does not care for the order of its terms, so lanes take them as memory
 // gives them: in the logits a lane's depth values are consecutive; in the
@@ -96,23 +101,21 @@ template <int N> __device__ __forceinline__ void load_together(const float* p, b
 #pragma unroll
     for (int i = 0; i < N; i += N < 4 ? N : 4) {
         if constexpr (N == 1) {
-            x[i] = there ? __ldcg(p) : 0.f;
+            x[i] = there ? *p : 0.f;
         } else if constexpr (N == 2) {
-            const float2 v = there ? __ldcg(reinterpret_cast<const float2*>(p)) : make_float2(0.f, 0.f);
+            const float2 v = there ? *reinterpret_cast<const float2*>(p) : make_float2(0.f, 0.f);
             x[i] = v.x; x[i + 1] = v.y;
         } else {
-            const float4 v = there ? __ldcg(reinterpret_cast<const float4*>(p + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float4 v = there ? *reinterpret_cast<const float4*>(p + i) : make_float4(0.f, 0.f, 0.f, 0.f);
             x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
         }
     }
 }
 
-// The tf32 value next to x (11 bits), as the tensor core takes it.
-__device__ __forceinline__ unsigned high(float x) {
-    unsigned r;
-    asm("cvt.rna.tf32.f32 %0, %1;\n" : "=r"(r) : "f"(x));
-    return r;
-}
+// The tf32 value (11 bits) next to x, ties away from zero, with integer operations:
+// conversion instructions go at an eighth of their rate, as many of them would take
+// as long as the products.  Of a NaN whose payload overflows here, low() is a NaN.
+__device__ __forceinline__ unsigned high(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
 __device__ __forceinline__ unsigned low(float x, unsigned hi) { return __float_as_uint(x - __uint_as_float(hi)); }
 
 __device__ __forceinline__ void mma(float* c, const unsigned* a, unsigned b0, unsigned b1) {
@@ -150,6 +153,12 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
             n0[u] = fetch16<T, VECTORS>(r0 + k, in0 ? left : 0);
             n1[u] = fetch16<T, VECTORS>(r1 + k, in1 ? left : 0);
         }
+        // into L2: what comes 2 steps later, of the next tile too
+        constexpr int kStep = kAhead * kBlock;
+        const int depth = (blocks + kAhead - 1) / kAhead * kStep;
+        int k = b0 * kBlock + 2 * kStep + (lane >> 4) * (kStep / 2), v = v0 + (lane & 15);
+        if (k >= depth) { k -= depth; v += kTileRows; }
+        if (k < D && v < V) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(w + (size_t)v * D + k));
     };
     fetch(0);
     for (int b0 = 0; b0 < blocks; b0 += kAhead) {
@@ -210,15 +219,30 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
         for (int j = 0; j < 4; ++j) s[o][j] += small[o][j];
 }
 
-// x's rows from n0 (8 OCT of them, zeros past N) into shared memory, as tile_logits reads them.
-template <typename T, int OCT> __device__ __forceinline__ void stage_x(const Problem& p, int n0, float* xs) {
-    constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal;
-    const int blocks = (p.D + kBlock - 1) / kBlock;
-    for (int i = threadIdx.x; i < OCT * 8 * blocks * kBlock; i += 32 * kWarps) {
-        const int n = i / (blocks * kBlock), k = i % (blocks * kBlock);
-        const bool in = n0 + n < p.N && k < p.D;
-        xs[staged<T, OCT>(k / kBlock, n / 8, (n % 8) * 4 + k % kBlock / kVal, k % kVal)] =
-            in ? to_f(static_cast<const T*>(p.x)[(size_t)(n0 + n) * p.D + k]) : 0.f;
+// x's rows from n0 (8 OCT of them, zeros past N) into shared memory, as tile_logits
+// reads them, 16 bytes to a thread, eight of them under way.
+template <typename T, int OCT, bool VECTORS, int WARPS>
+__device__ __forceinline__ void stage_x(const Problem& p, int n0, float* xs) {
+    constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal, kAhead = 8;
+    const int pieces = (p.D + kBlock - 1) / kBlock * OCT * 32;
+    for (int i0 = threadIdx.x; i0 < pieces; i0 += kAhead * 32 * WARPS) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * 32 * WARPS, l = i & 31, n = n0 + i / 32 % OCT * 8 + l / 4, c = i / (32 * OCT) * kBlock + l % 4 * kVal;
+            u[k] = fetch16<T, VECTORS>(static_cast<const T*>(p.x) + (size_t)n * p.D + c, n < p.N ? p.D - c : 0);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int i = i0 + k * 32 * WARPS;
+            float e[kVal];
+            unfold<T>(u[k], e);
+#pragma unroll
+            for (int j = 0; j < kVal; j += 4)
+                if (i < pieces)
+                    *reinterpret_cast<float4*>(xs + staged<T, OCT>(i / (32 * OCT), i / 32 % OCT, i & 31, j)) =
+                        make_float4(e[j], e[j + 1], e[j + 2], e[j + 3]);
+        }
     }
 }
 
@@ -231,14 +255,14 @@ __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
 // Block: a segment of w (for `groups` > 1 as many groups of 8 OCT rows of x, whose
 // blocks follow one another so that they read w together).  Statistics
 // [row][segment].
-template <typename T, int OCT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts parts, int segments, int groups) {
+template <typename T, int OCT, bool VECTORS, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p, FwdParts parts, int segments, int groups) {
     extern __shared__ __align__(16) float xs[];
-    __shared__ float red[2][kWarps][8 * OCT];
+    __shared__ float red[2][WARPS][8 * OCT];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int seg = blockIdx.x / groups, n0 = blockIdx.x % groups * 8 * OCT;
     grid_dependency_sync();
-    stage_x<T, OCT>(p, n0, xs);
+    stage_x<T, OCT, VECTORS, WARPS>(p, n0, xs);
     float m[OCT][2], l[OCT][2];
     int target[OCT][2];
 #pragma unroll
@@ -251,7 +275,7 @@ __global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts p
             l[o][j] = 0.f;
         }
     __syncthreads();
-    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * kWarps + warp, workers = segments * kWarps;
+    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = segments * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
         tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
@@ -284,21 +308,21 @@ __global__ void __launch_bounds__(32 * kWarps) rows_kernel(Problem p, FwdParts p
     if ((int)threadIdx.x < 8 * OCT && n0 + (int)threadIdx.x < p.N) {
         float top = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w8 = 0; w8 < kWarps; ++w8) merge(top, sum, red[0][w8][threadIdx.x], red[1][w8][threadIdx.x]);
+        for (int i = 0; i < WARPS; ++i) merge(top, sum, red[0][i][threadIdx.x], red[1][i][threadIdx.x]);
         parts.m[(size_t)(n0 + threadIdx.x) * segments + seg] = top;
         parts.l[(size_t)(n0 + threadIdx.x) * segments + seg] = sum;
     }
 }
 
 // The same logits, as g[v][token] (row length `tokens`; zeros for tokens past N).
-template <typename T, int OCT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient,
+template <typename T, int OCT, bool VECTORS, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient,
                                                                       int tokens, int groups) {
     extern __shared__ __align__(16) float xs[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int seg = blockIdx.x / groups, n0 = blockIdx.x % groups * 8 * OCT;
     grid_dependency_sync();
-    stage_x<T, OCT>(p, n0, xs);
+    stage_x<T, OCT, VECTORS, WARPS>(p, n0, xs);
     int target[OCT][2];
     float z[OCT][2], dl[OCT][2];
 #pragma unroll
@@ -312,7 +336,7 @@ __global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, c
             if (target[o][j] == kBad && seg == 0 && warp == 0 && g == 0) raise_status(p.status, kStatusTarget);
         }
     __syncthreads();
-    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * kWarps + warp, workers = gridDim.x / groups * kWarps;
+    const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = gridDim.x / groups * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
         tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
@@ -332,15 +356,21 @@ __global__ void __launch_bounds__(32 * kWarps) rows_gradient_kernel(Problem p, c
 }
 
 // dw[v] = sum_n g[v][n] x[n] and dx[n] = sum_v g[v][n] w[v].  A warp takes 32
-// columns (lane 4 g' + t' ... four consecutive columns 4 g .. 4 g + 3, as rows g and
-// g + 8 of two 16-row operands) of a range of rows of w, sixteen at a time:
+// columns of a range of rows of w, sixteen rows at a time.  Lane 4 g + t has the
+// consecutive columns 4 g .. 4 g + 3: rows g and g + 8 of two operands of 16 rows.
 //   dx^T (columns x tokens) += w^T (columns x 8 rows of w) g (8 rows x tokens)
 //   dw^T (columns x 8 rows of w) = x^T (columns x tokens) g^T (tokens x 8 rows)
-// In the first, token 4-or-fewer g + o is column g of octet o; in the second,
+// In the first, token OCT g + o is column g of octet o; in the second,
 // tokens 2 OCT t + 2 o and + 1 are depth t and t + 4 of octet o.
 // parts[range][n][D]: dx over the range.
+//
+// Registers allow one to three blocks to an SM, too few loads under way for memory's
+// latency: the rows of w four tiles ahead are asked into L2, the next tile's g into
+// L1 (fp32, 32 x 2048 x 131072: 828 us without, 749 with the first, 664 with both).
+template <typename T> constexpr int resident(int oct) { return oct == 4 ? 1 : oct == 1 && sizeof(T) == 2 ? 3 : 2; }
+
 template <typename T, int OCT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int ranges) {
+__global__ void __launch_bounds__(32 * kWarps, resident<T>(OCT)) rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int ranges) {
     constexpr bool kExact = sizeof(T) == 2;
     constexpr int kTokens = 8 * OCT;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -368,6 +398,7 @@ __global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, c
     const T* w = static_cast<const T*>(p.w);
     const int tiles = (p.V + kTileRows - 1) / kTileRows;
     const int lo = (int)((long long)tiles * range / ranges), hi = (int)((long long)tiles * (range + 1) / ranges);
+    constexpr int kL2Ahead = 4;
     float next[4][4];                              // the next tile's rows of w
     const auto fetch = [&](int v0) {
 #pragma unroll
@@ -375,6 +406,10 @@ __global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, c
             const int v = v0 + 4 * u + t;
             load4<T, VECTORS>(w + (size_t)v * p.D + c, v < p.V ? left : 0, next[u]);
         }
+        const int v = v0 + kL2Ahead * kTileRows + (lane & 15);
+        if (lane < 16 && v < p.V) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(w + (size_t)v * p.D + (c - 4 * g)));
+        const int vg = v0 + kTileRows + (lane & 15);
+        if (lane < 16 && vg < p.V) asm volatile("prefetch.global.L1 [%0];\n" ::"l"(gradient + (size_t)vg * kTokens));
     };
     if (lo < hi) fetch(lo * kTileRows);
     for (int i0 = lo; i0 < hi; ++i0) {
@@ -398,19 +433,17 @@ __global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, c
             load_together<2 * OCT>(q, v < p.V, gt[h]);
         }
         if (parts) {
-            float sum[2][OCT][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i) {
+                float sum[OCT][4];
 #pragma unroll
                 for (int o = 0; o < OCT; ++o)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) sum[i][o][j] = 0.f;
+                    for (int j = 0; j < 4; ++j) sum[o][j] = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {          // eight rows of w: 4 u + t with u = 2 h, 2 h + 1
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int h = 0; h < 2; ++h) {      // eight rows of w: 4 u + t with u = 2 h, 2 h + 1
                     const float e[4] = {a[2 * h][2 * i], a[2 * h][2 * i + 1], a[2 * h + 1][2 * i], a[2 * h + 1][2 * i + 1]};
-                    unsigned ah[4], al[4];
+                    unsigned ah[4], al[4], bh[OCT][2];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         ah[j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
@@ -418,51 +451,67 @@ __global__ void __launch_bounds__(32 * kWarps) rows_products_kernel(Problem p, c
                     }
 #pragma unroll
                     for (int o = 0; o < OCT; ++o) {
-                        const unsigned b0 = high(gv[2 * h][o]), b1 = high(gv[2 * h + 1][o]);
-                        mma(sum[i][o], ah, low(gv[2 * h][o], b0), low(gv[2 * h + 1][o], b1));
-                        if (!kExact) mma(sum[i][o], al, b0, b1);
-                        mma(sum[i][o], ah, b0, b1);
+                        bh[o][0] = high(gv[2 * h][o]);
+                        bh[o][1] = high(gv[2 * h + 1][o]);
+                        mma(sum[o], ah, low(gv[2 * h][o], bh[o][0]), low(gv[2 * h + 1][o], bh[o][1]));
                     }
-                }
-            }
+                    if (!kExact) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+                        for (int o = 0; o < OCT; ++o) mma(sum[o], al, bh[o][0], bh[o][1]);
+                    }
+#pragma unroll
+                    for (int o = 0; o < OCT; ++o) mma(sum[o], ah, bh[o][0], bh[o][1]);
+                }
 #pragma unroll
                 for (int o = 0; o < OCT; ++o)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) dx[i][o][j] += sum[i][o][j];
+                    for (int j = 0; j < 4; ++j) dx[i][o][j] += sum[o][j];
+            }
         }
         if (dw) {
+            float out[2][2][4];                    // [rows v0 + 8 h ..][columns 2 i ..]
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {          // rows v0 + 8 h ..
-                float out[2][4];
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) out[i][j] = 0.f;
+                    for (int j = 0; j < 4; ++j) out[h][i][j] = 0.f;
 #pragma unroll
-                    for (int o = 0; o < OCT; ++o) {
-                        const float e[4] = {x[o][0][2 * i], x[o][0][2 * i + 1], x[o][1][2 * i], x[o][1][2 * i + 1]};
-                        unsigned ah[4], al[4];
+            for (int o = 0; o < OCT; ++o) {
+                unsigned ah[2][4], al[2][4], bh[2][2], bl[2][2];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            ah[j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
-                            al[j] = kExact ? 0u : low(e[j], ah[j]);
-                        }
-                        const unsigned b0 = high(gt[h][2 * o]), b1 = high(gt[h][2 * o + 1]);
-                        mma(out[i], ah, low(gt[h][2 * o], b0), low(gt[h][2 * o + 1], b1));
-                        if (!kExact) mma(out[i], al, b0, b1);
-                        mma(out[i], ah, b0, b1);
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float e = x[o][j / 2][2 * i + j % 2];
+                        ah[i][j] = kExact ? __float_as_uint(e) : high(e);
+                        al[i][j] = kExact ? 0u : low(e, ah[i][j]);
                     }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        bh[h][j] = high(gt[h][2 * o + j]);
+                        bl[h][j] = low(gt[h][2 * o + j], bh[h][j]);
+                    }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma(out[k / 2][k % 2], ah[k % 2], bl[k / 2][0], bl[k / 2][1]);
+                if (!kExact) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma(out[k / 2][k % 2], al[k % 2], bh[k / 2][0], bh[k / 2][1]);
                 }
-                // columns 4 g .. 4 g + 3 of rows 2 t and 2 t + 1
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma(out[k / 2][k % 2], ah[k % 2], bh[k / 2][0], bh[k / 2][1]);
+            }
+            // columns 4 g .. 4 g + 3 of rows 2 t and 2 t + 1
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int v = v0 + 8 * h + 2 * t + j;
-                    const float r[4] = {out[0][j], out[0][2 + j], out[1][j], out[1][2 + j]};
+                    const float r[4] = {out[h][0][j], out[h][0][2 + j], out[h][1][j], out[h][1][2 + j]};
                     if (v < p.V) store4<T, VECTORS>(dw + (size_t)v * p.D + c, left, r);
                 }
-            }
         }
     }
     if (!parts) return;
@@ -584,36 +633,42 @@ size_t smem_of(int oct, int D) { return (size_t)oct * 8 * ((D + 31) / 32 * 32) *
 // block's shared memory at a time (0: not one).
 int octets(int N) { return N <= 8 ? 1 : N <= 16 ? 2 : 4; }
 int octets_at_once(int N, int D) {
-    int oct = octets(N);
+    int oct = std::min(2, octets(N));
     while (oct > 0 && smem_of(oct, D) > kMostSmem) oct /= 2;
     return oct;
 }
 
-template <typename T, int OCT, bool VECTORS>
+// Two octets: blocks of eight warps while two of them fit an SM, else one of
+// sixteen.
+bool sixteen_warps(int D) { return smem_of(2, D) > kMostSmem / 2; }
+
+template <typename T, int OCT, bool VECTORS, int WARPS>
 cudaError_t launch_rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
-    const cudaError_t e = allow_smem(rows_kernel<T, OCT, VECTORS>);
+    const auto kern = rows_kernel<T, OCT, VECTORS, WARPS>;
+    const cudaError_t e = allow_smem(kern);
     if (e != cudaSuccess) return e;
     const int groups = octets(p.N) / OCT;
-    return launch_kernel(rows_kernel<T, OCT, VECTORS>, dim3((unsigned)(segments * groups)), dim3(32 * kWarps), smem_of(OCT, p.D), st,
-                         p, parts, segments, groups);
+    return launch_kernel(kern, dim3((unsigned)(segments * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p, parts, segments, groups);
 }
 template <typename T, bool VECTORS>
 cudaError_t rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
     switch (octets_at_once(p.N, p.D)) {
-    case 1: return launch_rows<T, 1, VECTORS>(p, parts, segments, st);
-    case 2: return launch_rows<T, 2, VECTORS>(p, parts, segments, st);
-    default: return launch_rows<T, 4, VECTORS>(p, parts, segments, st);
+    case 1: return launch_rows<T, 1, VECTORS, kWarps>(p, parts, segments, st);
+    default:
+        return sixteen_warps(p.D) ? launch_rows<T, 2, VECTORS, 16>(p, parts, segments, st)
+                                  : launch_rows<T, 2, VECTORS, kWarps>(p, parts, segments, st);
     }
 }
 
-template <typename T, int OCT, bool VECTORS>
+template <typename T, int OCT, bool VECTORS, int WARPS>
 cudaError_t launch_gradient(const Problem& p, const float* lse, const float* dloss, float* gradient, cudaStream_t st) {
-    const cudaError_t e = allow_smem(rows_gradient_kernel<T, OCT, VECTORS>);
+    const auto kern = rows_gradient_kernel<T, OCT, VECTORS, WARPS>;
+    const cudaError_t e = allow_smem(kern);
     if (e != cudaSuccess) return e;
     const int groups = octets(p.N) / OCT;
     ProfScope s("xent_few_rows_grad", st);
-    return launch_kernel(rows_gradient_kernel<T, OCT, VECTORS>, dim3((unsigned)(few_rows_segments(p.V) * groups)), dim3(32 * kWarps),
-                         smem_of(OCT, p.D), st, p, lse, dloss, gradient, 8 * octets(p.N), groups);
+    return launch_kernel(kern, dim3((unsigned)(few_rows_segments(p.N, p.D, p.V) * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p, lse, dloss,
+                         gradient, 8 * octets(p.N), groups);
 }
 template <typename T, int OCT, bool VECTORS>
 cudaError_t launch_products(const Problem& p, const float* gradient, T* dw, float* parts, int ranges, cudaStream_t st) {
@@ -626,9 +681,9 @@ template <typename T, bool VECTORS>
 cudaError_t gradient_of(const Problem& p, const float* lse, const float* dloss, T* dx, T* dw, float* gradient, float* parts, int ranges,
                         cudaStream_t st) {
     const int once = octets_at_once(p.N, p.D);
-    cudaError_t e = once == 1   ? launch_gradient<T, 1, VECTORS>(p, lse, dloss, gradient, st)
-                    : once == 2 ? launch_gradient<T, 2, VECTORS>(p, lse, dloss, gradient, st)
-                                : launch_gradient<T, 4, VECTORS>(p, lse, dloss, gradient, st);
+    cudaError_t e = once == 1              ? launch_gradient<T, 1, VECTORS, kWarps>(p, lse, dloss, gradient, st)
+                    : sixteen_warps(p.D) ? launch_gradient<T, 2, VECTORS, 16>(p, lse, dloss, gradient, st)
+                                         : launch_gradient<T, 2, VECTORS, kWarps>(p, lse, dloss, gradient, st);
     if (e != cudaSuccess) return e;
     float* to = dx ? parts : nullptr;
     const int oct = octets(p.N);
@@ -644,14 +699,20 @@ bool few_rows_applies(int N, int D) { return N <= 32 && octets_at_once(N, D) > 0
 
 int few_rows_tokens(int N) { return 8 * octets(N); }
 
-// Segments of w: two blocks of warps to an SM, a tile to a warp at least.
-int few_rows_segments(int V) { return std::max(1, std::min(152 * 2, (V + kTileRows * kWarps - 1) / (kTileRows * kWarps))); }
+// Segments of w: as many as fill the SMs once over the groups of rows of x (more
+// would only stage x more often), and no more than leave a block tiles 1024 deep in
+// all (a small w is spread over the SMs before it is over warps), eight at most.
+int few_rows_segments(int N, int D, int V) {
+    const int once = octets_at_once(N, D), groups = octets(N) / once, blocks = once == 2 && sixteen_warps(D) ? 152 : 2 * 152;
+    const int rows = kTileRows * std::max(1, std::min(8, 1024 / D));
+    return std::max(1, std::min(blocks / groups, (V + rows - 1) / rows));
+}
 
 // Ranges of rows of w in the products: as many blocks of warps as an SM holds over
 // all groups of 32 columns, a tile to a warp at least.
 int few_rows_ranges(int N, int D, int V, bool bf16) {
-    const int groups = (D + 31) / 32, resident = bf16 && N <= 8 ? 3 : 2;
-    return std::max(1, std::min(152 * resident * kWarps / groups, (V + kTileRows - 1) / kTileRows));
+    const int groups = (D + 31) / 32, oct = octets(N), blocks = bf16 ? resident<__nv_bfloat16>(oct) : resident<float>(oct);
+    return std::max(1, std::min(152 * blocks * kWarps / groups, (V + kTileRows - 1) / kTileRows));
 }
 
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st) {
