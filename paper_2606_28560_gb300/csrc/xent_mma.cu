@@ -906,18 +906,24 @@ static bool several_planes(int N, int D, int V, bool bf16) {
 }
 
 // Forward and backward go the same way: p = exp(logit - lse) is good to the
-// logits' own rounding only if both come from the same arithmetic.  Forward and
-// backward together, us on the GPU, stream / few rows / tiles:
-//   512 wide, 32768 columns: bf16 35 / 48 / 67 (one row), 80 / 48 / 67 (eight),
-//                            - / 62 / 67 (sixteen), - / 109 / 65 (thirty-two)
-//                            fp32 58 / 79 / 211 (one row), 93 / 81 / 205 (eight),
-//                            - / 177 / 203 (thirty-two)
-//   2048 wide, 131072 columns: bf16 395 / 530 / 498 (one row), - / 770 / 500 (sixteen)
-//                            fp32 746 / 850 / 2640 (one row), - / 1290 / 2660 (sixteen)
-//   64 wide, 257 columns:    bf16 9 / 12 / 27 (one row), - / 18 / 30 (thirty-two)
+// logits' own rounding only if both come from the same arithmetic.  Of the three a
+// call takes the one that is faster.  Forward and backward together, us on the GPU,
+// few rows / tiles:
+//                              bf16: 8 rows     16 rows     32 rows    fp32: 32 rows
+//   512 wide, 32768 columns:       44 / 67     54 / 67     83 / 62       118 / 203
+//   1000 wide, 20000 columns:      52 / 67     64 / 67    102 / 64       153 / 270
+//   2048 wide, 131072 columns:   455 / 496   552 / 498   954 / 502     1357 / 2660
+//   512 wide, 4000 columns:        21 / 31     25 / 31     28 / 30        38 / 75
+// and stream / few rows:
+//                              bf16: 1 row      2 rows      4 rows     fp32: 4 rows
+//   512 wide, 32768 columns:       33 / 43     38 / 43     48 / 43        67 / 64
+//   1000 wide, 20000 columns:      42 / 51     50 / 51     65 / 51        91 / 78
+//   2048 wide, 131072 columns:   372 / 455   425 / 457   517 / 459      802 / 801
+//   512 wide, 4000 columns:        13 / 21     14 / 21     17 / 21        18 / 25
 static Way way_of(int N, int D, int V, bool bf16) {
-    if (stream_applies(N, D)) return Way::kStream;
-    const int most = !bf16 || (long long)V * D <= (1 << 20) ? 32 : D <= 512 ? 16 : 0;
+    const bool small = (long long)V * D <= (1 << 22);
+    if (stream_applies(N, D) && (N <= 2 || small)) return Way::kStream;
+    const int most = !bf16 || small ? 32 : D <= 1024 ? 16 : 8;
     return N <= most && few_rows_applies(N, D) ? Way::kFewRows : Way::kTiles;
 }
 

@@ -1,4 +1,4 @@
-// xent_rows.cu -- the cross entropy for five to 32 rows (a small batch over a large
+// xent_rows.cu -- the cross entropy for three to 32 rows (a small batch over a large
 // head), and the joins of per-row statistics and of dx's parts.
 //
 // With few rows the work is w read once per pass, and fp32 cannot afford to be
@@ -316,8 +316,8 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p,
 
 // The same logits, as g[v][token] (row length `tokens`; zeros for tokens past N).
 template <typename T, int OCT, bool VECTORS, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient,
-                                                                      int tokens, int groups) {
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
+rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient, int tokens, int groups) {
     extern __shared__ __align__(16) float xs[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int seg = blockIdx.x / groups, n0 = blockIdx.x % groups * 8 * OCT;
@@ -370,7 +370,8 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_gradient_kernel(P
 template <typename T> constexpr int resident(int oct) { return oct == 4 ? 1 : oct == 1 && sizeof(T) == 2 ? 3 : 2; }
 
 template <typename T, int OCT, bool VECTORS>
-__global__ void __launch_bounds__(32 * kWarps, resident<T>(OCT)) rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int ranges) {
+__global__ void __launch_bounds__(32 * kWarps, resident<T>(OCT))
+rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int ranges) {
     constexpr bool kExact = sizeof(T) == 2;
     constexpr int kTokens = 8 * OCT;
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -667,8 +668,8 @@ cudaError_t launch_gradient(const Problem& p, const float* lse, const float* dlo
     if (e != cudaSuccess) return e;
     const int groups = octets(p.N) / OCT;
     ProfScope s("xent_few_rows_grad", st);
-    return launch_kernel(kern, dim3((unsigned)(few_rows_segments(p.N, p.D, p.V) * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p, lse, dloss,
-                         gradient, 8 * octets(p.N), groups);
+    return launch_kernel(kern, dim3((unsigned)(few_rows_segments(p.N, p.D, p.V) * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p,
+                         lse, dloss, gradient, 8 * octets(p.N), groups);
 }
 template <typename T, int OCT, bool VECTORS>
 cudaError_t launch_products(const Problem& p, const float* gradient, T* dw, float* parts, int ranges, cudaStream_t st) {

@@ -94,6 +94,33 @@ def test_matches_definition(size, dtype):
     check(*make(*size, TYPES[dtype], seed=sum(size)))
 
 
+# two, eight, sixteen and 32 rows on both sides of 2^22 weights, rows of x that fill a
+# block's shared memory, small heads that are spread over the processors
+HEADS = [(2, 300, 20011), (3, 512, 9000), (4, 512, 9000), (8, 1032, 5001), (9, 1032, 5001), (16, 1024, 5001), (17, 1024, 5001),
+         (32, 2044, 3001), (24, 1500, 4099), (32, 512, 8192), (32, 512, 8193), (16, 2048, 17), (12, 1601, 1000)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", HEADS, ids=lambda s: "x".join(map(str, s)))
+def test_small_batches_over_heads(size, dtype):
+    check(*make(*size, TYPES[dtype], seed=sum(size)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [2, 9, 32, 100])
+@pytest.mark.parametrize("bits", [0x7fc00000, 0x7fffffff, -1, 0x7f800001])
+def test_nan_of_any_payload(bits, rows):
+    x, w, t, dl = make(rows, 40, 300, torch.float32, 12)
+    t[:] = torch.arange(rows, device="cuda")
+    x.view(torch.int32)[1, 3] = bits
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    assert torch.isnan(loss[1]) and torch.isnan(lse[1]) and torch.isnan(dx[1]).all() and torch.isnan(dw).all()
+    others = torch.arange(rows, device="cuda") != 1
+    assert torch.isfinite(loss[others]).all() and torch.isfinite(dx[others]).all()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("mask", ["none", "all"])
