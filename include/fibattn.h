@@ -290,10 +290,11 @@ int fibattn_fwd_noalloc(const void* q, const void* k, const void* v, void* out, 
  * (fibattn_check_status).  Limits: 0 <= N <= 2^24, 1 <= D <= 8192,
  * 1 <= V <= 2^24.  N == 0 launches nothing but the zeroing of dw.
  * Every product is accumulated in fp32; results do not depend on timing.  fp32
- * operands keep their 24 bits (on the tensor cores as sums of three bf16 values);
- * with bf16 I/O g is rounded to bf16 between the two products of the gradient
- * (relative to the largest |dloss|, so that equal weights round nothing), as a
- * bf16 tensor between two library calls would be.
+ * operands keep their 24 bits (on the tensor cores as sums of three bf16 values),
+ * in calls of three to 32 rows 22 of them (sums of two tf32 values); with bf16 I/O
+ * and more rows than that g is rounded to bf16 between the two products of the
+ * gradient (relative to the largest |dloss|, so that equal weights round nothing),
+ * as a bf16 tensor between two library calls would be.
  * As in any matrix product, an ignored row of x that holds an infinity or NaN
  * still reaches dw as 0 * NaN.
  * ------------------------------------------------------------------------- */

@@ -40,7 +40,7 @@ cudaError_t launch_join_rows(const Problem& p, const FwdParts& parts, int segmen
 // dx from parts [ranges][N][D].
 cudaError_t launch_join_dx(const Problem& p, const float* parts, int ranges, void* dx, bool bf16, cudaStream_t st);
 
-// One to four rows (xent_stream.cu).  Scratch of the gradient: parts [blocks][N][D].
+// One to four rows, as vectors (xent_stream.cu).  Scratch of the gradient: parts [blocks][N][D].
 bool stream_applies(int N, int D);
 int stream_segments(int V);
 cudaError_t launch_stream(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);

@@ -46,7 +46,7 @@ struct Maps {
     CUtensorMap m[4];
 };
 
-// Where a call goes: one to four rows, few rows, or tiles on the fifth-generation cores.
+// Where a call goes: rows as vectors, few rows, or tiles on the fifth-generation cores.
 enum class Way { kStream, kFewRows, kTiles };
 
 struct FwdPlan {

@@ -5,8 +5,9 @@
 // of each per step, against x in shared memory (fp32).  The gradient is one pass
 // too: the logits, g and both products of a batch of rows of w while it is in
 // cache.  Bound by memory for one row, by the FMA rate and the reductions from
-// about four (us on the GPU forward + backward, 512 wide, 32768 columns, bf16:
-// 10.6 + 24.4 for one row, 15.1 + 32.5 for four; w is read in 5.0 at the peak).
+// about four, which come here only over small heads (us on the GPU forward +
+// backward, 512 wide, bf16: one row over 32768 columns 8.9 + 24.2, w being read in
+// 5.0 at the peak; four over 4000 columns 6.2 + 11.2).
 #include <algorithm>
 
 #include "xent.cuh"
