@@ -50,7 +50,7 @@ cudaError_t launch_stream_gradient(const Problem& p, const float* lse, const flo
 
 // Few rows (xent_rows.cu).  Scratch of the gradient: gradient [V][tokens], parts
 // [ranges][N][D]; all fp32.
-bool few_rows_applies(int N, int D);
+bool few_rows_applies(int N);
 int few_rows_tokens(int N);                        // N rounded up to 8, 16 or 32
 int few_rows_segments(int N, int D, int V);
 cudaError_t launch_few_rows(const Problem& p, const FwdParts& parts, int segments, bool bf16, cudaStream_t st);

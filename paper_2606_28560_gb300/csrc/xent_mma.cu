@@ -914,6 +914,7 @@ static bool several_planes(int N, int D, int V, bool bf16) {
 //   1000 wide, 20000 columns:      52 / 67     64 / 67    102 / 64       153 / 270
 //   2048 wide, 131072 columns:   455 / 496   552 / 498   954 / 502     1357 / 2660
 //   512 wide, 4000 columns:        21 / 31     25 / 31     28 / 30        38 / 75
+//   8192 wide, 20000 columns:    322 / 355                              1415 / 1918
 // and stream / few rows:
 //                              bf16: 1 row      2 rows      4 rows     fp32: 4 rows
 //   512 wide, 32768 columns:       33 / 43     38 / 43     48 / 43        67 / 64
@@ -924,7 +925,7 @@ static Way way_of(int N, int D, int V, bool bf16) {
     const bool small = (long long)V * D <= (1 << 22);
     if (stream_applies(N, D) && (N <= 2 || small)) return Way::kStream;
     const int most = !bf16 || small ? 32 : D <= 1024 ? 16 : 8;
-    return N <= most && few_rows_applies(N, D) ? Way::kFewRows : Way::kTiles;
+    return N <= most && few_rows_applies(N) ? Way::kFewRows : Way::kTiles;
 }
 
 FwdPlan plan_forward(int N, int D, int V, bool bf16) {

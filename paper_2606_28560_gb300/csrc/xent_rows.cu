@@ -124,6 +124,14 @@ __device__ __forceinline__ void mma(float* c, const unsigned* a, unsigned b0, un
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Of x's blocks of depth (four lanes' 16 bytes), those that a block of threads can
+// hold for oct x 8 rows.
+constexpr size_t kMostSmem = 224 * 1024;           // of the 227 KB that it may have, two for statistics
+template <typename T> __host__ __device__ constexpr int staged_blocks(int oct, int D) {
+    const int block = 4 * Lane<T>::kValues, all = (D + block - 1) / block, most = (int)(kMostSmem / ((size_t)oct * 8 * block * 4));
+    return all < most ? all : most;
+}
+
 // Where value j of lane l's 16 bytes of block b of octet o's rows of x lies.
 template <typename T, int OCT> __device__ __forceinline__ int staged(int b, int o, int l, int j) {
     return (((b * OCT + o) * (Lane<T>::kValues / 4) + j / 4) * 32 + l) * 4 + j % 4;
@@ -131,9 +139,11 @@ template <typename T, int OCT> __device__ __forceinline__ int staged(int b, int 
 
 // Logits of 16 rows of w (from v0) and OCT x 8 rows of x (xs):
 // s[o][0..3] = rows g, g, g + 8, g + 8 and tokens 2 t, 2 t + 1, 2 t, 2 t + 1 of
-// octet o, lane = 4 g + t.
-template <typename T, int OCT, bool VECTORS>
-__device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, const float* xs, int lane, float (*s)[4]) {
+// octet o, lane = 4 g + t.  x: the same rows in memory, `rows` of them, read where they
+// are deeper than what is staged (never when WHOLE).
+template <typename T, int OCT, bool VECTORS, bool WHOLE>
+__device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, const float* xs, const T* x, int rows, int lane,
+                                            float (*s)[4]) {
     constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal, kAhead = 4;   // blocks of depth under way
     constexpr bool kExact = sizeof(T) == 2;
     const int g = lane >> 2, t = lane & 3, blocks = (D + kBlock - 1) / kBlock;
@@ -192,8 +202,14 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
                     }
 #pragma unroll
                     for (int o = 0; o < OCT; ++o) {
-                        const float4 x = *reinterpret_cast<const float4*>(xs + staged<T, OCT>(b0 + u, o, lane, 4 * q));
-                        const float e[4] = {x.x, x.y, x.z, x.w};
+                        float e[4];
+                        if (WHOLE || b0 + u < staged_blocks<T>(OCT, D)) {
+                            const float4 f = *reinterpret_cast<const float4*>(xs + staged<T, OCT>(b0 + u, o, lane, 4 * q));
+                            e[0] = f.x; e[1] = f.y; e[2] = f.z; e[3] = f.w;
+                        } else {
+                            const int n = 8 * o + g, k = (b0 + u) * kBlock + t * kVal + 4 * q;
+                            load4<T, VECTORS>(x + (size_t)n * D + k, n < rows ? D - k : 0, e);
+                        }
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             const unsigned b0h = kExact ? __float_as_uint(e[2 * h]) : high(e[2 * h]);
@@ -219,12 +235,12 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
         for (int j = 0; j < 4; ++j) s[o][j] += small[o][j];
 }
 
-// x's rows from n0 (8 OCT of them, zeros past N) into shared memory, as tile_logits
-// reads them, 16 bytes to a thread, eight of them under way.
+// x's rows from n0 (8 OCT of them, zeros past N), as deep as they fit, into shared memory,
+// as tile_logits reads them, 16 bytes to a thread, eight of them under way.
 template <typename T, int OCT, bool VECTORS, int WARPS>
 __device__ __forceinline__ void stage_x(const Problem& p, int n0, float* xs) {
     constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal, kAhead = 8;
-    const int pieces = (p.D + kBlock - 1) / kBlock * OCT * 32;
+    const int pieces = staged_blocks<T>(OCT, p.D) * OCT * 32;
     for (int i0 = threadIdx.x; i0 < pieces; i0 += kAhead * 32 * WARPS) {
         uint4 u[kAhead];
 #pragma unroll
@@ -255,7 +271,7 @@ __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
 // Block: a segment of w (for `groups` > 1 as many groups of 8 OCT rows of x, whose
 // blocks follow one another so that they read w together).  Statistics
 // [row][segment].
-template <typename T, int OCT, bool VECTORS, int WARPS>
+template <typename T, int OCT, bool VECTORS, int WARPS, bool WHOLE>
 __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p, FwdParts parts, int segments, int groups) {
     extern __shared__ __align__(16) float xs[];
     __shared__ float red[2][WARPS][8 * OCT];
@@ -278,7 +294,8 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p,
     const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = segments * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
-        tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
+        tile_logits<T, OCT, VECTORS, WHOLE>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
+                                            static_cast<const T*>(p.x) + (size_t)n0 * p.D, p.N - n0, lane, s);
         const int v = i * kTileRows + g;
 #pragma unroll
         for (int o = 0; o < OCT; ++o)
@@ -315,7 +332,7 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p,
 }
 
 // The same logits, as g[v][token] (row length `tokens`; zeros for tokens past N).
-template <typename T, int OCT, bool VECTORS, int WARPS>
+template <typename T, int OCT, bool VECTORS, int WARPS, bool WHOLE>
 __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gradient, int tokens, int groups) {
     extern __shared__ __align__(16) float xs[];
@@ -339,7 +356,8 @@ rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gra
     const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = gridDim.x / groups * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
-        tile_logits<T, OCT, VECTORS>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs, lane, s);
+        tile_logits<T, OCT, VECTORS, WHOLE>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
+                                            static_cast<const T*>(p.x) + (size_t)n0 * p.D, p.N - n0, lane, s);
 #pragma unroll
         for (int o = 0; o < OCT; ++o)
 #pragma unroll
@@ -622,53 +640,53 @@ __global__ void __launch_bounds__(256) join_rows_kernel(Problem p, FwdParts part
     }
 }
 
-constexpr size_t kMostSmem = 200 * 1024;
-
 template <typename K> cudaError_t allow_smem(K kern) {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostSmem);
 }
 
+// x of oct x 8 rows, whole (its values are fp32 there, its depth a multiple of 32).
 size_t smem_of(int oct, int D) { return (size_t)oct * 8 * ((D + 31) / 32 * 32) * 4; }
 
-// Octets of rows of x: 1, 2 or 4, as many as there are; and how many of them fit a
-// block's shared memory at a time (0: not one).
+// Octets of rows of x: 1, 2 or 4, as many as there are; and how many a block takes at a
+// time: two if they fit its shared memory (of one, the rest is read where it lies:
+// D > 7168).
 int octets(int N) { return N <= 8 ? 1 : N <= 16 ? 2 : 4; }
-int octets_at_once(int N, int D) {
-    int oct = std::min(2, octets(N));
-    while (oct > 0 && smem_of(oct, D) > kMostSmem) oct /= 2;
-    return oct;
-}
+int octets_at_once(int N, int D) { return N > 8 && smem_of(2, D) <= kMostSmem ? 2 : 1; }
 
-// Two octets: blocks of eight warps while two of them fit an SM, else one of
-// sixteen.
-bool sixteen_warps(int D) { return smem_of(2, D) > kMostSmem / 2; }
+// Blocks of eight warps while two of them fit an SM, else one of sixteen.
+bool sixteen_warps(int oct, int D) { return smem_of(oct, D) > 100 * 1024; }
 
-template <typename T, int OCT, bool VECTORS, int WARPS>
+template <typename T, int OCT, bool VECTORS, int WARPS, bool WHOLE = true>
 cudaError_t launch_rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
-    const auto kern = rows_kernel<T, OCT, VECTORS, WARPS>;
+    const auto kern = rows_kernel<T, OCT, VECTORS, WARPS, WHOLE>;
     const cudaError_t e = allow_smem(kern);
     if (e != cudaSuccess) return e;
     const int groups = octets(p.N) / OCT;
-    return launch_kernel(kern, dim3((unsigned)(segments * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p, parts, segments, groups);
+    const size_t smem = std::min(smem_of(OCT, p.D), kMostSmem);
+    return launch_kernel(kern, dim3((unsigned)(segments * groups)), dim3(32 * WARPS), smem, st, p, parts, segments, groups);
 }
 template <typename T, bool VECTORS>
 cudaError_t rows(const Problem& p, const FwdParts& parts, int segments, cudaStream_t st) {
     switch (octets_at_once(p.N, p.D)) {
-    case 1: return launch_rows<T, 1, VECTORS, kWarps>(p, parts, segments, st);
+    case 1:
+        return smem_of(1, p.D) > kMostSmem ? launch_rows<T, 1, VECTORS, 16, false>(p, parts, segments, st)
+               : sixteen_warps(1, p.D)     ? launch_rows<T, 1, VECTORS, 16>(p, parts, segments, st)
+                                           : launch_rows<T, 1, VECTORS, kWarps>(p, parts, segments, st);
     default:
-        return sixteen_warps(p.D) ? launch_rows<T, 2, VECTORS, 16>(p, parts, segments, st)
-                                  : launch_rows<T, 2, VECTORS, kWarps>(p, parts, segments, st);
+        return sixteen_warps(2, p.D) ? launch_rows<T, 2, VECTORS, 16>(p, parts, segments, st)
+                                     : launch_rows<T, 2, VECTORS, kWarps>(p, parts, segments, st);
     }
 }
 
-template <typename T, int OCT, bool VECTORS, int WARPS>
+template <typename T, int OCT, bool VECTORS, int WARPS, bool WHOLE = true>
 cudaError_t launch_gradient(const Problem& p, const float* lse, const float* dloss, float* gradient, cudaStream_t st) {
-    const auto kern = rows_gradient_kernel<T, OCT, VECTORS, WARPS>;
+    const auto kern = rows_gradient_kernel<T, OCT, VECTORS, WARPS, WHOLE>;
     const cudaError_t e = allow_smem(kern);
     if (e != cudaSuccess) return e;
     const int groups = octets(p.N) / OCT;
+    const size_t smem = std::min(smem_of(OCT, p.D), kMostSmem);
     ProfScope s("xent_few_rows_grad", st);
-    return launch_kernel(kern, dim3((unsigned)(few_rows_segments(p.N, p.D, p.V) * groups)), dim3(32 * WARPS), smem_of(OCT, p.D), st, p,
+    return launch_kernel(kern, dim3((unsigned)(few_rows_segments(p.N, p.D, p.V) * groups)), dim3(32 * WARPS), smem, st, p,
                          lse, dloss, gradient, 8 * octets(p.N), groups);
 }
 template <typename T, int OCT, bool VECTORS>
@@ -682,9 +700,12 @@ template <typename T, bool VECTORS>
 cudaError_t gradient_of(const Problem& p, const float* lse, const float* dloss, T* dx, T* dw, float* gradient, float* parts, int ranges,
                         cudaStream_t st) {
     const int once = octets_at_once(p.N, p.D);
-    cudaError_t e = once == 1              ? launch_gradient<T, 1, VECTORS, kWarps>(p, lse, dloss, gradient, st)
-                    : sixteen_warps(p.D) ? launch_gradient<T, 2, VECTORS, 16>(p, lse, dloss, gradient, st)
-                                         : launch_gradient<T, 2, VECTORS, kWarps>(p, lse, dloss, gradient, st);
+    const bool sixteen = sixteen_warps(once, p.D);
+    cudaError_t e = smem_of(1, p.D) > kMostSmem ? launch_gradient<T, 1, VECTORS, 16, false>(p, lse, dloss, gradient, st)
+                    : once == 1 && sixteen      ? launch_gradient<T, 1, VECTORS, 16>(p, lse, dloss, gradient, st)
+                    : once == 1                 ? launch_gradient<T, 1, VECTORS, kWarps>(p, lse, dloss, gradient, st)
+                    : sixteen                   ? launch_gradient<T, 2, VECTORS, 16>(p, lse, dloss, gradient, st)
+                                                : launch_gradient<T, 2, VECTORS, kWarps>(p, lse, dloss, gradient, st);
     if (e != cudaSuccess) return e;
     float* to = dx ? parts : nullptr;
     const int oct = octets(p.N);
@@ -696,7 +717,7 @@ cudaError_t gradient_of(const Problem& p, const float* lse, const float* dloss, 
 
 }  // namespace
 
-bool few_rows_applies(int N, int D) { return N <= 32 && octets_at_once(N, D) > 0; }
+bool few_rows_applies(int N) { return N <= 32; }
 
 int few_rows_tokens(int N) { return 8 * octets(N); }
 
@@ -704,7 +725,7 @@ int few_rows_tokens(int N) { return 8 * octets(N); }
 // would only stage x more often), and no more than leave a block tiles 1024 deep in
 // all (a small w is spread over the SMs before it is over warps), eight at most.
 int few_rows_segments(int N, int D, int V) {
-    const int once = octets_at_once(N, D), groups = octets(N) / once, blocks = once == 2 && sixteen_warps(D) ? 152 : 2 * 152;
+    const int once = octets_at_once(N, D), groups = octets(N) / once, blocks = sixteen_warps(once, D) ? 152 : 2 * 152;
     const int rows = kTileRows * std::max(1, std::min(8, 1024 / D));
     return std::max(1, std::min(blocks / groups, (V + rows - 1) / rows));
 }

@@ -107,6 +107,18 @@ def test_small_batches_over_heads(size, dtype):
     check(*make(*size, TYPES[dtype], seed=sum(size)))
 
 
+# rows of x deeper than a block's shared memory, and as deep
+DEEP = [(8, 7168, 200), (4, 7176, 900), (8, 8192, 333), (12, 7999, 517), (32, 8190, 100), (1, 8192, 50), (16, 3584, 300), (16, 3592, 300),
+        (8, 4096, 700)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("size", DEEP, ids=lambda s: "x".join(map(str, s)))
+def test_small_batches_of_deep_rows(size, dtype):
+    check(*make(*size, TYPES[dtype], seed=sum(size)))
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows", [2, 9, 32, 100])
 @pytest.mark.parametrize("bits", [0x7fc00000, 0x7fffffff, -1, 0x7f800001])
