@@ -910,16 +910,16 @@ static bool several_planes(int N, int D, int V, bool bf16) {
 // call takes the one that is faster.  Forward and backward together, us on the GPU,
 // few rows / tiles:
 //                              bf16: 8 rows     16 rows     32 rows    fp32: 32 rows
-//   512 wide, 32768 columns:       44 / 67     54 / 67     83 / 62       118 / 203
-//   1000 wide, 20000 columns:      52 / 67     64 / 67    102 / 64       153 / 270
-//   2048 wide, 131072 columns:   455 / 496   552 / 498   954 / 502     1357 / 2660
-//   512 wide, 4000 columns:        21 / 31     25 / 31     28 / 30        38 / 75
-//   8192 wide, 20000 columns:    322 / 355                              1415 / 1918
+//   512 wide, 32768 columns:       42 / 67     51 / 67     83 / 62       115 / 203
+//   1000 wide, 20000 columns:      52 / 67     63 / 67    102 / 65       150 / 279
+//   2048 wide, 131072 columns:   449 / 496   552 / 498   954 / 500     1336 / 2642
+//   512 wide, 4000 columns:        21 / 31     24 / 31     27 / 30        38 / 75
+//   8192 wide, 20000 columns:    322 / 355                              1414 / 1918
 // and stream / few rows:
 //                              bf16: 1 row      2 rows      4 rows     fp32: 4 rows
-//   512 wide, 32768 columns:       33 / 43     38 / 43     48 / 43        67 / 64
-//   1000 wide, 20000 columns:      42 / 51     50 / 51     65 / 51        91 / 78
-//   2048 wide, 131072 columns:   372 / 455   425 / 457   517 / 459      802 / 801
+//   512 wide, 32768 columns:       33 / 43     38 / 43     48 / 41        67 / 62
+//   1000 wide, 20000 columns:      42 / 51     50 / 51     65 / 51        91 / 79
+//   2048 wide, 131072 columns:   372 / 455   425 / 457   517 / 450      802 / 780
 //   512 wide, 4000 columns:        13 / 21     14 / 21     17 / 21        18 / 25
 static Way way_of(int N, int D, int V, bool bf16) {
     const bool small = (long long)V * D <= (1 << 22);

@@ -11,8 +11,8 @@
 // core truncates.
 //
 // Bound by memory in bf16 and up to 16 rows in fp32: 16 x 2048 x 131072 in fp32 takes
-// 191 us forward (5.6 TB/s) and 631 backward (2 x 1.07 GB read, 1.07 written).
-// With 32 rows, 354 and 1003, it is halfway between memory (159 and 476) and the
+// 188 us forward (5.7 TB/s) and 628 backward (2 x 1.07 GB read, 1.07 written).
+// With 32 rows, 344 and 992, it is halfway between memory (159 and 476) and the
 // tensor rate (150 T multiplications a second, three for one in fp32): what is
 // issued beside them, the splitting in two and the loads of x, is the rest.
 //
@@ -140,8 +140,9 @@ template <typename T, int OCT> __device__ __forceinline__ int staged(int b, int 
 // Logits of 16 rows of w (from v0) and OCT x 8 rows of x (xs):
 // s[o][0..3] = rows g, g, g + 8, g + 8 and tokens 2 t, 2 t + 1, 2 t, 2 t + 1 of
 // octet o, lane = 4 g + t.  x: the same rows in memory, `rows` of them, read where they
-// are deeper than what is staged (never when WHOLE).
-template <typename T, int OCT, bool VECTORS, bool WHOLE>
+// are deeper than what is staged (never when WHOLE).  AHEAD: w is asked into L2 two
+// steps before it is loaded.
+template <typename T, int OCT, bool VECTORS, bool WHOLE, bool AHEAD>
 __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, const float* xs, const T* x, int rows, int lane,
                                             float (*s)[4]) {
     constexpr int kVal = Lane<T>::kValues, kBlock = 4 * kVal, kAhead = 4;   // blocks of depth under way
@@ -163,12 +164,13 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
             n0[u] = fetch16<T, VECTORS>(r0 + k, in0 ? left : 0);
             n1[u] = fetch16<T, VECTORS>(r1 + k, in1 ? left : 0);
         }
-        // into L2: what comes 2 steps later, of the next tile too
-        constexpr int kStep = kAhead * kBlock;
-        const int depth = (blocks + kAhead - 1) / kAhead * kStep;
-        int k = b0 * kBlock + 2 * kStep + (lane >> 4) * (kStep / 2), v = v0 + (lane & 15);
-        if (k >= depth) { k -= depth; v += kTileRows; }
-        if (k < D && v < V) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(w + (size_t)v * D + k));
+        if constexpr (AHEAD) {                     // 256 bytes of each row, of the next tile's too
+            constexpr int kStep = kAhead * kBlock;
+            const int depth = (blocks + kAhead - 1) / kAhead * kStep;
+            int k = b0 * kBlock + 2 * kStep + (lane >> 4) * (kStep / 2), v = v0 + (lane & 15);
+            if (k >= depth) { k -= depth; v += kTileRows; }
+            if (k < D && v < V) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(w + (size_t)v * D + k));
+        }
     };
     fetch(0);
     for (int b0 = 0; b0 < blocks; b0 += kAhead) {
@@ -268,6 +270,12 @@ __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
     m = top;
 }
 
+// Whether tile_logits asks ahead: for eight deep rows it is memory's latency that bounds,
+// otherwise the instructions are missed elsewhere (fp32, us forward and backward, with
+// / without: 8 x 8192 x 20000 584 / 648, 8 x 7168 x 20000 465 / 489, 16 x 2048 x
+// 131072 830 / 814, 16 x 512 x 32768 79 / 75).
+constexpr bool asked_ahead(int oct, int warps) { return oct == 1 && warps == 16; }
+
 // Block: a segment of w (for `groups` > 1 as many groups of 8 OCT rows of x, whose
 // blocks follow one another so that they read w together).  Statistics
 // [row][segment].
@@ -294,8 +302,9 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) rows_kernel(Problem p,
     const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = segments * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
-        tile_logits<T, OCT, VECTORS, WHOLE>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
-                                            static_cast<const T*>(p.x) + (size_t)n0 * p.D, p.N - n0, lane, s);
+        tile_logits<T, OCT, VECTORS, WHOLE, asked_ahead(OCT, WARPS)>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
+                                                                               static_cast<const T*>(p.x) + (size_t)n0 * p.D,
+                                                                               p.N - n0, lane, s);
         const int v = i * kTileRows + g;
 #pragma unroll
         for (int o = 0; o < OCT; ++o)
@@ -356,8 +365,9 @@ rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gra
     const int tiles = (p.V + kTileRows - 1) / kTileRows, worker = seg * WARPS + warp, workers = gridDim.x / groups * WARPS;
     for (int i = (int)((long long)tiles * worker / workers); i < (int)((long long)tiles * (worker + 1) / workers); ++i) {
         float s[OCT][4];
-        tile_logits<T, OCT, VECTORS, WHOLE>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
-                                            static_cast<const T*>(p.x) + (size_t)n0 * p.D, p.N - n0, lane, s);
+        tile_logits<T, OCT, VECTORS, WHOLE, asked_ahead(OCT, WARPS)>(static_cast<const T*>(p.w), p.V, p.D, i * kTileRows, xs,
+                                                                               static_cast<const T*>(p.x) + (size_t)n0 * p.D,
+                                                                               p.N - n0, lane, s);
 #pragma unroll
         for (int o = 0; o < OCT; ++o)
 #pragma unroll

@@ -151,6 +151,38 @@ def test_several_pieces_of_the_vocabulary(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("N", [1, 8, 40])
+def test_offsets_beyond_31_bits(N):
+    """w and dw of more than 2^31 values: the definition in 64 bits a piece of the vocabulary at a time."""
+    D, V, piece = 2056 if N > 1 else 2048, 1_050_000, 1 << 16
+    x, w0, _, dl = make(N, D, piece, torch.bfloat16, 13, "none")
+    w = torch.empty(V, D, dtype=torch.bfloat16, device="cuda")
+    for k, at in enumerate(range(0, V, piece)):
+        w[at:at + piece] = w0.roll(k, 0)[:V - at]
+    t = V - 1 - 3 * torch.arange(N, device="cuda")
+    assert w.numel() > 2 ** 31
+    s = torch.cat([x.double() @ w[at:at + piece].double().t() for at in range(0, V, piece)], 1)
+    e = (D + 8) * U * float((x.double().abs() @ w0.double().abs().t()).max())      # every piece has w0's rows
+    want_lse = torch.logsumexp(s, 1)
+    tol = 2 * e + 16 * U * (1 + float(want_lse.abs().max()))
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    assert (lse.double() - want_lse).abs().max() <= tol
+    assert (loss.double() - (want_lse - s.gather(1, t[:, None])[:, 0])).abs().max() <= tol
+    g = torch.exp(s - want_lse[:, None])
+    g[torch.arange(N, device="cuda"), t] -= 1.0
+    g *= dl.double()[:, None]
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    want_dx, off = 0, 0
+    for at in range(0, V, piece):
+        part = g[:, at:at + piece]
+        want_dx = want_dx + part @ w[at:at + piece].double()
+        off += float((dw[at:at + piece].double() - part.t() @ x.double()).square().sum())
+    # by norms, with the bound that the whole matrices of the other tests have
+    assert float((dx.double() - want_dx).norm()) <= 3.2e-3 * float(want_dx.norm())
+    assert off ** 0.5 <= 3.2e-3 * float(sum((g[:, at:at + piece].t() @ x.double()).square().sum() for at in range(0, V, piece))) ** 0.5
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_large_logits(dtype):
     # spread of thousands: exp of anything but the maximum vanishes, nothing overflows
