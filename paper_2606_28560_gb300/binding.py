@@ -196,6 +196,19 @@ def _dtype_code(t: torch.Tensor) -> int:
     raise TypeError(f"unsupported dtype {t.dtype}: fp32 or bf16")
 
 
+def _check_device(index: int, *tensors):
+    """The tensors (None: not given) are on device ``index`` and that is the
+    current one, where the library puts its work: it cannot follow the pointers
+    of another."""
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors must be on one CUDA device")
+    current = torch.cuda.current_device()
+    if index != current:
+        raise ValueError(f"the tensors are on cuda:{index} and the current device is cuda:{current}: "
+                         f"make the call under torch.cuda.device({index})")
+
+
 def _stream_ptr(stream) -> int:
     s = stream if stream is not None else torch.cuda.current_stream()
     return int(s.cuda_stream)
@@ -314,6 +327,7 @@ def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, de
     for t in (q, k, v):
         if not (t.is_cuda and t.is_contiguous() and t.dtype == q.dtype):
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
+    _check_device(q.get_device(), k, v, out, lse, workspace, rotated_k, residuals)
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
@@ -351,6 +365,7 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
     for t in (q, k, v, dout) + ((out,) if out is not None else ()):
         if not (t.is_cuda and t.is_contiguous() and t.dtype == q.dtype):
             raise ValueError("q, k, v, dout, out must be contiguous CUDA tensors of one dtype")
+    _check_device(q.get_device(), k, v, lse, dout, out, dq, dk, dv, dtheta, dd, workspace, rotated_k, residuals)
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
@@ -396,6 +411,7 @@ def _check_xent(x, w, targets):
         raise ValueError("targets must be a contiguous CUDA int64 tensor")
     if w.get_device() != index or targets.get_device() != index:
         raise ValueError("x, w and targets must be on one device")
+    _check_device(index)
     return N, D, V, _dtype_code(x), index
 
 
@@ -494,6 +510,7 @@ def _clip(grads, max_norm, out, norm, workspace, stream, scale):
     if out is not None and n and (list(map(_dtype_of, outs)) != dtypes or
                                   list(map(torch.Tensor.numel, outs)) != sizes or not _on_device(outs, index)):
         raise ValueError("out must hold contiguous tensors like the gradients")
+    _check_device(index)
     device = grads[0].device if n else torch.device("cuda", index)
     if norm is None:
         norm = torch.empty((), dtype=torch.float32, device=device)
