@@ -209,6 +209,12 @@ def _check_device(index: int, *tensors):
                          f"make the call under torch.cuda.device({index})")
 
 
+def _check_workspace(workspace, index: int):
+    """Of a workspace that the caller gives; its size is checked by the library."""
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous buffer on the tensors' CUDA device")
+
+
 def _stream_ptr(stream) -> int:
     s = stream if stream is not None else torch.cuda.current_stream()
     return int(s.cuda_stream)
@@ -327,12 +333,14 @@ def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, de
     for t in (q, k, v):
         if not (t.is_cuda and t.is_contiguous() and t.dtype == q.dtype):
             raise ValueError("q, k, v must be contiguous CUDA tensors of one dtype")
-    _check_device(q.get_device(), k, v, out, lse, workspace, rotated_k, residuals)
+    _check_device(q.get_device(), k, v, out, lse, rotated_k, residuals)
     if out is None:
         out = torch.empty_like(q)
     if lse is None:
         lse = torch.empty((B, H, T), dtype=torch.float32, device=q.device)
-    if workspace is None:                        # (a given workspace's size is checked by the library)
+    if workspace is not None:
+        _check_workspace(workspace, q.get_device())
+    else:
         need = int(lib().fibattn_fwd_workspace_bytes(B, H, T, D, W, len(f), code, ctypes.byref(o)))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
     _check(lib().fibattn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
@@ -365,14 +373,16 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
     for t in (q, k, v, dout) + ((out,) if out is not None else ()):
         if not (t.is_cuda and t.is_contiguous() and t.dtype == q.dtype):
             raise ValueError("q, k, v, dout, out must be contiguous CUDA tensors of one dtype")
-    _check_device(q.get_device(), k, v, lse, dout, out, dq, dk, dv, dtheta, dd, workspace, rotated_k, residuals)
+    _check_device(q.get_device(), k, v, lse, dout, out, dq, dk, dv, dtheta, dd, rotated_k, residuals)
     dq = torch.empty_like(q) if dq is None else dq
     dk = torch.empty_like(k) if dk is None else dk
     dv = torch.empty_like(v) if dv is None else dv
     if rung_grads:
         dtheta = torch.empty(4, dtype=torch.float32, device=q.device) if dtheta is None else dtheta
         dd = torch.empty(max(K, 1), dtype=torch.float32, device=q.device) if dd is None else dd
-    if workspace is None:                        # (a given workspace's size is checked by the library)
+    if workspace is not None:
+        _check_workspace(workspace, q.get_device())
+    else:
         need = int(lib().fibattn_bwd_workspace_bytes(B, H, T, D, W, K, code, ctypes.byref(o)))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
     _check(lib().fibattn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr() if out is not None else None,
@@ -431,7 +441,9 @@ def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=N
     loss = torch.empty(N, dtype=torch.float32, device=x.device) if loss is None else _f32_row(loss, N, index, "loss")
     lse = torch.empty_like(loss) if lse is None else _f32_row(lse, N, index, "lse")
     L = lib()
-    if workspace is None:                        # (a given workspace's size is checked by the library)
+    if workspace is not None:
+        _check_workspace(workspace, index)
+    else:
         need = L.fibattn_linear_xent_fwd_workspace_bytes(N, D, V, code)
         workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
     _check(L.fibattn_linear_xent_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(), lse.data_ptr(),
@@ -454,7 +466,9 @@ def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=N
     dx = None if not want_dx else torch.empty_like(x) if dx is None else _grad_like(dx, x)
     dw = None if not want_dw else torch.empty_like(w) if dw is None else _grad_like(dw, w)
     L = lib()
-    if workspace is None:
+    if workspace is not None:
+        _check_workspace(workspace, index)
+    else:
         need = L.fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
         workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
     _check(L.fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
@@ -517,7 +531,9 @@ def _clip(grads, max_norm, out, norm, workspace, stream, scale):
     elif norm.dtype != torch.float32 or norm.numel() != 1 or norm.get_device() != index:
         raise ValueError("norm must be one fp32 value on the gradients' device")
     L = lib()
-    if workspace is None:
+    if workspace is not None:
+        _check_workspace(workspace, index)
+    else:
         workspace = torch.empty(L.fibattn_clip_grads_workspace_bytes(n), dtype=torch.uint8, device=device)
     ptrs = array.array("Q", map(torch.Tensor.data_ptr, grads))
     optrs = (ptrs if out is None else array.array("Q", map(torch.Tensor.data_ptr, outs))) if scale else None

@@ -80,14 +80,31 @@ def test_tensors_of_another_device_are_refused(name, library):
     assert not library.calls
 
 
-@pytest.mark.parametrize("given", ["k", "out", "lse", "workspace"])
+@pytest.mark.parametrize("given", ["k", "out", "lse"])
 def test_attention_tensors_of_two_devices_are_refused(given, library):
     q, k, v = heads("cuda:0", 3)
-    other = {"k": heads("cuda:1", 1)[0], "out": heads("cuda:1", 1)[0], "lse": torch.empty(1, 2, 16, device="cuda:1"),
-             "workspace": torch.empty(4096, dtype=U8, device="cuda:1")}[given]
+    other = {"k": heads("cuda:1", 1)[0], "out": heads("cuda:1", 1)[0], "lse": torch.empty(1, 2, 16, device="cuda:1")}[given]
     with pytest.raises(ValueError, match="one CUDA device"):
         if given == "k":
             fa.fwd(q, other, v, 1.0, OFFSETS, 8)
         else:
             fa.fwd(q, k, v, 1.0, OFFSETS, 8, **{given: other})
     assert not library.calls
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+@pytest.mark.parametrize("kind", ["cpu", "another device", "strided", "expanded"])
+def test_workspaces_that_are_not_the_devices_memory_are_refused(kind, name, library):
+    device = {"cpu": "cpu", "another device": "cuda:1"}.get(kind, "cuda:0")
+    ws = {"strided": lambda: torch.empty(8192, dtype=U8, device=device)[::2],
+          "expanded": lambda: torch.empty(1, dtype=U8, device=device).expand(4096)}.get(
+              kind, lambda: torch.empty(4096, dtype=U8, device=device))()
+    with pytest.raises(ValueError, match="workspace"):
+        CALLS[name]("cuda:0", workspace=ws)
+    assert not library.calls
+
+
+@pytest.mark.parametrize("name", list(CALLS))
+def test_a_workspace_of_the_device_is_used(name, library):
+    CALLS[name]("cuda:0", workspace=torch.empty(4096, dtype=U8, device="cuda:0"))
+    assert len(library.calls) == 1
