@@ -10,6 +10,7 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
+import inspect
 import operator
 import os
 import threading
@@ -220,6 +221,50 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+# The current stream of a device by its index, without the Stream object that
+# torch.cuda.current_stream() builds (some 4 us of every call).
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
+    lambda index: torch.cuda.current_stream(index).cuda_stream
+
+
+def _record(values, stream):
+    for t in values:
+        if torch.is_tensor(t):
+            t.record_stream(stream)
+        elif isinstance(t, (list, tuple)):
+            _record(t, stream)
+
+
+def _takes_stream(call):
+    """Gives a call a ``stream=``: the torch stream its kernels run on (default: the
+    current one).  The call is then made with that stream current, so that what
+    it allocates belongs to that stream and is not handed to other work while the
+    kernels use it.  Given tensors are recorded with that stream, results with the
+    caller's: dropping them frees nothing that the other stream still uses.  That
+    inputs are ready, and results finished, is the caller's to order, as between
+    any two streams."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream.cuda_stream))
+        caller = torch.cuda.current_stream(stream.device)
+        if caller == stream:
+            return call(*args, **kw)
+        with torch.cuda.stream(stream):
+            results = call(*args, **kw)
+        _record(args, stream)
+        _record(kw.values(), stream)
+        _record(results if isinstance(results, tuple) else (results,), caller)
+        return results
+
+    sig = inspect.signature(call)
+    on_stream.__signature__ = sig.replace(parameters=[
+        *sig.parameters.values(), inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
+    return on_stream
+
+
 def _offsets(offsets) -> np.ndarray:
     if isinstance(offsets, np.ndarray) and offsets.dtype == np.float32 and offsets.flags.c_contiguous:
         return offsets
@@ -311,8 +356,9 @@ def bwd_workspace_bytes(B, H, T, W, K, dtype, Hkv=None, D=64) -> int:
     return int(lib().fibattn_bwd_workspace_bytes(B, H, T, D, W, K, code, ctypes.byref(o)))
 
 
+@_takes_stream
 def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, dedup=True,
-        out=None, lse=None, workspace=None, stream=None, kernel="auto", rotated_k=None, residuals=None,
+        out=None, lse=None, workspace=None, kernel="auto", rotated_k=None, residuals=None,
         round_offsets=False):
     """Forward pass.  q [B,H,T,64]; k, v [B,Hkv,T,64] (fp32 or bf16, CUDA,
     contiguous).  ``kernel``: "auto", "gather" or "mma".  ``round_offsets``:
@@ -345,12 +391,13 @@ def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, de
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
     _check(lib().fibattn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                              B, H, T, D, int(W), float(alpha), f.ctypes.data, len(f), code, ctypes.byref(o),
-                             workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+                             workspace.data_ptr(), workspace.numel(), _raw_stream(q.get_device())))
     return out, lse
 
 
+@_takes_stream
 def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_base=1e4, scale=None, dedup=True,
-        dq=None, dk=None, dv=None, dtheta=None, dd=None, workspace=None, stream=None, kernel="auto",
+        dq=None, dk=None, dv=None, dtheta=None, dd=None, workspace=None, kernel="auto",
         rotated_k=None, rung_grads=True, residuals=None, round_offsets=False):
     """Backward pass.  ``out``: the forward output (optional; enables the
     tensor-core query pass).  ``kernel``: "auto", "gather" or "mma".
@@ -391,23 +438,13 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
                              dtheta.data_ptr() if dtheta is not None else None,
                              dd.data_ptr() if dd is not None else None,
                              B, H, T, D, int(W), float(alpha), f.ctypes.data, K, code, ctypes.byref(o),
-                             workspace.data_ptr(), workspace.numel(), _stream_ptr(stream)))
+                             workspace.data_ptr(), workspace.numel(), _raw_stream(q.get_device())))
     if dtheta is None and dd is None:
         return dq, dk, dv, None, None
     return dq, dk, dv, (dtheta[:1] if dtheta is not None else None), (dd[:K] if dd is not None else None)
 
 
 # ------------------------------------------- loss head, gradient clipping ----
-
-# The current stream of a device by its index, without the Stream object that
-# torch.cuda.current_stream() builds (some 4 us of every call).
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
-    lambda index: torch.cuda.current_stream(index).cuda_stream
-
-
-def _stream_of(stream, index: int) -> int:
-    return int(stream.cuda_stream) if stream is not None else _raw_stream(index)
-
 
 def _check_xent(x, w, targets):
     if x.dim() != 2 or w.dim() != 2 or targets.dim() != 1:
@@ -431,7 +468,8 @@ def _f32_row(t, N, index, name):
     return t
 
 
-def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=None, workspace=None, stream=None):
+@_takes_stream
+def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=None, workspace=None):
     """Cross entropy of the linear head ``x @ w.T`` without forming it in
     memory (fibattn_linear_xent_fwd).  x [N, D], w [V, D] (fp32 or bf16, CUDA,
     contiguous), targets [N] int64; rows whose target is ``ignore_index`` have
@@ -448,12 +486,13 @@ def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=N
         workspace = torch.empty(need or 256, dtype=torch.uint8, device=x.device)
     _check(L.fibattn_linear_xent_fwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), loss.data_ptr(), lse.data_ptr(),
                                      N, D, V, ignore_index, code, workspace.data_ptr(), workspace.numel(),
-                                     _stream_of(stream, index)))
+                                     _raw_stream(index)))
     return loss, lse
 
 
+@_takes_stream
 def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=None, dw=None, want_dx: bool = True,
-                    want_dw: bool = True, workspace=None, stream=None):
+                    want_dw: bool = True, workspace=None):
     """Gradients of ``sum(dloss * loss)`` by x and w (fibattn_linear_xent_bwd).
     lse [N] from ``linear_xent_fwd`` of the same inputs; dloss [N] fp32.
     Returns (dx [N, D], dw [V, D]) in x's dtype; without ``want_dx`` or
@@ -474,7 +513,7 @@ def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=N
     _check(L.fibattn_linear_xent_bwd(x.data_ptr(), w.data_ptr(), targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(),
                                      dx.data_ptr() if want_dx else None, dw.data_ptr() if want_dw else None, N, D, V,
                                      ignore_index, code, workspace.data_ptr(), workspace.numel(),
-                                     _stream_of(stream, index)))
+                                     _raw_stream(index)))
     return dx, dw
 
 
@@ -500,18 +539,19 @@ def clip_grads(grads, max_norm: float, *, out=None, norm=None, workspace=None, s
     grads: contiguous CUDA tensors on one device, fp32 and bf16 in any mix, any
     offset into a buffer.  ``out``: tensors of the same sizes and dtypes, or
     None to clip in place.  Returns norm, a 0-dim fp32 tensor on the device."""
-    return _clip(list(grads), float(max_norm), out, norm, workspace, stream, True)
+    return _clip(list(grads), float(max_norm), None if out is None else list(out), norm, workspace, True, stream=stream)
 
 
 def grad_norm(grads, *, norm=None, workspace=None, stream=None):
     """The norm alone, as ``clip_grads`` computes it; nothing else is written."""
-    return _clip(list(grads), float("inf"), None, norm, workspace, stream, False)
+    return _clip(list(grads), float("inf"), None, norm, workspace, False, stream=stream)
 
 
-def _clip(grads, max_norm, out, norm, workspace, stream, scale):
+@_takes_stream
+def _clip(grads, max_norm, out, norm, workspace, scale):
     # (a model has hundreds of tensors: each is looked at with few calls, made by map)
     n = len(grads)
-    outs = grads if out is None else list(out)
+    outs = grads if out is None else out
     if len(outs) != n:
         raise ValueError("out must hold one tensor for each gradient")
     index = grads[0].get_device() if n else torch.cuda.current_device()
@@ -540,7 +580,7 @@ def _clip(grads, max_norm, out, norm, workspace, stream, scale):
     arrays = [ptrs, optrs, array.array("q", sizes), array.array("i", map(_CLIP_CODE.__getitem__, dtypes))]
     at = [a.buffer_info()[0] if a is not None else None for a in arrays]
     _check(L.fibattn_clip_grads(n, *at, max_norm, norm.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                                _stream_of(stream, index)))
+                                _raw_stream(index)))
     return norm
 
 
