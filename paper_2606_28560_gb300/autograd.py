@@ -27,6 +27,30 @@ def alpha_of_theta(theta: float) -> float:
     return float(B.alpha_schedule("learned", 1, theta=[float(theta)])[0])
 
 
+class _Once(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, what, n, *tensors):
+        ctx.what = what
+        return tuple(t.detach() for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.what} has no second derivatives: its gradients cannot be differentiated")
+
+
+def differentiable_once(what: str, grads, *inputs):
+    """What a backward of this package returns.  The kernels form gradients, not a
+    graph of them: with ``create_graph`` the gradients depend on the inputs by a
+    node that raises, where constants would drop the second order without a word.
+    (torch's once_differentiable raises only if the incoming gradient itself
+    depends on something; that of a plain sum or mean does not.)"""
+    if not torch.is_grad_enabled() or not any(t.requires_grad for t in inputs):
+        return grads
+    live = [g for g in grads if g is not None]
+    live = iter(_Once.apply(what, len(live), *live, *inputs))
+    return tuple(None if g is None else next(live) for g in grads)
+
+
 class FibAttentionFunction(torch.autograd.Function):
     """out = attention(q, k, v) over the window and the scaled-Fibonacci rungs
     at alpha = 0.5 + sigmoid(theta).  Gradients flow to q, k, v and theta

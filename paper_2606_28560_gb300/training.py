@@ -7,12 +7,14 @@ from __future__ import annotations
 import torch
 
 from . import binding as B
+from .autograd import differentiable_once
 
 
 class LinearCrossEntropyFunction(torch.autograd.Function):
     """loss[n] = log sum_v exp(x[n] . w[v]) - x[n] . w[targets[n]], 0 where
     targets[n] is ignore_index.  Neither the logits nor their gradient are kept
-    between the forward and the backward; gradients flow to x and w."""
+    between the forward and the backward; gradients flow to x and w, once: a
+    second derivative raises."""
 
     @staticmethod
     def forward(ctx, x, w, targets, ignore_index):
@@ -27,7 +29,7 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
         want_dx, want_dw = ctx.needs_input_grad[:2]
         dx, dw = B.linear_xent_bwd(x, w, targets, lse, dloss.contiguous(), ignore_index=ctx.ignore_index,
                                    want_dx=want_dx, want_dw=want_dw)
-        return dx, dw, None, None
+        return *differentiable_once("linear_cross_entropy", (dx, dw), x, w, dloss), None, None
 
 
 def linear_cross_entropy(x, w, targets, *, ignore_index: int = -100, reduction: str = "mean"):
