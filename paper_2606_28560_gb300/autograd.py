@@ -54,7 +54,8 @@ def differentiable_once(what: str, grads, *inputs):
 class FibAttentionFunction(torch.autograd.Function):
     """out = attention(q, k, v) over the window and the scaled-Fibonacci rungs
     at alpha = 0.5 + sigmoid(theta).  Gradients flow to q, k, v and theta
-    (a 0-dim tensor); offsets, W and the options are constants."""
+    (a 0-dim tensor), once: a second derivative raises.  offsets, W and the
+    options are constants."""
 
     @staticmethod
     def forward(ctx, q, k, v, theta, offsets, W, rope_base, scale, dedup, alpha=None):
@@ -88,7 +89,8 @@ class FibAttentionFunction(torch.autograd.Function):
                                    rope_base=rope_base, scale=scale, dedup=dedup, rotated_k=rk,
                                    residuals=res if res.numel() else None)
         dtheta = dth.reshape(()).to(device=tdev, dtype=tdtype)
-        return dq, dk, dv, dtheta, None, None, None, None, None, None
+        grads = differentiable_once("fib_attention", (dq, dk, dv, dtheta), out, dout)   # (out: of all inputs)
+        return *grads, None, None, None, None, None, None
 
 
 def fib_attention(q, k, v, theta, offsets=None, W: int = 8, *, rope_base: float = 1e4, scale=None,

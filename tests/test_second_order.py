@@ -58,3 +58,38 @@ def test_loss_head_with_a_gradient_that_depends_on_something(head):
     dx, = torch.autograd.grad((loss * scale).sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="second derivatives"):
         dx.square().sum().backward()
+
+
+@pytest.mark.parametrize("wants", ["q", "k", "v", "theta"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention(dtype, wants, monkeypatch):
+    # a stand-in that is linear in q, k, v and theta
+    monkeypatch.setattr(B, "fwd", lambda q, k, v, alpha, *a, **kw: ((q + 2 * k + 3 * v).detach() * alpha, q.detach()[..., 0].float()))
+    monkeypatch.setattr(B, "bwd", lambda q, k, v, lse, do, alpha, *a, **kw: tuple(
+        (c * alpha * do).detach() for c in (1, 2, 3)) + (torch.full((1,), 5.0), None))
+    monkeypatch.setattr(B, "residuals_like", lambda q, *a: torch.zeros(4, dtype=torch.uint8))
+    monkeypatch.setattr(fa.autograd, "alpha_of_theta", lambda theta: 1.0)
+    leaves = {n: torch.ones(1, 1, 3, 64, dtype=dtype) for n in "qkv"} | {"theta": torch.tensor(0.25)}
+    leaf = leaves[wants].requires_grad_()
+
+    def run():
+        return fa.fib_attention(leaves["q"], leaves["k"], leaves["v"], leaves["theta"], [1.0, 2.0], 8).float().sum()
+
+    want = {"q": 1.0, "k": 2.0, "v": 3.0, "theta": 5.0}[wants]
+    first, = torch.autograd.grad(run(), leaf)
+    assert (first == want).all() and not first.requires_grad
+    out = run()
+    graph, = torch.autograd.grad(out, leaf, create_graph=True)
+    assert torch.equal(graph, first)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        (out + graph.float().square().sum()).backward()
+
+
+def test_theta_may_change_between_forward_and_backward(monkeypatch):
+    test_attention(torch.float32, "theta", monkeypatch)
+    q, theta = torch.ones(1, 1, 3, 64, requires_grad=True), torch.tensor(0.25, requires_grad=True)
+    out = fa.fib_attention(q, q, q, theta, [1.0, 2.0], 8)
+    with torch.no_grad():
+        theta.add_(1.0)
+    out.sum().backward()
+    assert theta.grad == 5.0
