@@ -233,3 +233,13 @@ def test_a_call_on_another_stream_keeps_its_memory(name):
         torch.cuda.current_stream().wait_stream(other)
         assert all(torch.equal(a, b) for a, b in zip(flat([got]), want))
         del got
+
+
+def test_lse_and_dloss_at_any_offset(library, monkeypatch):
+    """Views 4 and 12 bytes off a boundary go to the library as aligned copies."""
+    lse, dloss = row("cuda:0"), row("cuda:0")
+    at = {id(lse): 260, id(dloss): 268}
+    monkeypatch.setattr(torch.Tensor, "data_ptr", lambda t: at.get(id(t), 4096))
+    fa.linear_xent_bwd(*xent("cuda:0"), lse, dloss)
+    (name, args), = library.calls
+    assert name == "fibattn_linear_xent_bwd" and args[3] == 4096 and args[4] == 4096
