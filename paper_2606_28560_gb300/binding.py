@@ -468,7 +468,7 @@ def _f32_row(t, N, index, name):
     return t
 
 
-def _aligned(t):
+def aligned(t):
     """t, or a copy of it where it does not start on a 16-byte boundary, which the
     library asks of every tensor (a view into a longer one may not)."""
     return t if t.data_ptr() % 16 == 0 else t.clone()
@@ -505,7 +505,7 @@ def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=N
     Returns (dx [N, D], dw [V, D]) in x's dtype; without ``want_dx`` or
     ``want_dw`` that product is not computed and None is returned for it."""
     N, D, V, code, index = _check_xent(x, w, targets)
-    lse, dloss = _aligned(_f32_row(lse, N, index, "lse")), _aligned(_f32_row(dloss, N, index, "dloss"))
+    lse, dloss = aligned(_f32_row(lse, N, index, "lse")), aligned(_f32_row(dloss, N, index, "dloss"))
     if not (want_dx or want_dw):
         raise ValueError("neither dx nor dw is wanted")
     dx = None if not want_dx else torch.empty_like(x) if dx is None else _grad_like(dx, x)

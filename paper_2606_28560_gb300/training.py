@@ -34,16 +34,18 @@ class LinearCrossEntropyFunction(torch.autograd.Function):
 
 def linear_cross_entropy(x, w, targets, *, ignore_index: int = -100, reduction: str = "mean"):
     """Cross entropy of the logits ``x @ w.T``.  x [..., D] hidden states, w
-    [V, D] head weights of the same dtype (fp32 or bf16, CUDA, contiguous),
-    targets [...] int64.  ``reduction``: "mean" over the rows with a target (NaN
+    [V, D] head weights of the same dtype (fp32 or bf16, CUDA), targets [...]
+    int64; views are taken as they are where they are contiguous and start on a
+    16-byte boundary, and copied otherwise.  ``reduction``: "mean" over the rows with a target (NaN
     when there is none, as the mean of nothing is), "sum", or "none" (the shape
     of targets).  The loss is fp32."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be 'mean', 'sum' or 'none'")
     if x.shape[:-1] != targets.shape:
         raise ValueError("targets must have x's shape without its last dimension")
-    flat = targets.reshape(-1)
-    loss = LinearCrossEntropyFunction.apply(x.reshape(-1, x.shape[-1]), w, flat, int(ignore_index))
+    flat = targets.reshape(-1).contiguous()
+    x, w = (B.aligned(t.contiguous()) for t in (x.reshape(-1, x.shape[-1]), w))
+    loss = LinearCrossEntropyFunction.apply(x, w, flat, int(ignore_index))
     if reduction == "none":
         return loss.reshape(targets.shape)
     if reduction == "sum":
