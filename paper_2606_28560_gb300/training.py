@@ -57,10 +57,25 @@ def clip_grad_norm_(parameters, max_norm: float) -> torch.Tensor:
     """Clips the gradients of ``parameters`` (an iterable, or one tensor) to a
     global norm of ``max_norm`` in place; parameters without a gradient are left
     out.  Returns the norm before clipping, a 0-dim fp32 tensor on the device;
-    nothing waits for the GPU."""
+    nothing waits for the GPU, unless gradients are on the CPU (that of a theta
+    kept there): those are clipped with the others, through copies."""
     if torch.is_tensor(parameters):
         parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]
     if not grads:
         return torch.zeros(())
-    return B.clip_grads(grads, max_norm)
+    try:
+        return B.clip_grads(grads, max_norm)
+    except ValueError:                            # nothing was launched; not all can be passed as they are
+        return _clip_through_copies(grads, max_norm)
+
+
+@torch.no_grad()
+def _clip_through_copies(grads, max_norm):
+    device = next((g.device for g in grads if g.is_cuda), "cpu")
+    passed = [g.to(device) for g in grads]        # (the tensor itself where it is there already)
+    norm = B.clip_grads(passed, max_norm)
+    for g, p in zip(grads, passed):
+        if p is not g:
+            g.copy_(p)
+    return norm

@@ -58,3 +58,61 @@ def test_views(view, dtype):
     assert torch.equal(loss, want)
     got = cut(whole_x.grad, whole_w.grad)
     assert torch.equal(got[0], x.grad) and torch.equal(got[1], w.grad)
+
+
+# The norm's relative error: squares in fp32 runs of at most 258 roundings, half of that in the root, and
+# its own rounding; an output has the coefficient's and its own (bf16: 2^-9) on top.
+NORM_TOL = 131 * 2.0 ** -24
+
+
+def parameters_with(grads):
+    out = []
+    for g in grads:
+        p = torch.nn.Parameter(torch.zeros_like(g))
+        p.grad = g
+        out.append(p)
+    return out
+
+
+def check_clipped(grads, max_norm):
+    """Clips, and compares with the definition in 64 bits."""
+    keep = [g.detach().clone().double().cpu() for g in grads]
+    total = sum(float(k.square().sum()) for k in keep) ** 0.5
+    coef = min(1.0, max_norm / (total + 1e-6))
+    params = parameters_with(grads)
+    norm = fa.clip_grad_norm_(iter(params), max_norm)
+    assert norm.dtype == torch.float32 and norm.shape == () and abs(float(norm) - total) <= NORM_TOL * total
+    for p, g, k in zip(params, grads, keep):
+        assert p.grad is g
+        tol = 2.0 ** -8 if g.dtype == torch.bfloat16 else NORM_TOL + 2.0 ** -22
+        assert ((g.double().cpu() - k * coef).abs() <= tol * (k * coef).abs() + 1e-37).all()
+    return norm
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("max_norm", [0.5, 1e6])
+def test_clipping_with_gradients_on_the_cpu(max_norm):
+    """A model's layers on the GPU and its thetas on the CPU."""
+    g = torch.Generator().manual_seed(4)
+    grads = [torch.randn(33, 65, generator=g).cuda(), torch.randn((), generator=g), torch.randn(1000, generator=g).bfloat16().cuda(),
+             torch.randn((), generator=g), torch.randn(7, generator=g)]
+    assert check_clipped(grads, max_norm).is_cuda
+
+
+@pytest.mark.gpu
+def test_clipping_a_model_with_its_thetas_on_the_cpu():
+    layers = [fa.FibAttention(W=8, theta=0.1 * i) for i in range(2)]
+    up = torch.nn.Linear(64, 64, device="cuda")
+    q = torch.randn(1, 2, 50, 64, generator=torch.Generator().manual_seed(5)).cuda()
+    x = up(q)
+    for a in layers:
+        x = a(x, x, x)
+    x.square().sum().backward()
+    params = [*up.parameters(), *(a.theta for a in layers)]
+    assert not layers[0].theta.is_cuda and layers[0].theta.grad is not None
+    check_clipped([p.grad for p in params], 0.25)
+
+
+def test_clipping_on_the_cpu_alone_is_refused():
+    with pytest.raises(ValueError, match="CUDA"):
+        fa.clip_grad_norm_(parameters_with([torch.ones(3)]), 1.0)
