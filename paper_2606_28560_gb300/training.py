@@ -58,7 +58,8 @@ def clip_grad_norm_(parameters, max_norm: float) -> torch.Tensor:
     global norm of ``max_norm`` in place; parameters without a gradient are left
     out.  Returns the norm before clipping, a 0-dim fp32 tensor on the device;
     nothing waits for the GPU, unless gradients are on the CPU (that of a theta
-    kept there): those are clipped with the others, through copies."""
+    kept there): those are clipped with the others, through copies, as are those
+    whose values do not fill their memory (slices)."""
     if torch.is_tensor(parameters):
         parameters = [parameters]
     grads = [p.grad for p in parameters if p.grad is not None]
@@ -67,15 +68,26 @@ def clip_grad_norm_(parameters, max_norm: float) -> torch.Tensor:
     try:
         return B.clip_grads(grads, max_norm)
     except ValueError:                            # nothing was launched; not all can be passed as they are
-        return _clip_through_copies(grads, max_norm)
+        return _clip_elsewhere(grads, max_norm)
+
+
+def _in_memory_order(g):
+    """g with its dimensions in the order of its memory: contiguous if g is any
+    permutation of a contiguous tensor (the norm does not care for the order)."""
+    return g.permute(sorted(range(g.dim()), key=g.stride, reverse=True))
 
 
 @torch.no_grad()
-def _clip_through_copies(grads, max_norm):
+def _clip_elsewhere(grads, max_norm):
     device = next((g.device for g in grads if g.is_cuda), "cpu")
-    passed = [g.to(device) for g in grads]        # (the tensor itself where it is there already)
+    passed, copied = [], []
+    for g in grads:
+        p = _in_memory_order(g)
+        if p.device != device or not p.is_contiguous():
+            p = g.to(device).contiguous()
+            copied.append((g, p))
+        passed.append(p)
     norm = B.clip_grads(passed, max_norm)
-    for g, p in zip(grads, passed):
-        if p is not g:
-            g.copy_(p)
+    for g, p in copied:
+        g.copy_(p)
     return norm

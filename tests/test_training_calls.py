@@ -116,3 +116,46 @@ def test_clipping_a_model_with_its_thetas_on_the_cpu():
 def test_clipping_on_the_cpu_alone_is_refused():
     with pytest.raises(ValueError, match="CUDA"):
         fa.clip_grad_norm_(parameters_with([torch.ones(3)]), 1.0)
+
+
+LAYOUTS = {
+    "transposed": lambda t: t(40, 70).t(),
+    "channels last": lambda t: t(2, 5, 6, 3).permute(0, 3, 1, 2),
+    "permuted": lambda t: t(3, 1, 4, 9).permute(2, 0, 3, 1),
+    "columns": lambda t: t(40, 70)[:, 3:20],
+    "every other": lambda t: t(501)[::2],
+    "none": lambda t: t(0, 7).t(),
+    "on the CPU, transposed": lambda t: t(4, 7).cpu().t(),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [0.5, 1e6])
+@pytest.mark.parametrize("layout", list(LAYOUTS))
+def test_clipping_gradients_of_any_layout(layout, max_norm, dtype):
+    g = torch.Generator().manual_seed(6)
+    whole = []
+
+    def make(*shape):
+        whole.append(torch.randn(*shape, generator=g).to(dtype).cuda())
+        return whole[-1]
+
+    grads = [make(100), LAYOUTS[layout](make), make(3, 5)]
+    base = grads[1]._base if grads[1]._base is not None else grads[1]
+    outside = torch.ones_like(base, dtype=torch.bool)
+    torch.as_strided(outside, grads[1].shape, grads[1].stride(), grads[1].storage_offset()).fill_(False)
+    keep = base.clone()
+    check_clipped(grads, max_norm)
+    assert torch.equal(base[outside], keep[outside])
+
+
+@pytest.mark.gpu
+def test_clipping_gradients_in_the_order_of_their_memory_makes_no_copies(monkeypatch):
+    """A permutation of contiguous memory is clipped where it lies."""
+    seen = []
+    real = fa.training.B.clip_grads
+    monkeypatch.setattr(fa.training.B, "clip_grads", lambda g, m: seen.append([t.data_ptr() for t in g]) or real(g, m))
+    grads = [torch.randn(40, 70, device="cuda").t(), torch.randn(2, 5, 6, 3, device="cuda").permute(0, 3, 1, 2)]
+    check_clipped(grads, 0.5)
+    assert seen[-1] == [t.data_ptr() for t in grads]
