@@ -62,9 +62,10 @@ def clip_grad_norm_(parameters, max_norm: float) -> torch.Tensor:
     whose values do not fill their memory (slices)."""
     if torch.is_tensor(parameters):
         parameters = [parameters]
+    parameters = list(parameters)
     grads = [p.grad for p in parameters if p.grad is not None]
-    if not grads:
-        return torch.zeros(())
+    if not grads:                                 # nothing to clip: 0, where the parameters are
+        return torch.zeros((), device=next((p.device for p in parameters if p.device.type != "cpu"), "cpu"))
     try:
         return B.clip_grads(grads, max_norm)
     except ValueError:                            # nothing was launched; not all can be passed as they are

@@ -159,3 +159,14 @@ def test_clipping_gradients_in_the_order_of_their_memory_makes_no_copies(monkeyp
     grads = [torch.randn(40, 70, device="cuda").t(), torch.randn(2, 5, 6, 3, device="cuda").permute(0, 3, 1, 2)]
     check_clipped(grads, 0.5)
     assert seen[-1] == [t.data_ptr() for t in grads]
+
+
+def test_the_norm_of_no_gradients_is_where_the_parameters_are():
+    def device_of(*parameters):
+        norm = fa.clip_grad_norm_(iter(parameters), 1.0)
+        assert norm.shape == () and norm.dtype == torch.float32
+        return norm.device.type
+
+    cpu, meta = torch.nn.Parameter(torch.zeros(3)), torch.nn.Parameter(torch.zeros(3, device="meta"))   # meta: any device but the CPU
+    assert device_of() == "cpu" and device_of(cpu) == "cpu" and device_of(cpu, meta) == "meta"
+    assert float(fa.clip_grad_norm_(cpu, 1.0)) == 0.0
