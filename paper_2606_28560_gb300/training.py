@@ -36,13 +36,17 @@ def linear_cross_entropy(x, w, targets, *, ignore_index: int = -100, reduction: 
     """Cross entropy of the logits ``x @ w.T``.  x [..., D] hidden states, w
     [V, D] head weights of the same dtype (fp32 or bf16, CUDA), targets [...]
     int64; views are taken as they are where they are contiguous and start on a
-    16-byte boundary, and copied otherwise.  ``reduction``: "mean" over the rows with a target (NaN
+    16-byte boundary, and copied otherwise.  Where x and w differ under bf16
+    autocast (hidden states of the layers, an fp32 head), the fp32 one is cast, as
+    torch's own linear does.  ``reduction``: "mean" over the rows with a target (NaN
     when there is none, as the mean of nothing is), "sum", or "none" (the shape
     of targets).  The loss is fp32."""
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be 'mean', 'sum' or 'none'")
     if x.shape[:-1] != targets.shape:
         raise ValueError("targets must have x's shape without its last dimension")
+    if x.dtype != w.dtype and torch.is_autocast_enabled("cuda") and torch.get_autocast_dtype("cuda") == torch.bfloat16:
+        x, w = (t.bfloat16() if t.dtype == torch.float32 else t for t in (x, w))
     flat = targets.reshape(-1).contiguous()
     x, w = (B.aligned(t.contiguous()) for t in (x.reshape(-1, x.shape[-1]), w))
     loss = LinearCrossEntropyFunction.apply(x, w, flat, int(ignore_index))

@@ -170,3 +170,29 @@ def test_the_norm_of_no_gradients_is_where_the_parameters_are():
     cpu, meta = torch.nn.Parameter(torch.zeros(3)), torch.nn.Parameter(torch.zeros(3, device="meta"))   # meta: any device but the CPU
     assert device_of() == "cpu" and device_of(cpu) == "cpu" and device_of(cpu, meta) == "meta"
     assert float(fa.clip_grad_norm_(cpu, 1.0)) == 0.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp32", ["x", "w"])
+def test_types_that_differ_under_autocast(fp32):
+    x, w, t = head(20, 64, 50, torch.bfloat16)
+    x, w = (v.float().requires_grad_() if n == fp32 else v.requires_grad_() for n, v in (("x", x), ("w", w)))
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        loss = fa.linear_cross_entropy(x, w, t)
+    loss.backward()
+    x2, w2 = (v.detach().bfloat16().requires_grad_() for v in (x, w))
+    want = fa.linear_cross_entropy(x2, w2, t)
+    want.backward()
+    assert torch.equal(loss, want) and x.grad.dtype == x.dtype and w.grad.dtype == w.dtype
+    assert torch.equal(x.grad.float(), x2.grad.float()) and torch.equal(w.grad.float(), w2.grad.float())
+    for context in (torch.autocast("cuda", dtype=torch.float16), torch.autocast("cuda", enabled=False)):
+        with context, pytest.raises(ValueError, match="one dtype"):
+            fa.linear_cross_entropy(x, w, t)
+
+
+@pytest.mark.gpu
+def test_fp32_stays_fp32_under_autocast():
+    x, w, t = head(20, 64, 50, torch.float32)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        loss = fa.linear_cross_entropy(x, w, t)
+    assert torch.equal(loss, fa.linear_cross_entropy(x, w, t))
