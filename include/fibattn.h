@@ -330,11 +330,13 @@ int fibattn_linear_xent_bwd(const void* x, const void* w, const long long* targe
  * buffer will do).  outs == NULL: the norm alone.  outs[i] == grads[i] clips
  * in place (and, with norm below max_norm, writes nothing); otherwise an out
  * may not overlap a grad or another out.  max_norm >= 0 (infinity: no
- * clipping).  norm: device, 1 float.  A norm that is not finite passes into
- * the outputs by the formula above (NaN, or 0 with NaN where the infinities
- * were); the caller that wants to skip such a step looks at norm.  Squares
- * are summed in fp32 in runs of at most 128 values and in fp64 beyond; the
- * result does not depend on timing. */
+ * clipping).  norm: device, 1 float.  It is not finite if a value is not, or if
+ * it is itself beyond fp32; it then passes into the outputs by the formula above
+ * (NaN, or 0 with NaN where the infinities were), and the caller that wants to
+ * skip such a step looks at norm.  Squares are summed in fp32 in runs of at most
+ * 129 values, four runs to a thread are added in fp32, and all beyond in fp64;
+ * values whose squares leave fp32's range (above 1.8e19, tiny ones) are squared
+ * in fp64.  The result does not depend on timing. */
 size_t fibattn_clip_grads_workspace_bytes(int n);
 
 int fibattn_clip_grads(int n, const void* const* grads, void* const* outs,

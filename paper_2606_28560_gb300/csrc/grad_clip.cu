@@ -72,20 +72,48 @@ template <typename T> struct Vector {
 
 constexpr int kNormBatch = 8, kClipBatch = 4;   // vectors that a thread has under way at a time
 
-template <typename T> __device__ __forceinline__ float sum_squares(const T* p, int n) {
+// The same values as sum_squares takes with this thread, in 64 bits.
+template <typename T> __device__ __noinline__ double sum_squares_wide(const T* p, int n) {
+    using V = Vector<T>;
+    const int head = head_of(p, n), vectors = (n - head) / V::kValues, tail = head + vectors * V::kValues;
+    double s = 0.0;
+    const auto add = [&](float x) { s = fma((double)x, (double)x, s); };
+    if ((int)threadIdx.x < head) add(to_f(p[threadIdx.x]));
+    if (tail + (int)threadIdx.x < n) add(to_f(p[tail + threadIdx.x]));
+    for (int i = threadIdx.x; i < vectors; i += kThreads) {
+        V v;
+        v.u = __ldg(reinterpret_cast<const uint4*>(p + head) + i);
+#pragma unroll
+        for (int j = 0; j < V::kValues; ++j) add(v.get(j));
+    }
+    return s;
+}
+
+// Squares leave fp32's range long before the values do (above 1.8e19, below 1e-22).
+// A thread whose sum has done so, or is so small that what was lost below 2^-149
+// may count (129 terms in a run: 2^-143, 2^-33 of the limit), takes its values
+// again in 64 bits; one with zeros alone does not.
+constexpr float kLeastSum = 0x1p-110f;
+
+template <typename T> __device__ __forceinline__ double sum_squares(const T* p, int n) {
     using V = Vector<T>;
     const int head = head_of(p, n), vectors = (n - head) / V::kValues, tail = head + vectors * V::kValues;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
+    unsigned bits = 0;                     // of all values
     if ((int)threadIdx.x < head) {         // (head and tail hold fewer than 8 values)
         const float x = to_f(p[threadIdx.x]);
         s[0] = x * x;
+        bits |= __float_as_uint(x) << 1;
     }
     if (tail + (int)threadIdx.x < n) {
         const float x = to_f(p[tail + threadIdx.x]);
         s[1] = x * x;
+        bits |= __float_as_uint(x) << 1;
     }
+    unsigned body_bits = 0;
     const uint4* body = reinterpret_cast<const uint4*>(p + head);
     const auto add = [&](const V& v) {
+        body_bits |= (v.u.x | v.u.y) | (v.u.z | v.u.w);
 #pragma unroll
         for (int j = 0; j < V::kValues; ++j) {
             const float x = v.get(j);
@@ -108,7 +136,10 @@ template <typename T> __device__ __forceinline__ float sum_squares(const T* p, i
 #pragma unroll
         for (int k = 0; k < kNormBatch; ++k) add(v[k]);
     }
-    return (s[0] + s[1]) + (s[2] + s[3]);
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    bits |= body_bits & (sizeof(T) == 4 ? 0x7fffffffu : 0x7fff7fffu);
+    if (sum >= kLeastSum && sum < INFINITY || bits == 0) return sum;
+    return sum_squares_wide(p, n);
 }
 
 __device__ double block_sum(double s, double* red) {

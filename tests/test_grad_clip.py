@@ -173,6 +173,44 @@ def test_parameters():
     assert m[2].weight.grad is None
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("scale", [1e20, 1e30, 1e-18, 1e-24, 1e-34])
+@pytest.mark.parametrize("offset", [0, 3])
+def test_values_whose_squares_leave_fp32(offset, scale, dtype):
+    """The norm of finite values is theirs, and large ones are clipped to it, though
+    no square of theirs is an fp32 number.  1e-18: squares are numbers, sums of a
+    thread lie below the limit of the second way."""
+    grads, flats = tensors([(n, dtype) for n in (1, 7, 4099, 70001)], 9, offset, scale)
+    keep = [g.clone() for g in grads]
+    want, coef = truth(grads, 1.0)
+    norm = fa.clip_grads(grads, 1.0)
+    assert abs(float(norm) - want) <= NORM_TOL * want and guards_hold(flats)
+    close(grads, keep, coef)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("at", [0, 1, 8, 2047, 40000, 69999, 70000])
+def test_one_large_value_among_ordinary_ones(at, dtype):
+    a = torch.randn(70001, generator=torch.Generator().manual_seed(at)).to(dtype).cuda()
+    a[at] = 3e25
+    keep, (want, coef) = a.clone(), truth([a], 1.0)
+    norm = fa.clip_grads([a], 1.0)
+    assert abs(float(norm) - want) <= NORM_TOL * want
+    close([a], [keep], coef)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F, H])
+def test_zeros_with_a_tiny_value(dtype):
+    a = torch.zeros(200_000, dtype=dtype, device="cuda")
+    a[::2] = -0.0
+    assert float(fa.grad_norm([a])) == 0.0
+    a[123_457] = 2.0 ** -100
+    assert float(fa.grad_norm([a])) == 2.0 ** -100
+
+
 # -------------------------------------------------------------- refusals ----
 
 @pytest.fixture(scope="module", autouse=True)
