@@ -12,11 +12,12 @@
 // no exchange.  Two accumulators of 256 columns alternate (or, for products
 // wider than 256 columns, are two halves of a tile of 512 that shares A).
 //
-// The tensor core truncates as it accumulates (some 2e-8 of the running sum
-// for each 16 of depth), so a long depth is cut into runs whose sums are added
-// in registers: 512 deep for bf16 logits, whose loss and lse are fp32 results.
-// The products of bf16 gradients, rounded to 8 bits at the end, are cut only
-// where their depth passes 2^17.
+// The tensor core truncates as it accumulates (for each 16 of depth it loses 2e-8
+// of a sum 512 deep, 9e-8 of one 2^15 deep or more, all terms of one sign), so a long
+// depth is cut into runs whose sums are added in fp32: 512 deep for bf16 logits,
+// whose loss and lse are fp32 results, and 2^15 for the products of bf16 gradients,
+// rounded to 8 bits at the end (2^18 rows of positive terms: dw 1.8e-4 low, a tenth
+// of such a rounding; 1.3e-3 uncut; at no cost in time).
 // fp32 operands are sums of three bf16 planes ("wide" below: several planes,
 // runs of 128, CUDA's expf).
 #include <algorithm>
@@ -34,6 +35,7 @@ constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr unsigned kOperandBytes = 16384;          // 128 rows x 64 deep, bf16
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kDeepest = 1 << 15;                  // of products of bf16 values: depth that the tensor core sums alone
 
 enum Mode { kForward, kGradient, kProducts };
 
@@ -317,7 +319,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
 
     const int combos = WIDE ? a.combos : 1;        // products of planes for one of values
     // Depth of a run (chunks of 64) whose sums stay in the tensor core.
-    constexpr int kRun = WIDE ? 2 : MODE != kProducts ? 8 : NB == 1 ? 2048 : 1 << 30;
+    constexpr int kRun = WIDE ? 2 : MODE != kProducts ? 8 : kDeepest / 64;
 
     if (warp < 4) {
         tc5::registers_down<56>();
@@ -508,12 +510,15 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 if (target == kBad && a.v0 + it.n0 == 0 && half == 0) raise_status(a.p.status, kStatusTarget);
             }
             float acc[128];
+            const int runs = (it.k1 - it.k0 + kRun - 1) / kRun;
+            // A thread has registers for one block's sums: with two blocks the runs of a
+            // tile are added up in memory, a turn over the blocks for each run.
+            const int turns = NB == 2 ? runs : 1;
 #pragma unroll 1
-            for (int b = 0; b < NB; ++b) {
-                const int runs = (it.k1 - it.k0 + kRun - 1) / kRun;
+            for (int turn = 0, b = 0; turn < turns; turn += b == NB - 1, b = (b + 1) % NB) {
                 unsigned n_run = run;
 #pragma unroll 1
-                for (int r = 0; r < runs; ++r, ++n_run) {
+                for (int r = 0; r < (NB == 2 ? 1 : runs); ++r, ++n_run) {
                     const unsigned buf = NB == 2 ? (unsigned)b : n_run & 1u, use = NB == 2 ? n_run : n_run >> 1;
                     ok = ok && tc5::wait_parity(acc_full + 8 * buf, use & 1u);
                     if (!ok) continue;
@@ -651,14 +656,17 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 } else if constexpr (MODE == kProducts) {
                     const int end = min(a.out_cols, it.n0 + a.tile_cols);
                     if (c0 >= end) continue;                 // (uniform over the warp)
-                    if (it.whole) {
-                        write_product<WIDE, 128>(a, it.problem, row, c0, end - c0, out_scale, acc);
-                    } else {
-                        float* mine = slot_at<NB>(a, 2 * cluster + (it.begins ? 0 : 1), (int)rank, b, ew) + lane;
-                        if (row < a.prob[it.problem].rows) {
+                    float* mine = slot_at<NB>(a, 2 * cluster + (it.begins ? 0 : 1), (int)rank, b, ew) + lane;
+                    const bool in = row < a.prob[it.problem].rows;
+                    if (NB == 2 && turn > 0 && in) {         // the runs before, this thread's own
 #pragma unroll
-                            for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
-                        }
+                        for (int j = 0; j < 128; ++j) acc[j] += __ldcg(mine + 32 * j);
+                    }
+                    if (it.whole && turn == turns - 1) {
+                        write_product<WIDE, 128>(a, it.problem, row, c0, end - c0, out_scale, acc);
+                    } else if (in) {
+#pragma unroll
+                        for (int j = 0; j < 128; ++j) __stcg(mine + 32 * j, acc[j]);
                     }
                 }
             }
@@ -1044,10 +1052,9 @@ BwdPlan plan_backward(int N, int D, int V, bool bf16) {
     plan_operands(N, D, bf16, &f.pack, &f.planes, &f.depth);
     f.wide = several_planes(N, D, V, bf16);
     f.g_planes = f.wide ? 3 : 1;
-    // (a tile of two blocks keeps its sums in the tensor core over its whole depth)
-    f.blocks = !f.wide && D > 256 && std::max(N, V) <= (1 << 18) ? 2 : 1;
     const long long fit = (512ll << 20) / (2ll * f.g_planes * std::max(N, 1)) / 256 * 256;
     f.cols = (int)std::min<long long>(V, std::max(256ll, fit));
+    f.blocks = !f.wide && D > 256 ? 2 : 1;
     f.ldg = (f.cols + 7) / 8 * 8;
     size_t off = 0;
     const auto take = [&](size_t n) { const size_t at = off; off += up256(n); return at; };

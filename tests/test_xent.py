@@ -322,6 +322,43 @@ def test_depth_beyond_a_run_of_the_tensor_core():
 
 
 @pytest.mark.gpu
+def test_depth_of_the_products_beyond_a_run():
+    """dw over 2^18 rows, all terms positive: what truncation takes from a sum grows
+    with the depth that the tensor core sums alone, by 2.2e-8 (sums 512 deep) to
+    4.3e-8 (4096 deep) of the sum for each 16.  Runs of 2^17 keep it below
+    2^13 * 4.3e-8; the roundings of g and of dw go both ways and leave the median."""
+    N, D, V = 1 << 18, 8192, 1024
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x = torch.rand(N, D, generator=g, device="cuda", dtype=torch.bfloat16).add_(0.5)
+    w = (torch.randn(V, D, generator=g, device="cuda") * 0.038).bfloat16()
+    t = torch.zeros(N, dtype=torch.int64, device="cuda")
+    dl = torch.rand(N, generator=g, device="cuda") * 0.5 + 0.5
+    lse = fa.linear_xent_fwd(x, w, t)[1]
+    dw = fa.linear_xent_bwd(x, w, t, lse, dl)[1]
+    some = torch.arange(7, V, 32, device="cuda")
+    want = torch.zeros(len(some), D, dtype=torch.float64, device="cuda")
+    for at in range(0, N, 1 << 14):
+        rows = slice(at, at + (1 << 14))
+        xd = x[rows].double()
+        want += (torch.exp(xd @ w[some].double().t() - lse[rows, None].double()) * dl[rows, None]).t() @ xd
+    off = float(((dw[some].double() - want) / want).median())
+    assert abs(off) <= 2 ** 13 * 4.3e-8, off
+
+
+# deep products over tiles of one block and of two, whole and cut, with a ragged last run
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", [(70_001, 300, 515), (33_000, 1030, 700), (100_000, 100, 300), (300, 520, 70_001), (270, 2056, 40_000),
+                                  (40_000, 2100, 2000)], ids=lambda s: "x".join(map(str, s)))
+def test_products_in_several_runs(size):
+    check(*make(*size, torch.bfloat16, seed=sum(size)))
+
+
+@pytest.mark.gpu
+def test_pieces_of_a_vocabulary_above_2_18():
+    check(*make(2100, 264, 270_001, torch.bfloat16, 23))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_writes_only_its_outputs(dtype):
     """Outputs and workspace lie between guards of a known pattern."""
