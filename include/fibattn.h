@@ -289,12 +289,17 @@ int fibattn_fwd_noalloc(const void* q, const void* k, const void* v, void* out, 
  * loss is NaN, it adds nothing to the gradients, and status bit 2 is set
  * (fibattn_check_status).  Limits: 0 <= N <= 2^24, 1 <= D <= 8192,
  * 1 <= V <= 2^24.  N == 0 launches nothing but the zeroing of dw.
- * Every product is accumulated in fp32; results do not depend on timing.  fp32
- * operands keep their 24 bits (on the tensor cores as sums of three bf16 values),
- * in calls of three to 32 rows 22 of them (sums of two tf32 values); with bf16 I/O
- * and more rows than that g is rounded to bf16 between the two products of the
- * gradient (relative to the largest |dloss|, so that equal weights round nothing),
- * as a bf16 tensor between two library calls would be.
+ * Every product is accumulated in fp32; results do not depend on timing.  How many
+ * bits its operands keep follows from the sizes, alike in forward and backward:
+ *   N <= 2, or N <= 4 and V*D <= 2^22, with D <= 2048: all of them;
+ *   other calls of few rows -- N <= 32 in fp32, and in bf16 if V*D <= 2^22, else
+ *     N <= 16 if D <= 1024, N <= 8 if not: fp32 operands, and g between the two
+ *     products of the gradient, 22 bits (sums of two tf32 values);
+ *   all others: fp32 operands and their g 24 bits (sums of three bf16 values).
+ *     With bf16 I/O g is rounded to bf16 (relative to the largest |dloss|, so that
+ *     equal weights round nothing), as a bf16 tensor between two library calls would
+ *     be; it keeps 24 bits in calls of at most 2^26 products, N and V counted up to
+ *     multiples of 256.
  * As in any matrix product, an ignored row of x that holds an infinity or NaN
  * still reaches dw as 0 * NaN.
  * ------------------------------------------------------------------------- */
@@ -310,7 +315,10 @@ int fibattn_linear_xent_fwd(const void* x, const void* w, const long long* targe
  *   g[n][v] = dloss[n] (exp(s[n][v] - lse[n]) - [v == targets[n]]), 0 for ignored rows;
  *   dx = g w [N][D],  dw = g^T x [V][D], in `dtype`, overwritten.
  * The logits are formed again, a piece of the vocabulary at a time; g of one
- * piece is held in the workspace (at most 512 MiB of it).  dx or dw may be NULL
+ * piece is held in the workspace: at most 512 MiB of it, or 256 columns where
+ * those are more (512 N bytes in bf16, 1536 N in fp32).  Calls of few rows (the
+ * second kind above) hold g of all columns, N rounded up to 8, 16 or 32, in fp32
+ * (at most 128 V bytes).  dx or dw may be NULL
  * when only the other is wanted (a frozen head; a probe on frozen states).  They
  * may not alias each other, an input or the workspace. */
 size_t fibattn_linear_xent_bwd_workspace_bytes(int N, int D, int V, int dtype);

@@ -345,6 +345,13 @@ def test_depth_of_the_products_beyond_a_run():
     assert abs(off) <= 2 ** 13 * 4.3e-8, off
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_millions_of_rows(dtype):
+    # more rows than g of 256 columns fits in 512 MiB
+    check(*make((1 << 21) + 5, 8, 520, TYPES[dtype], 24))
+
+
 # deep products over tiles of one block and of two, whole and cut, with a ragged last run
 @pytest.mark.gpu
 @pytest.mark.parametrize("size", [(70_001, 300, 515), (33_000, 1030, 700), (100_000, 100, 300), (300, 520, 70_001), (270, 2056, 40_000),
@@ -504,6 +511,34 @@ def test_workspace_sizes():
     # far below the fp32 logits of the same call
     assert 0 < f(16384, 512, 32768, 1) < 16384 * 32768 * 4 // 64
     assert 0 < b(16384, 512, 32768, 1) < 16384 * 32768 * 4 // 3
+
+
+MIB = 1 << 20
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [40, 20_000, 1 << 20, 1 << 21, 1 << 24])
+def test_workspace_of_many_rows(N, dtype):
+    """What the header says of g: 512 MiB or 256 columns, whichever is more.  The
+    rest: both operands as planes, dx over the pieces, sums over a part of a depth."""
+    D, V, code, planes = 64, 32768, list(TYPES).index(dtype), 3 if dtype == "f32" else 1
+    need = B.lib().fibattn_linear_xent_bwd_workspace_bytes(N, D, V, code)
+    g = 2 * planes * N * V
+    if g > 512 * MIB:
+        g = max(512 * MIB, 256 * 2 * planes * N)
+    rest = (2 * planes * (N + V) * D if dtype == "f32" else 0) + 4 * N * D
+    assert g * 0.99 <= need <= g + rest + 128 * MIB
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N,rows", [(3, 8), (8, 8), (9, 16), (17, 32), (32, 32)])
+def test_workspace_of_few_rows(N, rows, dtype):
+    """g of all columns in fp32, where the call is one of few rows."""
+    D, V = 64, 1 << 24
+    need = B.lib().fibattn_linear_xent_bwd_workspace_bytes(N, D, V, list(TYPES).index(dtype))
+    few = dtype == "f32" or N <= 16                # bf16 over a large head, D <= 1024
+    g = 4 * rows * V if few else 512 * MIB
+    assert g * 0.99 <= need <= g + (1 << 30 if not few else 64 * MIB)
 
 
 def test_python_checks():
