@@ -35,6 +35,10 @@ constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr unsigned kOperandBytes = 16384;          // 128 rows x 64 deep, bf16
 constexpr float kLog2e = 1.4426950408889634f;
+// exp(s - m) goes as exp2(s log2e - m log2e) in one FMA.  Beyond this the second term
+// may overflow, and the difference is taken first: a tile's row whose tokens are all
+// masked by the lowest bf16 value has such an m.
+constexpr float kFarLogit = 0x1p126f;
 constexpr int kDeepest = 1 << 15;                  // of products of bf16 values: depth that the tensor core sums alone
 
 enum Mode { kForward, kGradient, kProducts };
@@ -486,7 +490,7 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
         Item it;
         unsigned run = 0;
         bool ok = true;
-        float m = -INFINITY, l = 0.f, z = 0.f, z2 = 0.f, dl = 0.f;
+        float m = -INFINITY, l = 0.f, z = 0.f, dl = 0.f;
         int target = kIgnored;
         float out_scale = 1.f;
         if (MODE == kGradient) {
@@ -506,7 +510,6 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                 target = row < a.p.N ? target_column(a.p, row) : kIgnored;
                 z = row < a.p.N ? a.lse[row] : 0.f;
                 dl = row < a.p.N ? a.dloss[row] / out_scale : 0.f;
-                z2 = z * kLog2e;
                 if (target == kBad && a.v0 + it.n0 == 0 && half == 0) raise_status(a.p.status, kStatusTarget);
             }
             float acc[128];
@@ -573,7 +576,13 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
                         for (int j = 0; j < 128; ++j) s[j & 3] += expf(acc[j] - ms);
                         l = l * expf(m - ms);
                     } else {
-                        const float off = -ms * kLog2e;
+                        float off = -ms * kLog2e;
+                        if (fabsf(ms) > kFarLogit) {
+#pragma unroll
+                            for (int j = 0; j < 128; ++j) acc[j] -= ms;
+                            m -= ms;
+                            off = 0.f;
+                        }
                         const unsigned long long scale2 = pair(kLog2e, kLog2e), off2 = pair(off, off);
                         unsigned long long s2[2] = {0ull, 0ull};
 #pragma unroll
@@ -603,7 +612,13 @@ xent_kernel(const __grid_constant__ Args a, const __grid_constant__ Maps maps) {
 #pragma unroll
                             for (int j = 0; j < 128; ++j) acc[j] = dl * expf(acc[j] - z);
                         } else {
-                            const unsigned long long scale2 = pair(kLog2e, kLog2e), off2 = pair(-z2, -z2), dl2 = pair(dl, dl);
+                            float off = -z * kLog2e;
+                            if (fabsf(z) > kFarLogit) {
+#pragma unroll
+                                for (int j = 0; j < 128; ++j) acc[j] -= z;
+                                off = 0.f;
+                            }
+                            const unsigned long long scale2 = pair(kLog2e, kLog2e), off2 = pair(off, off), dl2 = pair(dl, dl);
 #pragma unroll
                             for (int j = 0; j < 128; j += 2) {
                                 float u, v;

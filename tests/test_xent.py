@@ -192,6 +192,59 @@ def test_large_logits(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("D", [64, 65, 520])
+@pytest.mark.parametrize("N", [1, 3, 8, 20, 40, 300])
+@pytest.mark.parametrize("value", ["lowest", "-inf"])
+def test_columns_masked_by_a_bias(value, N, D, dtype):
+    """A head with a bias, as a column of w against ones in x.  The bias of tokens
+    that are not to be had is the type's lowest value or -infinity: single tokens,
+    and a block of the vocabulary.  They add nothing."""
+    V, T = 1500, TYPES[dtype]
+    x, w, t, dl = make(N, D, V, T, 25, "none")
+    out = torch.zeros(V, dtype=torch.bool, device="cuda")
+    out[::3] = True
+    out[200:1200] = True
+    left = (~out).nonzero()[:, 0]
+    t = torch.where(out[t], left[t % len(left)], t)
+    t[-1] = V - 1 if not out[V - 1] else V - 2
+    x[:, -1], w[:, -1] = 1.0, 0.0
+    w[out, -1] = torch.finfo(T).min if value == "lowest" else -float("inf")
+    at = torch.searchsorted(left, t)
+    r = truth(x, w[left], at, dl)
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    assert (lse.double() - r["lse"]).abs().max() <= r["tol"] and (loss.double() - r["loss"]).abs().max() <= r["tol"]
+    dx, dw = fa.linear_xent_bwd(x, w, t, lse, dl)
+    bf = dtype == "bf16"
+    assert not dw[out].any()
+    for got, want, mag, K in ((dx[:, :-1], r["dx"][:, :-1], r["ax"][:, :-1], V), (dw[left], r["dw"], r["aw"], N)):
+        rel = 2 * r["tol"] + (K + 8) * U + (2.0 ** -8 if bf else 0.0)
+        assert ((got.double() - want).abs() <= rel * mag + (2.0 ** -8 if bf else U) * want.abs() + 1e-30).all()
+    if value == "lowest":                         # (0 times an infinity is none, as in any matrix product)
+        assert not dx[:, -1].any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("D", [64, 520])
+@pytest.mark.parametrize("N", [2, 20, 40, 300])
+def test_rows_with_nothing_but_masked_columns(N, D, dtype):
+    """All logits are the type's lowest value (what x and w have besides vanishes
+    beside it): equal logits, next to which log V vanishes too."""
+    V, T = 600, TYPES[dtype]
+    x, w, t, dl = make(N, D, V, T, 26, "none")
+    low = torch.finfo(T).min
+    x[:, -1], w[:, -1] = 1.0, low
+    loss, lse = fa.linear_xent_fwd(x, w, t)
+    assert ((lse.double() - low).abs() <= (D + 8) * U * abs(low)).all() and (loss == 0).all()
+    dw = fa.linear_xent_bwd(x, w, t, lse, dl)[1]
+    # exp(s - lse) is 1 there, as in the plain form: g = dloss (1 - [v = target])
+    one = torch.nn.functional.one_hot(t, V).double()
+    want = (dl.double()[:, None] * (1 - one)).t() @ x.double()
+    assert float((dw.double() - want).norm()) <= 3.2e-3 * float(want.norm())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_zero_rows_and_columns(dtype):
     x, w, t, dl = make(200, 64, 300, TYPES[dtype], 8)
