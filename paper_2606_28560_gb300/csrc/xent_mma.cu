@@ -707,6 +707,15 @@ __global__ void __launch_bounds__(256) maxima_kernel(Problem p, const float* dlo
     if (threadIdx.x == 0) maxima[blockIdx.x] = m;
 }
 
+// x, or bf16's largest value with its sign where x is larger; NaN stays.  The planes
+// but the last hold this: the lowest fp32 value, a usual mask, would else round to an
+// infinity in the first, and an infinity leave NaN in the next.
+__device__ __forceinline__ float within_bf16(float x) {
+    float r;
+    asm("min.NaN.xorsign.abs.f32 %0, %1, %2;\n" : "=f"(r) : "f"(x), "f"(__uint_as_float(0x7f7f0000u)));
+    return r;
+}
+
 // Rows of T as `planes` bf16 planes of row length `depth`, a multiple of eight
 // (zeros past D): one plane rounds nothing (bf16 rows of a length that TMA
 // cannot address), three hold an fp32 value to 24 bits.  A thread takes eight
@@ -733,10 +742,11 @@ template <typename T> __global__ void __launch_bounds__(256) pack_kernel(PackJob
             for (int j = 0; j < 8; ++j) x[j] = c + j < D ? to_f(src[j]) : 0.f;
         }
         for (int p = 0; p < planes; ++p) {
+            const bool more = p + 1 < planes;
             unsigned u[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                u[j] = mma::pack_bf16(x[2 * j], x[2 * j + 1]);
+                u[j] = mma::pack_bf16(more ? within_bf16(x[2 * j]) : x[2 * j], more ? within_bf16(x[2 * j + 1]) : x[2 * j + 1]);
                 x[2 * j] -= __uint_as_float(u[j] << 16);
                 x[2 * j + 1] -= __uint_as_float(u[j] & 0xffff0000u);
             }

@@ -116,6 +116,15 @@ template <int N> __device__ __forceinline__ void load_together(const float* p, b
 // conversion instructions go at an eighth of their rate, as many of them would take
 // as long as the products.  Of a NaN whose payload overflows here, low() is a NaN.
 __device__ __forceinline__ unsigned high(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
+// The same for values of w, of which a mask may be the lowest fp32 value or an infinity:
+// tf32's largest value with their sign, what is left (an infinity's: itself) to low().
+// (Forward and backward of 16 x 2048 x 131072 in fp32 822 us instead of 813, of 32 rows
+// 1400 instead of 1340.)
+__device__ __forceinline__ unsigned high_of_weight(float x) {
+    float r;
+    asm("min.NaN.xorsign.abs.f32 %0, %1, %2;\n" : "=f"(r) : "f"(x), "f"(__uint_as_float(0x7f7fe000u)));
+    return high(r);
+}
 __device__ __forceinline__ unsigned low(float x, unsigned hi) { return __float_as_uint(x - __uint_as_float(hi)); }
 
 __device__ __forceinline__ void mma(float* c, const unsigned* a, unsigned b0, unsigned b1) {
@@ -198,7 +207,7 @@ __device__ __forceinline__ void tile_logits(const T* w, int V, int D, int v0, co
                                             a1[u][4 * q + 2 * h + 1]};
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            ah[h][j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
+                            ah[h][j] = kExact ? __float_as_uint(e[j]) : high_of_weight(e[j]);
                             al[h][j] = kExact ? 0u : low(e[j], ah[h][j]);
                         }
                     }
@@ -475,7 +484,7 @@ rows_products_kernel(Problem p, const float* gradient, T* dw, float* parts, int 
                     unsigned ah[4], al[4], bh[OCT][2];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        ah[j] = kExact ? __float_as_uint(e[j]) : high(e[j]);
+                        ah[j] = kExact ? __float_as_uint(e[j]) : high_of_weight(e[j]);
                         al[j] = kExact ? 0u : low(e[j], ah[j]);
                     }
 #pragma unroll

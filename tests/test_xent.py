@@ -192,7 +192,7 @@ def test_large_logits(dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("D", [64, 65, 520])
 @pytest.mark.parametrize("N", [1, 3, 8, 20, 40, 300])
 @pytest.mark.parametrize("value", ["lowest", "-inf"])
@@ -225,7 +225,7 @@ def test_columns_masked_by_a_bias(value, N, D, dtype):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("D", [64, 520])
 @pytest.mark.parametrize("N", [2, 20, 40, 300])
 def test_rows_with_nothing_but_masked_columns(N, D, dtype):
