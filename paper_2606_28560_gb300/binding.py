@@ -10,7 +10,6 @@ from __future__ import annotations
 import array
 import ctypes
 import functools
-import inspect
 import operator
 import os
 import threading
@@ -204,7 +203,7 @@ def _check_device(index: int, *tensors):
     for t in tensors:
         if t is not None and t.get_device() != index:
             raise ValueError("all tensors must be on one CUDA device")
-    current = torch.cuda.current_device()
+    current = _current_device()
     if index != current:
         raise ValueError(f"the tensors are on cuda:{index} and the current device is cuda:{current}: "
                          f"make the call under torch.cuda.device({index})")
@@ -221,8 +220,10 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
-# The current stream of a device by its index, without the Stream object that
-# torch.cuda.current_stream() builds (some 4 us of every call).
+# The current device, and the current stream of a device by its index, without
+# the looks at the state of torch.cuda and the Stream object that the calls of
+# torch.cuda cost (some 4 us of every call).
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 _raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else \
     lambda index: torch.cuda.current_stream(index).cuda_stream
 
@@ -235,34 +236,25 @@ def _record(values, stream):
             _record(t, stream)
 
 
-def _takes_stream(call):
-    """Gives a call a ``stream=``: the torch stream its kernels run on (default: the
-    current one).  The call is then made with that stream current, so that what
-    it allocates belongs to that stream and is not handed to other work while the
-    kernels use it.  Given tensors are recorded with that stream, results with the
-    caller's: dropping them frees nothing that the other stream still uses.  That
-    inputs are ready, and results finished, is the caller's to order, as between
-    any two streams."""
-    @functools.wraps(call)
-    def on_stream(*args, stream=None, **kw):
-        if stream is None:
-            return call(*args, **kw)
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream.cuda_stream))
-        caller = torch.cuda.current_stream(stream.device)
-        if caller == stream:
-            return call(*args, **kw)
-        with torch.cuda.stream(stream):
-            results = call(*args, **kw)
-        _record(args, stream)
-        _record(kw.values(), stream)
-        _record(results if isinstance(results, tuple) else (results,), caller)
-        return results
-
-    sig = inspect.signature(call)
-    on_stream.__signature__ = sig.replace(parameters=[
-        *sig.parameters.values(), inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
-    return on_stream
+def _on_stream(stream, call, *args, **kw):
+    """call(*args, **kw) for a caller that gave ``stream=``, the torch stream its
+    kernels are to run on: made with that stream current, so that what it allocates
+    belongs to that stream and is not handed to other work while the kernels use
+    it.  Given tensors are recorded with that stream, results with the caller's:
+    dropping them frees nothing that the other stream still uses.  That inputs are
+    ready, and results finished, is the caller's to order, as between any two
+    streams."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream.cuda_stream))
+    if stream.device_index == _current_device() and stream.cuda_stream == _raw_stream(stream.device_index):
+        return call(*args, **kw)                  # it is the current one
+    caller = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        results = call(*args, **kw)
+    _record(args, stream)
+    _record(kw.values(), stream)
+    _record(results if isinstance(results, tuple) else (results,), caller)
+    return results
 
 
 def _offsets(offsets) -> np.ndarray:
@@ -356,9 +348,8 @@ def bwd_workspace_bytes(B, H, T, W, K, dtype, Hkv=None, D=64) -> int:
     return int(lib().fibattn_bwd_workspace_bytes(B, H, T, D, W, K, code, ctypes.byref(o)))
 
 
-@_takes_stream
 def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, dedup=True,
-        out=None, lse=None, workspace=None, kernel="auto", rotated_k=None, residuals=None,
+        out=None, lse=None, workspace=None, stream=None, kernel="auto", rotated_k=None, residuals=None,
         round_offsets=False):
     """Forward pass.  q [B,H,T,64]; k, v [B,Hkv,T,64] (fp32 or bf16, CUDA,
     contiguous).  ``kernel``: "auto", "gather" or "mma".  ``round_offsets``:
@@ -368,6 +359,10 @@ def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, de
     optional buffer (``residuals_like(q, W, K)``) that receives the rotated
     queries, p of every slot and the rung score differences for a later
     ``bwd(..., residuals=...)`` (tensor-core forward only).  Returns (out, lse)."""
+    if stream is not None:
+        return _on_stream(stream, fwd, q, k, v, alpha, offsets, W, rope_base=rope_base, scale=scale, dedup=dedup, out=out,
+                          lse=lse, workspace=workspace, kernel=kernel, rotated_k=rotated_k, residuals=residuals,
+                          round_offsets=round_offsets)
     B, H, T, D = q.shape
     Hkv = k.shape[1]
     f = _offsets(offsets)
@@ -395,9 +390,8 @@ def fwd(q, k, v, alpha: float, offsets, W: int, *, rope_base=1e4, scale=None, de
     return out, lse
 
 
-@_takes_stream
 def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_base=1e4, scale=None, dedup=True,
-        dq=None, dk=None, dv=None, dtheta=None, dd=None, workspace=None, kernel="auto",
+        dq=None, dk=None, dv=None, dtheta=None, dd=None, workspace=None, stream=None, kernel="auto",
         rotated_k=None, rung_grads=True, residuals=None, round_offsets=False):
     """Backward pass.  ``out``: the forward output (optional; enables the
     tensor-core query pass).  ``kernel``: "auto", "gather" or "mma".
@@ -408,6 +402,10 @@ def bwd(q, k, v, lse, dout, alpha: float, offsets, W: int, *, out=None, rope_bas
     dL/dtheta and dL/dd_k (a fixed schedule; required with ``round_offsets``).
     Returns (dq, dk, dv, dtheta [1], dd [K]) on the device (dtheta, dd None
     without rung_grads)."""
+    if stream is not None:
+        return _on_stream(stream, bwd, q, k, v, lse, dout, alpha, offsets, W, out=out, rope_base=rope_base, scale=scale,
+                          dedup=dedup, dq=dq, dk=dk, dv=dv, dtheta=dtheta, dd=dd, workspace=workspace, kernel=kernel,
+                          rotated_k=rotated_k, rung_grads=rung_grads, residuals=residuals, round_offsets=round_offsets)
     B, H, T, D = q.shape
     Hkv = k.shape[1]
     f = _offsets(offsets)
@@ -474,13 +472,15 @@ def aligned(t):
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
-@_takes_stream
-def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=None, workspace=None):
+def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=None, workspace=None, stream=None):
     """Cross entropy of the linear head ``x @ w.T`` without forming it in
     memory (fibattn_linear_xent_fwd).  x [N, D], w [V, D] (fp32 or bf16, CUDA,
     contiguous), targets [N] int64; rows whose target is ``ignore_index`` have
     loss 0.  Returns (loss [N], lse [N]) in fp32; ``lse`` goes to
     ``linear_xent_bwd``."""
+    if stream is not None:
+        return _on_stream(stream, linear_xent_fwd, x, w, targets, ignore_index=ignore_index, loss=loss, lse=lse,
+                          workspace=workspace)
     N, D, V, code, index = _check_xent(x, w, targets)
     loss = torch.empty(N, dtype=torch.float32, device=x.device) if loss is None else _f32_row(loss, N, index, "loss")
     lse = torch.empty_like(loss) if lse is None else _f32_row(lse, N, index, "lse")
@@ -496,14 +496,16 @@ def linear_xent_fwd(x, w, targets, *, ignore_index: int = -100, loss=None, lse=N
     return loss, lse
 
 
-@_takes_stream
 def linear_xent_bwd(x, w, targets, lse, dloss, *, ignore_index: int = -100, dx=None, dw=None, want_dx: bool = True,
-                    want_dw: bool = True, workspace=None):
+                    want_dw: bool = True, workspace=None, stream=None):
     """Gradients of ``sum(dloss * loss)`` by x and w (fibattn_linear_xent_bwd).
     lse [N] from ``linear_xent_fwd`` of the same inputs; dloss [N] fp32 (views at
     any offset).
     Returns (dx [N, D], dw [V, D]) in x's dtype; without ``want_dx`` or
     ``want_dw`` that product is not computed and None is returned for it."""
+    if stream is not None:
+        return _on_stream(stream, linear_xent_bwd, x, w, targets, lse, dloss, ignore_index=ignore_index, dx=dx, dw=dw,
+                          want_dx=want_dx, want_dw=want_dw, workspace=workspace)
     N, D, V, code, index = _check_xent(x, w, targets)
     lse, dloss = aligned(_f32_row(lse, N, index, "lse")), aligned(_f32_row(dloss, N, index, "dloss"))
     if not (want_dx or want_dw):
@@ -545,16 +547,17 @@ def clip_grads(grads, max_norm: float, *, out=None, norm=None, workspace=None, s
     grads: contiguous CUDA tensors on one device, fp32 and bf16 in any mix, any
     offset into a buffer.  ``out``: tensors of the same sizes and dtypes, or
     None to clip in place.  Returns norm, a 0-dim fp32 tensor on the device."""
-    return _clip(list(grads), float(max_norm), None if out is None else list(out), norm, workspace, True, stream=stream)
+    return _clip(list(grads), float(max_norm), None if out is None else list(out), norm, workspace, stream, True)
 
 
 def grad_norm(grads, *, norm=None, workspace=None, stream=None):
     """The norm alone, as ``clip_grads`` computes it; nothing else is written."""
-    return _clip(list(grads), float("inf"), None, norm, workspace, False, stream=stream)
+    return _clip(list(grads), float("inf"), None, norm, workspace, stream, False)
 
 
-@_takes_stream
-def _clip(grads, max_norm, out, norm, workspace, scale):
+def _clip(grads, max_norm, out, norm, workspace, stream, scale):
+    if stream is not None:
+        return _on_stream(stream, _clip, grads, max_norm, out, norm, workspace, None, scale)
     # (a model has hundreds of tensors: each is looked at with few calls, made by map)
     n = len(grads)
     outs = grads if out is None else out

@@ -35,7 +35,7 @@ def library(monkeypatch):
     rec = Library()
     monkeypatch.setattr(B, "lib", lambda: rec)
     monkeypatch.setattr(B, "_residual_bytes", lambda *a: 1000)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
     monkeypatch.setattr(B, "_raw_stream", lambda index: 0)
     monkeypatch.setattr(torch.Tensor, "data_ptr", lambda t: 256)
     with FakeTensorMode():
@@ -113,7 +113,7 @@ def test_a_workspace_of_the_device_is_used(name, library):
 
 class Stream:
     """A stand-in stream; `now` is the current one."""
-    device = torch.device("cuda:0")
+    device, device_index = torch.device("cuda:0"), 0
 
     def __init__(self, handle):
         self.cuda_stream = handle
