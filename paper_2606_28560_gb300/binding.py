@@ -1,7 +1,8 @@
 """Thin ctypes binding of the C ABI in ``include/fibattn.h``.
 
 Argument marshalling only: tensors are passed as raw device pointers with the
-caller's current CUDA stream; every step of the computation runs in the CUDA
+caller's current CUDA stream, or the torch stream given as ``stream=`` (see
+``_on_stream`` for what it then does with memory); every step of the computation runs in the CUDA
 library.  The binding raises ``RuntimeError`` when the library is missing or
 a call returns a non-OK status -- there is no fallback.
 """

@@ -11,8 +11,8 @@
 // core truncates.
 //
 // Bound by memory in bf16 and up to 16 rows in fp32: 16 x 2048 x 131072 in fp32 takes
-// 188 us forward (5.7 TB/s) and 628 backward (2 x 1.07 GB read, 1.07 written).
-// With 32 rows, 344 and 992, it is halfway between memory (159 and 476) and the
+// 193 us forward (5.6 TB/s) and 633 backward (2 x 1.07 GB read, 1.07 written).
+// With 32 rows, 361 and 1040, it is halfway between memory (159 and 476) and the
 // tensor rate (150 T multiplications a second, three for one in fp32): what is
 // issued beside them, the splitting in two and the loads of x, is the rest.
 //
@@ -281,8 +281,8 @@ __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
 
 // Whether tile_logits asks ahead: for eight deep rows it is memory's latency that bounds,
 // otherwise the instructions are missed elsewhere (fp32, us forward and backward, with
-// / without: 8 x 8192 x 20000 584 / 648, 8 x 7168 x 20000 465 / 489, 16 x 2048 x
-// 131072 830 / 814, 16 x 512 x 32768 79 / 75).
+// / without: 8 x 8192 x 20000 609 / 653, 8 x 7168 x 20000 475 / 492, 16 x 2048 x
+// 131072 833 / 823, 16 x 512 x 32768 74 / 73).
 constexpr bool asked_ahead(int oct, int warps) { return oct == 1 && warps == 16; }
 
 // Block: a segment of w (for `groups` > 1 as many groups of 8 OCT rows of x, whose
@@ -403,7 +403,7 @@ rows_gradient_kernel(Problem p, const float* lse, const float* dloss, float* gra
 //
 // Registers allow one to three blocks to an SM, too few loads under way for memory's
 // latency: the rows of w four tiles ahead are asked into L2, the next tile's g into
-// L1 (fp32, 32 x 2048 x 131072: 828 us without, 749 with the first, 664 with both).
+// L1 (fp32, 32 x 2048 x 131072: 904 us without, 763 with the first, 705 with both).
 template <typename T> constexpr int resident(int oct) { return oct == 4 ? 1 : oct == 1 && sizeof(T) == 2 ? 3 : 2; }
 
 template <typename T, int OCT, bool VECTORS>
