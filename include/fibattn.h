@@ -52,8 +52,9 @@ typedef enum {
                                       kernel gave up a bounded wait (see
                                       fibattn_check_status)                        */
     FIBATTN_ERR_RANGE = 5          /* an operand left the range of the library's
-                                      16-bit rotated rows, or a target that of the
-                                      vocabulary (fibattn_check_status)            */
+                                      16-bit rotated rows, a target that of the
+                                      vocabulary, or a page that of the pool
+                                      (fibattn_check_status)                       */
 } fibattn_status;
 
 typedef enum { FIBATTN_F32 = 0, FIBATTN_BF16 = 1 } fibattn_dtype;
@@ -179,10 +180,12 @@ const char* fibattn_last_error(void);
  *            which cannot hold it.
  *   bit 2 -- fibattn_linear_xent_fwd or _bwd met a target outside [0, V) that
  *            is not ignore_index (that row's loss is NaN).
+ *   bit 3 -- a call on a paged cache met a sequence, storage slot, page or
+ *            parent that does not exist (see fibattn_cache_init).
  * fibattn_check_status synchronises `stream`, reads the calling thread's
  * current device's word into *flags (may be NULL) and clears it.  Returns
- * FIBATTN_ERR_INTERNAL if bit 0 was set, else FIBATTN_ERR_RANGE if bit 1 or 2
- * was set, else FIBATTN_OK.  Compute calls never synchronise to look at it.
+ * FIBATTN_ERR_INTERNAL if bit 0 was set, else FIBATTN_ERR_RANGE if bit 1, 2 or
+ * 3 was set, else FIBATTN_OK.  Compute calls never synchronise to look at it.
  * ------------------------------------------------------------------------- */
 int fibattn_check_status(void* stream, unsigned* flags);
 
@@ -350,6 +353,90 @@ size_t fibattn_clip_grads_workspace_bytes(int n);
 int fibattn_clip_grads(int n, const void* const* grads, void* const* outs,
                        const long long* numels, const int* dtypes, float max_norm,
                        float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Generating with the attention: a paged cache of keys and values, and the
+ * attention of new tokens over it (Section 2, "Attended set": the same window
+ * and rungs as fibattn_fwd, of queries that come later than the keys).
+ *
+ * A cache is two pools of pages for one layer, keys (RoPE-rotated; fp16 for
+ * bf16 I/O, fp32 for fp32 I/O, as in fibattn_opts.rotated_k) and values (the I/O
+ * type), both [pages][page_rows][Hkv][64] with the same strides, and a table
+ * [seqs][pages_per_seq] of 32-bit page numbers on the device.  Storage slot j of
+ * sequence b is row j % page_rows of page table[b][j / page_rows].  Strides are
+ * in elements, the last dimension is contiguous and the others are any multiples
+ * of 64 (a layer of a larger pool, pages with the heads before the rows, ...).
+ * Limits: pages_per_seq * page_rows <= 2^30; every row's offset, counted in rows
+ * of 64, below 2^32.
+ *
+ * Tokens lie behind one another, whichever sequence they belong to: token n of
+ * N belongs to sequence seqs[n] (seqs NULL: sequence n) and stands at
+ * positions[n], both 32-bit on the device, so that a captured call can be replayed
+ * for other positions.  A token with a negative position or sequence is padding:
+ * fibattn_cache_append writes nothing for it, the attention writes out = 0 and
+ * lse = -infinity.
+ *
+ * What does not exist is never read or written: a sequence that is not in the
+ * table, a slot beyond pages_per_seq pages, a page outside the pool (an unused
+ * table entry, say -1).  An append then leaves the token out, an attention gives
+ * NaN for the token's out and lse, and status bit 3 is set (fibattn_check_status).
+ * Pages that no query reads may be taken from a sequence at any time: a query
+ * reads no further back than max(W, ceil(largest d_k)).
+ *
+ * fibattn_cache_init checks a cache's arguments and fills *c with them and with
+ * what follows from rope_base (0: 1e4); it touches no device memory.  *c is read
+ * by the calls below during the call only, and may be copied.  Its fields are not
+ * for the caller to change.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    void* k_pages;
+    void* v_pages;
+    const int* table;
+    long long page_stride, row_stride, head_stride;
+    int pages, page_rows, Hkv, seqs, pages_per_seq, dtype;
+    unsigned ready;
+    unsigned long long phase[32];
+} fibattn_cache;
+
+int fibattn_cache_init(fibattn_cache* c, void* k_pages, void* v_pages, int pages, int page_rows, int Hkv, int D,
+                       long long page_stride, long long row_stride, long long head_stride,
+                       const int* table, int seqs, int pages_per_seq, int dtype, float rope_base);
+
+/* Writes N tokens' keys, rotated at positions[n], and values into the cache, at
+ * storage slot slots[n] (32-bit, on the device; NULL: at slot positions[n]).  k and
+ * v: [N][Hkv][64] in the cache's I/O type, contiguous in the last dimension, with
+ * strides in elements that are multiples of 16 bytes.  Two tokens of one call at
+ * the same slot of the same sequence leave that slot with a mixture of both;
+ * nothing else is affected. */
+int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_token_stride, long long k_head_stride,
+                         const void* v, long long v_token_stride, long long v_head_stride,
+                         const int* positions, const int* slots, const int* seqs, int N, void* stream);
+
+/* Attention of N tokens over the cache: q [N][H][64] as k above (H a multiple of
+ * the cache's Hkv; query head h reads head h / (H / Hkv)), out [N][H][64]
+ * contiguous, lse [N][H] fp32.  The query at position p reads slots p .. p-W and,
+ * for every active rung with d_k <= p, slots p - floor(d_k) and, where d_k is no
+ * integer, p - floor(d_k) - 1: its own key and value too, which have to be
+ * appended before.  opts: scale, no_dedup and round_offsets are used; the other
+ * fields have to be zero (rope_base is the cache's).  Products and sums are fp32;
+ * q is rotated in fp32 and not rounded.  Limits of W, K and alpha as for
+ * fibattn_fwd; 0 <= N, N * H < 2^31. */
+int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
+                       void* out, float* lse, const int* positions, const int* seqs, int N, int H, int W,
+                       float alpha, const float* offsets, int K, const fibattn_opts* opts, void* stream);
+
+/* The same for drafted tokens that form trees: parents[n] is the token (row of this
+ * batch, before n) that token n continues, or -1 if it continues the cached
+ * sequence itself; its position is one more than its parent's.  The ancestor at
+ * distance j, j steps up (0: the token itself), is read from storage slot
+ * slots[ancestor], where fibattn_cache_append put it; what lies further back than
+ * the root from the slot of its position.  A parent that is not before its child
+ * counts as one that does not exist (above).  That it belongs to the child's
+ * sequence is not checked: its slot would be looked up in the child's pages. */
+int fibattn_tree_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
+                     void* out, float* lse, const int* positions, const int* parents, const int* slots,
+                     const int* seqs, int N, int H, int W,
+                     float alpha, const float* offsets, int K, const fibattn_opts* opts, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Opt-in kernel timing (no counterpart in the paper; used to attribute time

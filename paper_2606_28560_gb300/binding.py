@@ -42,6 +42,14 @@ class Opts(ctypes.Structure):
                 ("round_offsets", ctypes.c_int)]
 
 
+class CacheStruct(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("page_stride", ctypes.c_longlong), ("row_stride", ctypes.c_longlong),
+                ("head_stride", ctypes.c_longlong), ("pages", ctypes.c_int), ("page_rows", ctypes.c_int),
+                ("Hkv", ctypes.c_int), ("seqs", ctypes.c_int), ("pages_per_seq", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("ready", ctypes.c_uint), ("phase", ctypes.c_ulonglong * 32)]
+
+
 def library_path() -> str:
     return _build.LIB
 
@@ -97,6 +105,14 @@ def lib():
             L.fibattn_clip_grads_workspace_bytes.restype = sz
             L.fibattn_clip_grads.argtypes = [ci, vp, vp, vp, vp, cf, vp, vp, sz, vp]
             L.fibattn_clip_grads.restype = ci
+            L.fibattn_cache_init.argtypes = [vp, vp, vp, ci, ci, ci, ci, ll, ll, ll, vp, ci, ci, ci, cf]
+            L.fibattn_cache_init.restype = ci
+            L.fibattn_cache_append.argtypes = [vp, vp, ll, ll, vp, ll, ll, vp, vp, vp, ci, vp]
+            L.fibattn_cache_append.restype = ci
+            L.fibattn_cached_fwd.argtypes = [vp, vp, ll, ll, vp, vp, vp, vp, ci, ci, ci, cf, vp, ci, vp, vp]
+            L.fibattn_cached_fwd.restype = ci
+            L.fibattn_tree_fwd.argtypes = [vp, vp, ll, ll, vp, vp, vp, vp, vp, vp, ci, ci, ci, cf, vp, ci, vp, vp]
+            L.fibattn_tree_fwd.restype = ci
             _lib = L
     return _lib
 
@@ -233,6 +249,8 @@ def _record(values, stream):
     for t in values:
         if torch.is_tensor(t):
             t.record_stream(stream)
+        elif isinstance(t, PagedCache):
+            _record((t.k_pages, t.v_pages, t.block_table), stream)
         elif isinstance(t, (list, tuple)):
             _record(t, stream)
 
@@ -594,13 +612,171 @@ def _clip(grads, max_norm, out, norm, workspace, stream, scale):
     return norm
 
 
+# ------------------------------------------ generating: the paged cache ----
+
+class PagedCache:
+    """One layer's cache of keys and values in pages (fibattn_cache_init).
+
+    k_pages, v_pages [pages, rows of a page, Hkv, 64]: pools on one device, of the
+    same shape and strides; the rotated keys in fp16 and the values in bf16, or
+    both in fp32.  Any strides that are multiples of 64, the last dimension
+    contiguous (a layer of a larger pool, a transposed pool with the heads first).
+    block_table [seqs, pages of a sequence] int32: where the pages of each sequence
+    lie; entries may change between calls, unused ones are -1 or anything else.
+
+    The object keeps the three tensors and what follows from them; their memory is
+    the caller's.  ``PagedCache.empty`` makes pools."""
+
+    def __init__(self, k_pages, v_pages, block_table, *, rope_base: float = 1e4):
+        if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or k_pages.shape[3] != 64:
+            raise ValueError("k_pages and v_pages must be [pages, rows, Hkv, 64], alike")
+        want = {torch.bfloat16: torch.float16, torch.float32: torch.float32}.get(v_pages.dtype)
+        if want is None or k_pages.dtype != want:
+            raise TypeError("a cache holds fp16 keys and bf16 values, or both in fp32")
+        index = k_pages.get_device()
+        if index < 0 or v_pages.get_device() != index or block_table.get_device() != index:
+            raise ValueError("the pools and block_table must be on one CUDA device")
+        if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
+            raise ValueError("block_table must be a contiguous int32 tensor [seqs, pages of a sequence]")
+        strides = _pool_strides(k_pages)
+        if strides != _pool_strides(v_pages):
+            raise ValueError("k_pages and v_pages must have the same strides")
+        self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
+        self.dtype, self.Hkv, self.index = v_pages.dtype, k_pages.shape[2], index
+        pages, rows, heads, D = k_pages.shape
+        self._struct = CacheStruct()
+        self._at = ctypes.addressof(self._struct)
+        _check(lib().fibattn_cache_init(self._at, k_pages.data_ptr(), v_pages.data_ptr(), pages, rows, heads, D, *strides,
+                                        block_table.data_ptr(), *block_table.shape, _dtype_code(v_pages), float(rope_base)))
+
+    @classmethod
+    def empty(cls, pages: int, rows: int, Hkv: int, block_table, *, dtype=torch.bfloat16, rope_base: float = 1e4):
+        """A cache over new pools on block_table's device, for tensors of ``dtype``."""
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError(f"unsupported dtype {dtype}: fp32 or bf16")
+        shape = (pages, rows, Hkv, 64)
+        keys = torch.float16 if dtype == torch.bfloat16 else torch.float32
+        return cls(torch.empty(shape, dtype=keys, device=block_table.device),
+                   torch.empty(shape, dtype=dtype, device=block_table.device), block_table, rope_base=rope_base)
+
+
+def _pool_strides(t):
+    """Strides of a pool's first three dimensions; that of a dimension of one is of no matter."""
+    if t.shape[3] > 1 and t.stride(3) != 1:
+        raise ValueError("the last dimension of a pool must be contiguous")
+    return tuple(64 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()))
+
+
+def _token_strides(t, cache, name):
+    """Strides of tokens [N, heads, 64] as the library takes them."""
+    if t.dim() != 3 or t.shape[2] != 64 or t.dtype != cache.dtype or t.get_device() != cache.index:
+        raise ValueError(f"{name} must be [tokens, heads, 64] of the cache's dtype, on its device")
+    token, head, last = t.stride()
+    N, heads, _ = t.shape
+    token, head = 0 if N == 1 else token, 0 if heads == 1 else head
+    unit = 8 if cache.dtype == torch.bfloat16 else 4
+    if last != 1 or token % unit or head % unit:
+        raise ValueError(f"{name} must be contiguous in its last dimension, with strides of whole 16 bytes")
+    return token, head
+
+
+def _check_ints(N, index, **given):
+    for name, t in given.items():
+        if name == "positions" and t is None:
+            raise ValueError("positions are needed")
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != N or t.get_device() != index or
+                              not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor of {N} values on the cache's device")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def cache_append(cache: PagedCache, k, v, positions, *, seqs=None, slots=None, stream=None):
+    """Writes the keys and values of N tokens into the cache, the keys rotated on
+    the way (fibattn_cache_append).  k, v [N, Hkv, 64]: views of a fused projection
+    will do.  positions [N] int32: where each token stands; seqs [N] int32: whose
+    it is (default: token n is sequence n's); slots [N] int32: where it is stored
+    (default: at its position; drafted tokens lie elsewhere).  A negative position or
+    sequence is padding.  Nothing is returned."""
+    if stream is not None:
+        return _on_stream(stream, cache_append, cache, k, v, positions, seqs=seqs, slots=slots)
+    ks, vs = _token_strides(k, cache, "k"), _token_strides(v, cache, "v")
+    N, index = k.shape[0], cache.index
+    if v.shape != k.shape or k.shape[1] != cache.Hkv:
+        raise ValueError("k and v must be [tokens, the cache's Hkv, 64]")
+    _check_ints(N, index, positions=positions, seqs=seqs, slots=slots)
+    _check_device(index)
+    _check(lib().fibattn_cache_append(cache._at, k.data_ptr(), *ks, v.data_ptr(), *vs, positions.data_ptr(), _ptr(slots),
+                                      _ptr(seqs), N, _raw_stream(index)))
+
+
+def cached_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, *, seqs=None, scale=None, dedup=True,
+               round_offsets=False, out=None, lse=None, stream=None):
+    """Attention of N tokens over the cache (fibattn_cached_fwd): ``fwd``'s window
+    and rungs, read from the pages.  q [N, H, 64] (views of a fused projection will
+    do), positions and seqs as for ``cache_append``; the tokens' own keys and values
+    have to be in the cache.  One token per sequence, chunks of a prompt, or any mix.
+    Returns (out [N, H, 64], lse [N, H] fp32); padding has out 0 and lse -infinity."""
+    if stream is not None:
+        return _on_stream(stream, cached_fwd, q, cache, alpha, offsets, W, positions, seqs=seqs, scale=scale, dedup=dedup,
+                          round_offsets=round_offsets, out=out, lse=lse)
+    return _attention(q, cache, alpha, offsets, W, positions, None, None, seqs, scale, dedup, round_offsets, out, lse)
+
+
+def tree_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, parents, slots, *, seqs=None, scale=None,
+             dedup=True, round_offsets=False, out=None, lse=None, stream=None):
+    """Attention of drafted tokens that form trees (fibattn_tree_fwd): a token sees
+    its ancestors in place of the positions they stand at, and the cached sequence
+    behind the root.  parents [N] int32: the row of this batch, before n, that token
+    n continues, or -1; slots [N] int32: where ``cache_append`` put each token.  The
+    rest as for ``cached_fwd``.  A parent is of its child's sequence, its position one
+    less (not checked: another's slot would be looked up in the child's pages).
+    Accepted tokens are appended again, at their
+    positions."""
+    if stream is not None:
+        return _on_stream(stream, tree_fwd, q, cache, alpha, offsets, W, positions, parents, slots, seqs=seqs, scale=scale,
+                          dedup=dedup, round_offsets=round_offsets, out=out, lse=lse)
+    if parents is None or slots is None:
+        raise ValueError("a tree needs parents and slots")
+    return _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, scale, dedup, round_offsets, out, lse)
+
+
+def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, scale, dedup, round_offsets, out, lse):
+    strides, index = _token_strides(q, cache, "q"), cache.index
+    N, H, D = q.shape
+    _check_ints(N, index, positions=positions, seqs=seqs, parents=parents, slots=slots)
+    _check_device(index)
+    f = _offsets(offsets)
+    if out is None:
+        out = torch.empty((N, H, D), dtype=q.dtype, device=q.device)
+    elif out.dtype != q.dtype or out.shape != q.shape or out.get_device() != index or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and dtype on its device")
+    if lse is None:
+        lse = torch.empty((N, H), dtype=torch.float32, device=q.device)
+    elif lse.dtype != torch.float32 or lse.shape != (N, H) or lse.get_device() != index or not lse.is_contiguous():
+        raise ValueError("lse must be a contiguous fp32 tensor [N, H] on q's device")
+    o = None if scale is None and dedup and not round_offsets else \
+        ctypes.addressof(opts := _opts(0.0, scale, 0, dedup, round_offsets=round_offsets))   # noqa: F841 (kept alive)
+    L, tail = lib(), (N, H, int(W), float(alpha), f.ctypes.data, len(f), o, _raw_stream(index))
+    if parents is None:
+        _check(L.fibattn_cached_fwd(cache._at, q.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(),
+                                    positions.data_ptr(), _ptr(seqs), *tail))
+    else:
+        _check(L.fibattn_tree_fwd(cache._at, q.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(),
+                                  positions.data_ptr(), parents.data_ptr(), slots.data_ptr(), _ptr(seqs), *tail))
+    return out, lse
+
+
 # ---------------------------------------------------------- device status ----
 
 def check_status(stream=None):
     """Synchronise ``stream`` and read and clear the device status word
     (fibattn_check_status).  Returns the flags; raises FibattnError when a
-    kernel gave up a bounded wait (status 4), a rotated row overflowed fp16 or a
-    cross-entropy target was outside the vocabulary (status 5)."""
+    kernel gave up a bounded wait (status 4), a rotated row overflowed fp16, a
+    cross-entropy target was outside the vocabulary or a token named a part of a
+    cache that does not exist (status 5)."""
     flags = ctypes.c_uint(0)
     rc = lib().fibattn_check_status(_stream_ptr(stream), ctypes.byref(flags))
     if rc != 0:

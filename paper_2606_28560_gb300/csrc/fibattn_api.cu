@@ -271,6 +271,10 @@ int set_errorf(int code, const char* fmt, ...) {
     return fail(code, "%s", buf);
 }
 int bind_device_context() { return bind_context(); }
+int prepare_rungs(float alpha, const float* f, int K, int W, int dedup, int T, RungParams* r, int round_offsets) {
+    return prep_rungs(alpha, f, K, W, dedup, T, r, round_offsets);
+}
+void prepare_rope(float base, RopeParams* rp) { prep_rope(base, rp); }
 int device_status_word(unsigned** out) { return status_word(out); }
 
 // During stream capture the records become external event nodes of the
@@ -616,6 +620,9 @@ int fibattn_check_status(void* stream, unsigned* flags) {
     if (h & kStatusTarget)
         return fail(FIBATTN_ERR_RANGE, "a cross-entropy target was outside the vocabulary and not ignore_index "
                                        "(the loss of such rows is NaN)");
+    if (h & kStatusPage)
+        return fail(FIBATTN_ERR_RANGE, "a token named a sequence, storage slot, page or parent that its cache does "
+                                       "not have (it was not appended; its attention is NaN)");
     return FIBATTN_OK;
 }
 

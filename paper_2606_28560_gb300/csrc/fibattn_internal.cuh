@@ -68,6 +68,7 @@ struct Shape {
 constexpr unsigned kStatusWaitTimeout = 1u;   // a bounded wait on a staging copy ran out
 constexpr unsigned kStatusRange = 2u;         // a rotated row overflowed its fp16 storage
 constexpr unsigned kStatusTarget = 4u;        // a cross-entropy target outside the vocabulary
+constexpr unsigned kStatusPage = 8u;          // a cache's sequence, slot, page or parent that does not exist
 __device__ __forceinline__ void raise_status(unsigned* st, unsigned bits) {
     if (st) atomicOr(st, bits);
 }
@@ -336,6 +337,8 @@ int set_errorf(int code, const char* fmt, ...);
 // Host: makes the primary context of the thread's current device current;
 // the device address of its status word.  Both return a fibattn_status.
 int bind_device_context();
+int prepare_rungs(float alpha, const float* f, int K, int W, int dedup, int T, RungParams* r, int round_offsets);
+void prepare_rope(float base, RopeParams* rp);
 int device_status_word(unsigned** out);
 
 // Opt-in per-kernel timing: when enabled, each launch is bracketed by CUDA
