@@ -55,14 +55,17 @@ struct AttnArgs {
     const int* parents;                              // trees only
     const int* slots;
     int N, H, G;                                     // G = H / Hkv query heads per key/value head
-    int parts, per_part;                             // a group's heads are cut into parts of per_part
+    int parts, per_part;                             // fp32: a group's heads are cut into parts of per_part
+    unsigned units;                                  // bf16: warps
+    FastDiv dRest, dParts;                           // by the warps of a token, by the parts of a group
     float scale;                                     // times log2 e: softmax in base 2
     Rows r;
     unsigned* status;
 };
 
 cudaError_t launch_append(const AppendArgs& a, bool bf16, cudaStream_t st);
-cudaError_t launch_attention(const AttnArgs& a, bool bf16, cudaStream_t st);
+cudaError_t launch_attention_f32(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attention_mma(const AttnArgs& a, cudaStream_t st);          // bf16
 
 // cos and sin of the angle of pair m at position pos, to fp32 rounding: the phase
 // is an integer fraction of a turn (RopeParams), so its quadrant is taken off

@@ -105,7 +105,7 @@ int attention(const fibattn_cache* c, const void* q, long long q_token, long lon
     if ((rc = device_status_word(&a.status))) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     ProfScope p(parents ? "tree_fwd" : "cached_fwd", st);
-    const cudaError_t e = cache::launch_attention(a, c->dtype == FIBATTN_BF16, st);
+    const cudaError_t e = c->dtype == FIBATTN_BF16 ? cache::launch_attention_mma(a, st) : cache::launch_attention_f32(a, st);
     return e == cudaSuccess ? FIBATTN_OK : launch_failed(e, "attention over the cache");
 }
 

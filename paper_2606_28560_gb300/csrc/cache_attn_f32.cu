@@ -1,17 +1,17 @@
-// cache_attn.cu -- attention of new tokens over a paged cache (arXiv 2606.28560,
-// Section 2, "Attended set"): s = scale q~ . key, softmax over window and rungs,
+// cache_attn_f32.cu -- attention of new tokens over a paged cache, fp32 (arXiv
+// 2606.28560, Section 2, "Attended set"): s = scale q~ . key, softmax over window and rungs,
 // out = sum p value; a rung's key and value are interpolated from two rows, so its
 // score is (1-w) s_floor + w s_far and its rows have weights p (1-w) and p w.
 //
 // A warp has one token and key/value head (its group of query heads, or a part of
 // it).  32 rows at a time: each lane finds one row through the page table; then all
-// lanes load rows, eight lanes to a row (16 bytes of it each, 32 in fp32), four rows
+// lanes load rows, eight lanes to a row (32 bytes of it each), four rows
 // to an instruction, all of keys and values at once.  Eight partial dot products per
 // lane are exchanged so that a lane ends with the score of the row it looked up, and
 // the softmax is one value per lane.
 #include <algorithm>
 
-#include "cache.cuh"
+#include "cache_rows.cuh"
 
 namespace fibattn {
 namespace cache {
@@ -19,8 +19,6 @@ namespace cache {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr unsigned kAll = 0xffffffffu;
 
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -33,34 +31,11 @@ __device__ __forceinline__ float warp_sum(float x) {
     return x;
 }
 
-// Eight elements of a row as they lie in memory.
-template <typename T> struct Raw { uint4 w[sizeof(T) / 2]; };
-template <typename T>
-__device__ __forceinline__ void load_raw(const void* pool, unsigned row, int c, Raw<T>& r) {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const T*>(pool) + (size_t)row * kHeadDim + 8 * c);
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 2); ++i) r.w[i] = p[i];
-}
-__device__ __forceinline__ void unpack(const Raw<float>& r, float* x) {
-    *reinterpret_cast<uint4*>(x) = r.w[0];
-    *reinterpret_cast<uint4*>(x + 4) = r.w[1];
-}
-__device__ __forceinline__ void unpack(const Raw<__nv_bfloat16>& r, float* x) {
-    const unsigned w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ void unpack(const Raw<__half>& r, float* x) {
-    const unsigned w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
+// Eight elements of a row.
+struct Raw { float4 lo, hi; };
+__device__ __forceinline__ Raw load_raw(const void* pool, unsigned row, int c) {
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(pool) + (size_t)row * kHeadDim + 8 * c);
+    return {p[0], p[1]};
 }
 
 // v[i] summed over the eight lanes of a group, each lane keeping i = its number:
@@ -78,63 +53,12 @@ __device__ __forceinline__ float sum_own(float (&v)[8], int c) {
     return v[0];
 }
 
-template <typename T> __device__ __forceinline__ void store2(T* p, float x, float y);
-template <> __device__ __forceinline__ void store2(float* p, float x, float y) {
-    *reinterpret_cast<float2*>(p) = make_float2(x, y);
-}
-template <> __device__ __forceinline__ void store2(__nv_bfloat16* p, float x, float y) {
-    *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y);
-}
-
-// Row r of a query's list: its distance, its weight within its slot, and whether it
-// is one of two.  need: the distance that the query must have behind it.
-struct RowOf { int distance, need; float weight; bool pair; };
-__device__ __forceinline__ RowOf row_of(const Rows& r, int i) {
-    RowOf o;
-    o.pair = i < 2 * r.pairs;
-    if (o.pair) {
-        const int k = i >> 1, far = i & 1;
-        const float w = r.far[k];
-        o.need = r.near[k] + 1;
-        o.distance = r.near[k] + far;
-        o.weight = far ? w : 1.f - w;
-    } else {
-        const int k = i - 2 * r.pairs;
-        o.distance = o.need = k < r.singles ? r.near[r.pairs + k] : k - r.singles;
-        o.weight = 1.f;
-    }
-    return o;
-}
-
-// The storage slot of a lane's row: the slot of its position, or, in a tree, that of
-// the ancestor `distance` steps up, where the tree reaches that far.  All lanes walk
-// together, one parent at a time.  Returns false if a parent is not before its child.
-template <bool kTree>
-__device__ __forceinline__ bool slot_of(const AttnArgs& a, int n, int pos, int distance, bool live, int& slot) {
-    slot = pos - distance;
-    if (!kTree) return true;
-    int furthest = live ? distance : -1;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) furthest = max(furthest, __shfl_xor_sync(kAll, furthest, o));
-    int mine = -1, cur = n;
-    for (int j = 0; j <= furthest; ++j) {
-        if (j == distance) mine = cur;
-        const int up = a.parents[cur];
-        if (up < -1 || up >= cur) return false;       // (the same for all lanes)
-        if (up < 0) break;
-        cur = up;
-    }
-    if (live && mine >= 0) slot = a.slots[mine];
-    return true;
-}
-
 // Running softmax of one query head over the rows so far: m the largest score, l the
 // sum of weights (each lane its own rows'), acc the values (each lane's rows and dims).
 struct Running { float m, l, acc[8]; };
 
 // One group of up to 32 rows, loaded: scores, weights, values for one query head.
-template <typename T, typename R>
-__device__ __forceinline__ void attend(const Raw<R> (&k)[8], const Raw<T> (&v)[8], const float* q, int c, bool live,
+__device__ __forceinline__ void attend(const Raw (&k)[8], const Raw (&v)[8], const float* q, int c, bool live,
                                        const RowOf& row, Running& run) {
     float s[8];
     float qc[8];
@@ -142,8 +66,7 @@ __device__ __forceinline__ void attend(const Raw<R> (&k)[8], const Raw<T> (&v)[8
     *reinterpret_cast<float4*>(qc + 4) = *reinterpret_cast<const float4*>(q + 8 * c + 4);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        float x[8];
-        unpack(k[i], x);
+        const float x[8] = {k[i].lo.x, k[i].lo.y, k[i].lo.z, k[i].lo.w, k[i].hi.x, k[i].hi.y, k[i].hi.z, k[i].hi.w};
         float2 t = __fmul2_rn(make_float2(x[0], x[1]), make_float2(qc[0], qc[1]));
 #pragma unroll
         for (int j = 1; j < 4; ++j)
@@ -166,8 +89,7 @@ __device__ __forceinline__ void attend(const Raw<R> (&k)[8], const Raw<T> (&v)[8
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const float w = __shfl_sync(kAll, p, group + i);
-        float x[8];
-        unpack(v[i], x);
+        const float x[8] = {v[i].lo.x, v[i].lo.y, v[i].lo.z, v[i].lo.w, v[i].hi.x, v[i].hi.y, v[i].hi.z, v[i].hi.w};
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
             const float2 t = __ffma2_rn(make_float2(w, w), make_float2(x[j], x[j + 1]),
@@ -178,9 +100,8 @@ __device__ __forceinline__ void attend(const Raw<R> (&k)[8], const Raw<T> (&v)[8
     }
 }
 
-template <typename T, bool kTree>
+template <bool kTree>
 __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_constant__ AttnArgs a) {
-    using R = typename RotOf<T>::type;
     __shared__ __align__(16) float qs[kWarps][kHeadDim];
     grid_dependency_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 7, group = lane >> 3;
@@ -188,7 +109,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_con
     if (unit >= (long long)a.N * a.c.Hkv * a.parts) return;
     const int part = (int)(unit % a.parts), h = (int)(unit / a.parts % a.c.Hkv), n = (int)(unit / a.parts / a.c.Hkv);
     const int g0 = h * a.G + part * a.per_part, g1 = h * a.G + min(a.G, (part + 1) * a.per_part);
-    T* out = static_cast<T*>(a.out) + (size_t)n * a.H * kHeadDim;
+    float* out = static_cast<float*>(a.out) + (size_t)n * a.H * kHeadDim;
     float* lse = a.lse + (size_t)n * a.H;
     const int pos = a.positions[n], seq = a.seqs ? a.seqs[n] : n;
     const int* pages = a.c.table + (size_t)max(seq, 0) * a.c.pages_per_seq;
@@ -203,8 +124,8 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_con
 #pragma unroll
         for (int j = 0; j < 8; ++j) run.acc[j] = 0.f;
         if (!padding && !bad) {
-            const T* q = static_cast<const T*>(a.q) + n * a.q_token + g * a.q_head;
-            const float x = to_f(q[lane]) * a.scale, y = to_f(q[lane + kHalf]) * a.scale;
+            const float* q = static_cast<const float*>(a.q) + n * a.q_token + g * a.q_head;
+            const float x = q[lane] * a.scale, y = q[lane + kHalf] * a.scale;
             __syncwarp();
             qs[warp][lane] = x * cs - y * sn;
             qs[warp][lane + kHalf] = y * cs + x * sn;
@@ -223,17 +144,15 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_con
             bad = __any_sync(kAll, !found);
             if (bad) break;
             at += h * a.c.head_stride;
-            Raw<R> k[8];
-            Raw<T> v[8];
+            Raw k[8], v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const unsigned from = __shfl_sync(kAll, at, 8 * group + j);
                 const bool there = __shfl_sync(kAll, (int)live, 8 * group + j);
-                k[j] = Raw<R>{};
-                v[j] = Raw<T>{};
+                k[j] = v[j] = Raw{};
                 if (there) {
-                    load_raw<R>(a.c.k, from, c, k[j]);
-                    load_raw<T>(a.c.v, from, c, v[j]);
+                    k[j] = load_raw(a.c.k, from, c);
+                    v[j] = load_raw(a.c.v, from, c);
                 }
             }
             attend(k, v, qs[warp], c, live, row, run);
@@ -256,7 +175,7 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_con
         if (padding) { by = 0.f; z = -INFINITY; }
         if (bad && !padding) by = z = NAN;
         const int d = 8 * c + 4 * up2 + 2 * up1;
-        store2<T>(out + (size_t)g * kHeadDim + d, o2[0] * by, o2[1] * by);
+        *reinterpret_cast<float2*>(out + (size_t)g * kHeadDim + d) = make_float2(o2[0] * by, o2[1] * by);
         if (lane == 0) lse[g] = z * kLn2;
     }
     if (bad && !padding && lane == 0) raise_status(a.status, kStatusPage);
@@ -264,18 +183,15 @@ __global__ void __launch_bounds__(32 * kWarps) attention_kernel(const __grid_con
 
 }  // namespace
 
-cudaError_t launch_attention(const AttnArgs& args, bool bf16, cudaStream_t st) {
+cudaError_t launch_attention_f32(const AttnArgs& args, cudaStream_t st) {
     AttnArgs a = args;
     const long long units = (long long)a.N * a.c.Hkv;
     a.parts = (int)std::max(1LL, std::min<long long>(a.G, 152LL * 16 / units));
     a.per_part = (a.G + a.parts - 1) / a.parts;
     a.parts = (a.G + a.per_part - 1) / a.per_part;
     const dim3 grid((unsigned)((units * a.parts + kWarps - 1) / kWarps)), block(32 * kWarps);
-    if (a.parents)
-        return bf16 ? launch_kernel(attention_kernel<__nv_bfloat16, true>, grid, block, 0, st, a)
-                    : launch_kernel(attention_kernel<float, true>, grid, block, 0, st, a);
-    return bf16 ? launch_kernel(attention_kernel<__nv_bfloat16, false>, grid, block, 0, st, a)
-                : launch_kernel(attention_kernel<float, false>, grid, block, 0, st, a);
+    return a.parents ? launch_kernel(attention_kernel<true>, grid, block, 0, st, a)
+                     : launch_kernel(attention_kernel<false>, grid, block, 0, st, a);
 }
 
 }  // namespace cache

@@ -9,6 +9,10 @@ and a tree of 4: 20u of sum |q d k d| at most, with the slot's interpolation 24u
 A below bounds that sum.  exp2 has 2 ulp and its argument, at most 2A + 1 log2 e
 in size, 3 roundings: a weight is off by 2 * 24u A + 6u (A + 1) + 4u of itself,
 and so is the sum of weights; values are summed over R rows: (R / 4 + 8) u.
+bf16 goes through products of 16-bit halves: those of q keep 22 bits (4u), those of
+p 16 (2^-17 = 128u), and a product of 16 may lose of each of its 17 terms what lies
+below 2^-24 of the largest: four of them in a score, 4 * 17 u A, and two for 32
+rows in a value, (R / 32 + 1) * 34 u V.
 """
 from __future__ import annotations
 
@@ -106,8 +110,10 @@ class Model:
 def check(got, want, W, K):
     """got: out, lse; want: out, lse, A, V."""
     (out, lse), (ro, rl, A, V) = (t.cpu() for t in got), want
-    weight = 48 * U * A + 6 * U * (A + 1) + 4 * U
-    rows = (W + 1 + 2 * K) / 4 + 8
+    halves = out.dtype == BF
+    score = (24 + halves * (4 + 4 * 17)) * U * A
+    weight = 2 * score + 6 * U * (A + 1) + 4 * U
+    rows = (W + 1 + 2 * K) / 4 + 8 + halves * (128 + 34 * ((W + 1 + 2 * K) / 32 + 1))
     half = torch.finfo(out.dtype).eps / 2
     err = (out.double() - ro).abs()
     assert (err <= (V * (2 * weight + rows * U))[..., None] * (1 + half) + half * ro.abs()).all(), float(err.max())
