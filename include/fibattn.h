@@ -365,7 +365,8 @@ int fibattn_clip_grads(int n, const void* const* grads, void* const* outs,
  * [seqs][pages_per_seq] of 32-bit page numbers on the device.  Storage slot j of
  * sequence b is row j % page_rows of page table[b][j / page_rows].  Strides are
  * in elements, the last dimension is contiguous and the others are any multiples
- * of 64 (a layer of a larger pool, pages with the heads before the rows, ...).
+ * of 64 (a layer of a larger pool, pages with the heads before the rows, ...);
+ * the pools start on 32 bytes.
  * Limits: pages_per_seq * page_rows <= 2^30; every row's offset, counted in rows
  * of 64, below 2^32.
  *

@@ -642,7 +642,8 @@ class PagedCache:
         if strides != _pool_strides(v_pages):
             raise ValueError("k_pages and v_pages must have the same strides")
         self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
-        self.dtype, self.Hkv, self.index = v_pages.dtype, k_pages.shape[2], index
+        self.dtype, self.Hkv, self.index, self.device = v_pages.dtype, k_pages.shape[2], index, k_pages.device
+        self.unit = 16 // v_pages.element_size()          # strides of tokens are multiples of this
         pages, rows, heads, D = k_pages.shape
         self._struct = CacheStruct()
         self._at = ctypes.addressof(self._struct)
@@ -667,30 +668,58 @@ def _pool_strides(t):
     return tuple(64 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()))
 
 
-def _token_strides(t, cache, name):
-    """Strides of tokens [N, heads, 64] as the library takes them."""
-    if t.dim() != 3 or t.shape[2] != 64 or t.dtype != cache.dtype or t.get_device() != cache.index:
+def _tokens(t, cache, name):
+    """(pointer, token stride, head stride) of tokens [N, heads, 64] as the library takes them."""
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != 64 or t.dtype is not cache.dtype or t.get_device() != cache.index:
         raise ValueError(f"{name} must be [tokens, heads, 64] of the cache's dtype, on its device")
     token, head, last = t.stride()
-    N, heads, _ = t.shape
-    token, head = 0 if N == 1 else token, 0 if heads == 1 else head
-    unit = 8 if cache.dtype == torch.bfloat16 else 4
-    if last != 1 or token % unit or head % unit:
+    if shape[0] == 1:
+        token = 0
+    if shape[1] == 1:
+        head = 0
+    if last != 1 or token % cache.unit or head % cache.unit:
         raise ValueError(f"{name} must be contiguous in its last dimension, with strides of whole 16 bytes")
-    return token, head
+    return t.data_ptr(), token, head
 
 
-def _check_ints(N, index, **given):
-    for name, t in given.items():
-        if name == "positions" and t is None:
-            raise ValueError("positions are needed")
-        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != N or t.get_device() != index or
-                              not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous int32 tensor of {N} values on the cache's device")
+def _ints(t, shape, index, name):
+    """The pointer of a tensor with one int32 per token."""
+    if t is None or t.dtype is not torch.int32 or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {shape[0]} values on the cache's device")
+    return t.data_ptr()
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+# What the library reads on the host at a call on the cache, by value: finding a few
+# numbers again takes a fraction of the time of handing them over anew.
+_offset_tables, _opt_structs = {}, {}
+
+
+def _offset_table(offsets):
+    """(address of the offsets as floats, how many, what has to live meanwhile)"""
+    f = _offsets(offsets)
+    key = f.tobytes()
+    got = _offset_tables.get(key)
+    if got is None:
+        if len(_offset_tables) > 255:
+            _offset_tables.clear()
+        f = f.copy()
+        got = _offset_tables[key] = f.ctypes.data, f.size, f
+    return got
+
+
+def _opt_struct(scale, dedup, round_offsets):
+    """(address of the options, or None for the library's own; what has to live meanwhile)"""
+    if scale is None and dedup and not round_offsets:
+        return None, None
+    key = scale if scale is None else float(scale), bool(dedup), bool(round_offsets)
+    got = _opt_structs.get(key)
+    if got is None:
+        if len(_opt_structs) > 255:
+            _opt_structs.clear()
+        o = _opts(0.0, scale, 0, dedup, round_offsets=round_offsets)
+        got = _opt_structs[key] = ctypes.addressof(o), o
+    return got
 
 
 def cache_append(cache: PagedCache, k, v, positions, *, seqs=None, slots=None, stream=None):
@@ -702,14 +731,18 @@ def cache_append(cache: PagedCache, k, v, positions, *, seqs=None, slots=None, s
     sequence is padding.  Nothing is returned."""
     if stream is not None:
         return _on_stream(stream, cache_append, cache, k, v, positions, seqs=seqs, slots=slots)
-    ks, vs = _token_strides(k, cache, "k"), _token_strides(v, cache, "v")
-    N, index = k.shape[0], cache.index
-    if v.shape != k.shape or k.shape[1] != cache.Hkv:
+    index, shape = cache.index, k.shape
+    k_at, v_at = _tokens(k, cache, "k"), _tokens(v, cache, "v")
+    if v.shape != shape or shape[1] != cache.Hkv:
         raise ValueError("k and v must be [tokens, the cache's Hkv, 64]")
-    _check_ints(N, index, positions=positions, seqs=seqs, slots=slots)
+    each = shape[:1]
+    p = _ints(positions, each, index, "positions")
+    b = None if seqs is None else _ints(seqs, each, index, "seqs")
+    at = None if slots is None else _ints(slots, each, index, "slots")
     _check_device(index)
-    _check(lib().fibattn_cache_append(cache._at, k.data_ptr(), *ks, v.data_ptr(), *vs, positions.data_ptr(), _ptr(slots),
-                                      _ptr(seqs), N, _raw_stream(index)))
+    rc = lib().fibattn_cache_append(cache._at, *k_at, *v_at, p, at, b, shape[0], _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def cached_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, *, seqs=None, scale=None, dedup=True,
@@ -744,28 +777,30 @@ def tree_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, par
 
 
 def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, scale, dedup, round_offsets, out, lse):
-    strides, index = _token_strides(q, cache, "q"), cache.index
-    N, H, D = q.shape
-    _check_ints(N, index, positions=positions, seqs=seqs, parents=parents, slots=slots)
+    at, index, shape = _tokens(q, cache, "q"), cache.index, q.shape
+    each, N, H = shape[:1], shape[0], shape[1]
+    p = _ints(positions, each, index, "positions")
+    b = None if seqs is None else _ints(seqs, each, index, "seqs")
     _check_device(index)
-    f = _offsets(offsets)
+    f, K, alive = _offset_table(offsets)
+    o, kept = _opt_struct(scale, dedup, round_offsets)
     if out is None:
-        out = torch.empty((N, H, D), dtype=q.dtype, device=q.device)
-    elif out.dtype != q.dtype or out.shape != q.shape or out.get_device() != index or not out.is_contiguous():
+        out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
+    elif out.dtype is not cache.dtype or out.shape != shape or out.get_device() != index or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape and dtype on its device")
     if lse is None:
-        lse = torch.empty((N, H), dtype=torch.float32, device=q.device)
-    elif lse.dtype != torch.float32 or lse.shape != (N, H) or lse.get_device() != index or not lse.is_contiguous():
+        lse = torch.empty((N, H), dtype=torch.float32, device=cache.device)
+    elif lse.dtype is not torch.float32 or lse.shape != (N, H) or lse.get_device() != index or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [N, H] on q's device")
-    o = None if scale is None and dedup and not round_offsets else \
-        ctypes.addressof(opts := _opts(0.0, scale, 0, dedup, round_offsets=round_offsets))   # noqa: F841 (kept alive)
-    L, tail = lib(), (N, H, int(W), float(alpha), f.ctypes.data, len(f), o, _raw_stream(index))
     if parents is None:
-        _check(L.fibattn_cached_fwd(cache._at, q.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(),
-                                    positions.data_ptr(), _ptr(seqs), *tail))
+        rc = lib().fibattn_cached_fwd(cache._at, *at, out.data_ptr(), lse.data_ptr(), p, b, N, H, int(W), float(alpha), f, K,
+                                      o, _raw_stream(index))
     else:
-        _check(L.fibattn_tree_fwd(cache._at, q.data_ptr(), *strides, out.data_ptr(), lse.data_ptr(),
-                                  positions.data_ptr(), parents.data_ptr(), slots.data_ptr(), _ptr(seqs), *tail))
+        rc = lib().fibattn_tree_fwd(cache._at, *at, out.data_ptr(), lse.data_ptr(), p, _ints(parents, each, index, "parents"),
+                                    _ints(slots, each, index, "slots"), b, N, H, int(W), float(alpha), f, K, o,
+                                    _raw_stream(index))
+    if rc:
+        _check(rc)
     return out, lse
 
 

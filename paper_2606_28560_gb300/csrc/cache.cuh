@@ -56,7 +56,8 @@ struct AttnArgs {
     const int* slots;
     int N, H, G;                                     // G = H / Hkv query heads per key/value head
     int parts, per_part;                             // fp32: a group's heads are cut into parts of per_part
-    unsigned units;                                  // bf16: warps
+    int run;                                         // bf16: key/value heads of a warp
+    unsigned units;                                  // warps
     FastDiv dRest, dParts;                           // by the warps of a token, by the parts of a group
     float scale;                                     // times log2 e: softmax in base 2
     Rows r;

@@ -101,7 +101,6 @@ int attention(const fibattn_cache* c, const void* q, long long q_token, long lon
             }
     a.r.window = W + 1;
     a.r.total = 2 * a.r.pairs + a.r.singles + a.r.window;
-    if ((rc = bind_device_context())) return rc;
     if ((rc = device_status_word(&a.status))) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     ProfScope p(parents ? "tree_fwd" : "cached_fwd", st);
@@ -125,8 +124,8 @@ int fibattn_cache_init(fibattn_cache* c, void* k_pages, void* v_pages, int pages
     if ((long long)page_rows * pages_per_seq > kMaxSlots)
         return set_error(FIBATTN_ERR_INVALID_ARG, "page_rows * pages_per_seq must be at most 2^30");
     if (!k_pages || !v_pages || !table) return set_error(FIBATTN_ERR_INVALID_ARG, "NULL pool or table pointer");
-    if (misaligned16(k_pages) || misaligned16(v_pages) || ((uintptr_t)table & 3u))
-        return set_error(FIBATTN_ERR_INVALID_ARG, "pool pointers must be 16-byte aligned (table: 4-byte)");
+    if (((uintptr_t)k_pages & 31u) || ((uintptr_t)v_pages & 31u) || ((uintptr_t)table & 3u))
+        return set_error(FIBATTN_ERR_INVALID_ARG, "pool pointers must be 32-byte aligned (table: 4-byte)");
     const long long strides[3] = {page_stride, row_stride, head_stride}, sizes[3] = {pages, page_rows, Hkv};
     long long last = 0;                              // the last row of the pool, counted in rows of 64
     for (int i = 0; i < 3; ++i) {
@@ -183,7 +182,6 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
     a.slots = slots;
     a.seqs = seqs;
     a.N = N;
-    if ((rc = bind_device_context())) return rc;
     if ((rc = device_status_word(&a.status))) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     ProfScope p("cache_append", st);

@@ -16,9 +16,9 @@
 // share one set of sums, one softmax and one way out.
 //   Scores: a lane of column n holds 16 of row n's 64 dims, as they lie in memory;
 // the order of dims within a product is free as long as q has the same.
-//   Values: a lane's four rows of a 16-row product are those whose weights it holds
-// after the scores; it loads the same eight dims of each and pairs them by byte
-// permutes; product j takes dim j of the eight, so a lane ends with 16 dims in order.
+//   Values: the sum runs over rows, of which a lane needs four and of each a part, so
+// that loads into registers meet in the same banks; they go through shared memory,
+// 16 bytes at a time, and are transposed on their way out of it.
 #include <algorithm>
 
 #include "cache_rows.cuh"
@@ -39,47 +39,46 @@ __device__ __forceinline__ void fit_half(float largest, float& up, float& down) 
     down = __uint_as_float((unsigned)(254 - e) << 23);
 }
 
-struct Part { uint4 x[8]; };                         // a lane's part of 32 rows' keys or values
-struct Places { unsigned k[4], v[8]; };              // where they lie, for key/value head 0
+constexpr unsigned kBytes = 32 * kHeadDim * 2;       // of 32 rows of a head
+struct Places { unsigned k[4], v[8]; };              // where rows lie, for key/value head 0: 8i + g; 4i + lane / 8
 
-__device__ __forceinline__ void load_keys(const AttnArgs& a, const Places& p, unsigned head, int t, Part& b) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint4* row = reinterpret_cast<const uint4*>(
-            static_cast<const __half*>(a.c.k) + 8 * t + (size_t)(p.k[i] + head) * kHeadDim);
-        b.x[2 * i] = row[0];
-        b.x[2 * i + 1] = row[4];
-    }
+// Row 8i + g's part.
+__device__ __forceinline__ void load_keys(const AttnArgs& a, unsigned row, int t, unsigned* x) {
+    const __half* from = static_cast<const __half*>(a.c.k) + 16 * t + (size_t)row * kHeadDim;
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
+                 : "l"(from));
 }
-__device__ __forceinline__ int value_row(int i, int t) { return 8 * (i >> 1) + 2 * t + (i & 1); }
-__device__ __forceinline__ void load_values(const AttnArgs& a, const Places& p, unsigned head, int g, Part& b) {
+// Chunk c (16 bytes) of row r lies at r * 128 + 16 (c ^ r % 8): neither these writes nor
+// the reads below meet in a bank.
+__device__ __forceinline__ void load_values(const AttnArgs& a, const Places& p, unsigned head, int lane, unsigned to) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        b.x[i] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.c.v) + 8 * g +
-                                                 (size_t)(p.v[i] + head) * kHeadDim);
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3), c = lane & 7;
+        const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.c.v) + 8 * c + (size_t)(p.v[i] + head) * kHeadDim;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n"
+                     :: "r"(to + r * 128 + ((c ^ (r & 7)) << 4)), "l"(from) : "memory");
+    }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
 }
 
 // A product of the heads' weights of 16 rows with these rows' values, for each of eight
-// dims; kFirst: not added to anything.
-template <bool kFirst>
-__device__ __forceinline__ void add_values(float (&acc)[8][4], const unsigned* p, const uint4* v) {
+// chunks of dims; from: the lane's place in the first.
+__device__ __forceinline__ void add_values(float (&acc)[8][4], const unsigned* p, unsigned from) {
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int j = 0; j < 4; ++j) {
         unsigned r[4];
+        mma::ldsm_x4_t(from ^ (j << 5), r[0], r[1], r[2], r[3]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = w == 0 ? v[i].x : w == 1 ? v[i].y : w == 2 ? v[i].z : v[i].w;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const unsigned pick = e ? 0x7632 : 0x5410, b0 = __byte_perm(r[0], r[1], pick), b1 = __byte_perm(r[2], r[3], pick);
-            if (kFirst) mma::mma_bf16_16816_z(acc[2 * w + e], p, b0, b1);
-            else mma::mma_bf16_16816(acc[2 * w + e], p, b0, b1);
-        }
+        for (int e = 0; e < 2; ++e)
+            mma::mma_bf16_16816(acc[2 * j + e], p, r[2 * e], r[2 * e + 1]);
     }
 }
 
-// kRun: key/value heads of a warp; kMany: queries read more than 32 rows.
-template <int kRun, bool kMany, bool kTree>
-__global__ void __launch_bounds__(32 * kWarps, 4) attention_mma_kernel(const __grid_constant__ AttnArgs a) {
+// kMany: queries read more than 32 rows.
+template <bool kMany, bool kTree>
+__global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kernel(const __grid_constant__ AttnArgs a) {
+    __shared__ __align__(128) unsigned char values[kWarps][2][kBytes];
     __shared__ __align__(16) float turn[kWarps][2][kHalf];         // cos and sin of the token's angles
     grid_dependency_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -89,25 +88,31 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_mma_kernel(const __g
     const int pos = a.positions[n], seq = a.seqs ? a.seqs[n] : (int)n;
     // the lane's query head: the mine-th key/value head of the warp's, and its own number
     const unsigned run = fdiv(rest, a.dParts), part = rest - run * a.dParts.d;
-    const int h0 = run * kRun, mine = kRun == 1 ? 0 : g / a.G, own = kRun == 1 ? (int)part * 8 + g : g - mine * a.G;
-    const bool real = mine < kRun && own < a.G && h0 + mine < a.c.Hkv;
+    const int h0 = run * a.run, heads = min(a.run, a.c.Hkv - h0), mine = a.G >= 8 ? 0 : g / a.G;
+    const int own = (int)part * 8 + g - mine * a.G;
+    const bool real = mine < heads && own < a.G;
     const int head = (h0 + mine) * a.G + own;
-    uint4 qa = make_uint4(0, 0, 0, 0), qb = qa;
+    uint4 qa[2] = {}, qb[2] = {};                      // dims 16t .. 16t+15 and those that they turn with
     if (real) {
         const uint4* row = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + n * a.q_token +
                                                           head * a.q_head);
-        qa = row[t];
-        qb = row[t + 4];
+        qa[0] = row[2 * t];
+        qa[1] = row[2 * t + 1];
+        qb[0] = row[2 * (t ^ 2)];
+        qb[1] = row[2 * (t ^ 2) + 1];
     }
     const int* pages = a.c.table + (size_t)max(seq, 0) * a.c.pages_per_seq;
     const bool padding = pos < 0 || seq < 0;
     bool bad = !padding && seq >= a.c.seqs, turned = false;
     float m = -INFINITY, l = 0.f, sc = 0.f, acc[8][4];
     unsigned qf[4][4];                                 // four products of 16 dims: (half, half of the dims)
+    auto clear = [&] {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
+            for (int e = 0; e < 4; ++e) acc[j][e] = 0.f;
+    };
+    if (kMany) clear();
     for (int r0 = 0; r0 < (kMany ? a.r.total : 1) && !padding && !bad; r0 += 32) {
         const RowOf row = row_of(a.r, r0 + lane);
         const unsigned live = __ballot_sync(kAll, r0 + lane < a.r.total && pos >= row.need);
@@ -126,67 +131,59 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_mma_kernel(const __g
 #pragma unroll
         for (int i = 0; i < 4; ++i) at.k[i] = __shfl_sync(kAll, place, 8 * i + g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at.v[i] = __shfl_sync(kAll, place, value_row(i, t));
-        // the warp's key/value heads, keys of all and then values of all, two parts under way
-        Part b[2];
-        auto load = [&](int item) {
-            const unsigned h = (unsigned)min(h0 + item % kRun, a.c.Hkv - 1) * a.c.head_stride;
-            if (item < kRun) load_keys(a, at, h, t, b[item & 1]);
-            else load_values(a, at, h, g, b[item & 1]);
-        };
-        load(0);
-        load(1);
+        for (int i = 0; i < 8; ++i) at.v[i] = __shfl_sync(kAll, place, 4 * i + (lane >> 3));
+        // of the warp's key/value heads, the keys of one and the values of two are under way
+        unsigned k[4][8];
+        const unsigned vs = mma::smem_u32(values[warp][0]), step = a.c.head_stride, first = h0 * step;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_keys(a, at.k[i] + first, t, k[i]);
+        if (kMany) __syncwarp();                       // the values of the rows before have been read
+        load_values(a, at, first, lane, vs);
+        if (heads > 1) load_values(a, at, first + step, lane, vs + kBytes);
         if (!turned) {
             turned = true;
             rope_cs_f32(a.c.rope, lane, pos, turn[warp][0][lane], turn[warp][1][lane]);
             __syncwarp();
-            float y[16];
-            const unsigned w[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
+            const unsigned w[8] = {qa[0].x, qa[0].y, qa[0].z, qa[0].w, qa[1].x, qa[1].y, qa[1].z, qa[1].w};
+            const unsigned o[8] = {qb[0].x, qb[0].y, qb[0].z, qb[0].w, qb[1].x, qb[1].y, qb[1].z, qb[1].w};
+            const float sign = t < 2 ? -1.f : 1.f;
+            float y[16], largest = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[2 * i] = __uint_as_float(w[i] << 16);
-                y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-            float largest = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float cs = turn[warp][0][8 * t + i], sn = turn[warp][1][8 * t + i], u = y[i], v = y[8 + i];
-                y[i] = u * cs - v * sn;
-                y[8 + i] = v * cs + u * sn;
-                largest = fmaxf(largest, fmaxf(fabsf(y[i]), fabsf(y[8 + i])));
+            for (int i = 0; i < 16; ++i) {
+                const float cs = turn[warp][0][16 * (t & 1) + i], sn = turn[warp][1][16 * (t & 1) + i] * sign;
+                const float u = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+                const float v = __uint_as_float(i & 1 ? o[i >> 1] & 0xffff0000u : o[i >> 1] << 16);
+                y[i] = u * cs + v * sn;
+                largest = fmaxf(largest, fabsf(y[i]));
             }
             float up, down;
             fit_half(mma::quad_max(largest), up, down);
             sc = down * a.scale;
 #pragma unroll
-            for (int s = 0; s < 4; ++s)                // dims 8t + 4 (s & 1) + 32 (s >> 1) + 0..3
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int d = 8 * (s >> 1) + 4 * (s & 1) + 2 * e;
-                    const float y0 = y[d] * up, y1 = y[d + 1] * up;
-                    const __half2 hi = __floats2half2_rn(y0, y1);
-                    qf[s][2 * e] = *reinterpret_cast<const unsigned*>(&hi);
-                    const float2 f = __half22float2(hi);
-                    qf[s][2 * e + 1] = mma::pack_f16(y0 - f.x, y1 - f.y);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float y0 = y[2 * i] * up, y1 = y[2 * i + 1] * up;
+                const __half2 hi = __floats2half2_rn(y0, y1);
+                qf[i >> 1][2 * (i & 1)] = *reinterpret_cast<const unsigned*>(&hi);
+                const float2 f = __half22float2(hi);
+                qf[i >> 1][2 * (i & 1) + 1] = mma::pack_f16(y0 - f.x, y1 - f.y);
+            }
         }
         float s[4][2];
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            const Part& k = b[j & 1];
+#pragma unroll 1
+        for (int j = 0; j < heads; ++j) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float c[4];
-                mma::mma_f16_16816_z(c, qf[0], k.x[2 * i].x, k.x[2 * i].y);
-                mma::mma_f16_16816(c, qf[1], k.x[2 * i].z, k.x[2 * i].w);
-                mma::mma_f16_16816(c, qf[2], k.x[2 * i + 1].x, k.x[2 * i + 1].y);
-                mma::mma_f16_16816(c, qf[3], k.x[2 * i + 1].z, k.x[2 * i + 1].w);
+                mma::mma_f16_16816_z(c, qf[0], k[i][0], k[i][1]);
+                mma::mma_f16_16816(c, qf[1], k[i][2], k[i][3]);
+                mma::mma_f16_16816(c, qf[2], k[i][4], k[i][5]);
+                mma::mma_f16_16816(c, qf[3], k[i][6], k[i][7]);
+                if (j + 1 < heads) load_keys(a, at.k[i] + first + (j + 1) * step, t, k[i]);
                 if (j == 0 || mine == j) {
                     s[i][0] = c[0] + c[2];
                     s[i][1] = c[1] + c[3];
                 }
             }
-            if (j + 2 < 2 * kRun) load(j + 2);
         }
         const unsigned pairs = __ballot_sync(kAll, row.pair);
         float weight[4][2], top = -INFINITY;
@@ -221,60 +218,64 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_mma_kernel(const __g
             p[i][0] = mma::pack_bf16(p0, p1);
             p[i][1] = mma::pack_bf16(p0 - __uint_as_float(p[i][0] << 16), p1 - __uint_as_float(p[i][0] & 0xffff0000u));
         }
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) {
-            const Part& v = b[(kRun + j) & 1];
+        if (!kMany) clear();
+#pragma unroll 1
+        for (int j = 0; j < heads; ++j) {
+            if (j + 1 < heads) asm volatile("cp.async.wait_group 1;\n" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+            __syncwarp();
             unsigned pj[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) pj[i] = kRun == 1 || mine == j ? p[i >> 1][i & 1] : 0u;
-            if (!kMany && j == 0) add_values<true>(acc, pj, v.x);
-            else add_values<false>(acc, pj, v.x);
-            add_values<false>(acc, pj + 4, v.x + 4);
-            if (kRun + j + 2 < 2 * kRun) load(kRun + j + 2);
+            for (int i = 0; i < 8; ++i) pj[i] = mine == j ? p[i >> 1][i & 1] : 0u;
+            const unsigned from = vs + (j & 1) * kBytes + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+            add_values(acc, pj, from);
+            add_values(acc, pj + 4, from + 16 * 128);
+            if (j + 2 < heads) {
+                __syncwarp();                          // all lanes have read what is written over
+                load_values(a, at, first + (j + 2) * step, lane, vs + (j & 1) * kBytes);
+            }
         }
     }
     l = mma::quad_sum(l);
-    float z = m + log2f(l), by = 1.f / l;
-    if (padding) { by = 0.f; z = -INFINITY; }
-    if (bad) by = z = NAN;
+    float z = m + log2f(l);
+    const float by = 1.f / l, none = bad ? NAN : 0.f;
+    if (padding) z = -INFINITY;
+    if (bad) z = NAN;
     if (real) {
         const size_t at = (size_t)n * a.H + head;
-        uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.out) + at * kHeadDim + 16 * t);
-        unsigned w[8];
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at * kHeadDim + 2 * t;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            w[j] = mma::pack_bf16((acc[2 * j][0] + acc[2 * j][2]) * by, (acc[2 * j + 1][0] + acc[2 * j + 1][2]) * by);
-            w[4 + j] = mma::pack_bf16((acc[2 * j][1] + acc[2 * j][3]) * by, (acc[2 * j + 1][1] + acc[2 * j + 1][3]) * by);
-        }
-        out[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        out[1] = make_uint4(w[4], w[5], w[6], w[7]);
+        for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<__nv_bfloat162*>(out + 8 * j) =
+                padding || bad ? __float2bfloat162_rn(none)
+                               : __floats2bfloat162_rn((acc[j][0] + acc[j][2]) * by, (acc[j][1] + acc[j][3]) * by);
         if (t == 0) a.lse[at] = z * kLn2;
     }
     if (bad && lane == 0) raise_status(a.status, kStatusPage);
 }
 
-template <int kRun, bool kMany>
-cudaError_t launch(AttnArgs& a, cudaStream_t st) {
-    const unsigned parts = (a.G + 7) / 8, runs = (a.c.Hkv + kRun - 1) / kRun;
-    a.units = (unsigned)a.N * runs * parts;
-    a.dRest = FastDiv::make(runs * parts);
-    a.dParts = FastDiv::make(parts);
+template <bool kMany>
+cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
     const dim3 grid((a.units + kWarps - 1) / kWarps), block(32 * kWarps);
-    return a.parents ? launch_kernel(attention_mma_kernel<kRun, kMany, true>, grid, block, 0, st, a)
-                     : launch_kernel(attention_mma_kernel<kRun, kMany, false>, grid, block, 0, st, a);
+    return a.parents ? launch_kernel(attention_mma_kernel<kMany, true>, grid, block, 0, st, a)
+                     : launch_kernel(attention_mma_kernel<kMany, false>, grid, block, 0, st, a);
 }
 
 }  // namespace
 
 cudaError_t launch_attention_mma(const AttnArgs& args, cudaStream_t st) {
     AttnArgs a = args;
-    // key/value heads of a warp: as many as its eight query heads allow, once that leaves
-    // warps enough for the GPU
-    const long long warps = (long long)a.N * a.c.Hkv;
-    const long long most = std::min<long long>(std::min(8 / std::min(a.G, 8), a.c.Hkv), warps / (152 * 8));
-    if (a.r.total > 32) return launch<1, true>(a, st);
-    return most >= 8 ? launch<8, false>(a, st) : most >= 4 ? launch<4, false>(a, st)
-           : most >= 2 ? launch<2, false>(a, st) : launch<1, false>(a, st);
+    // Key/value heads of a warp, as far as its eight query heads go: the rows are looked up
+    // once for all, but few warps leave the GPU waiting.  Of 8, one token each, us: 256 tokens
+    // with 1, 2, 4 heads a warp 5.2, 4.7, 5.1; 512 tokens 8.5, 6.2, 6.7; 1024 tokens with 2, 4,
+    // 8 heads 13.7, 11.2, 13.9; 4096 tokens 48.4, 43.1, 42.7.
+    const int units = a.N * a.c.Hkv, most = std::min(8 / std::min(a.G, 8), a.c.Hkv);
+    a.run = a.r.total > 32 || units < 2048 ? 1 : std::min(most, std::max(2, units / 2048));
+    const unsigned parts = (a.G + 7) / 8, runs = (a.c.Hkv + a.run - 1) / a.run;
+    a.units = (unsigned)a.N * runs * parts;
+    a.dRest = FastDiv::make(runs * parts);
+    a.dParts = FastDiv::make(parts);
+    return a.r.total > 32 ? launch<true>(a, st) : launch<false>(a, st);
 }
 
 }  // namespace cache
