@@ -31,7 +31,7 @@ struct AppendArgs {
     const int* slots;                                // or nullptr: positions
     const int* seqs;                                 // or nullptr: token n is sequence n
     int N;
-    int heads;                                       // heads per thread
+    int per;                                         // tokens of a warp
     unsigned* status;
 };
 
@@ -55,8 +55,7 @@ struct AttnArgs {
     const int* parents;                              // trees only
     const int* slots;
     int N, H, G;                                     // G = H / Hkv query heads per key/value head
-    int parts, per_part;                             // fp32: a group's heads are cut into parts of per_part
-    int run;                                         // bf16: key/value heads of a warp
+    int run;                                         // of a warp: key/value heads (bf16), query heads (fp32)
     unsigned units;                                  // warps
     FastDiv dRest, dParts;                           // by the warps of a token, by the parts of a group
     float scale;                                     // times log2 e: softmax in base 2

@@ -1,8 +1,14 @@
 // cache_append.cu -- keys and values of new tokens into a paged cache, the keys
 // rotated on the way: k~ = R(pos) k (arXiv 2606.28560, Section 2: RoPE at true
 // positions, before the gather), values as they are.
-#include <algorithm>
-
+//
+// Bound by memory: each value is read and written once.  A warp has eight rows (heads
+// of one token, or of several), four lanes to a row, so that a rotation's pair stays
+// in its lane.  What is read does not wait for where it goes: the loads are under way
+// while the warp looks up pages and evaluates its tokens' 32 angles, one to a lane,
+// once for all heads.  Of 64 prompts of 1024 tokens (8 heads, bf16, 268 MB) 42.0 us,
+// 6.4 TB/s; two steps of a warp at once take 44.6, blocks of eight warps 42.9 but the
+// 256 tokens of a decoding batch 3.0 us instead of 2.6.
 #include "cache.cuh"
 
 namespace fibattn {
@@ -10,50 +16,88 @@ namespace cache {
 
 namespace {
 
+constexpr int kWarps = 4;
+constexpr unsigned kAll = 0xffffffffu;
+
+// A lane's 16 of a row's 64 elements, 8c .. 8c+7 and 32 more, as they lie in memory.
+template <typename T> struct Part { uint4 x[sizeof(T)]; };
 template <typename T>
-__device__ __forceinline__ void copy_chunk(const T* from, T* to, int c) {
-    constexpr int n = (int)sizeof(T) / 2;            // 16-byte vectors in 8 elements
-    const uint4* f = reinterpret_cast<const uint4*>(from + 8 * c);
-    const uint4* g = reinterpret_cast<const uint4*>(from + kHalf + 8 * c);
-    uint4 x[2 * n];
-#pragma unroll
-    for (int i = 0; i < n; ++i) { x[i] = f[i]; x[n + i] = g[i]; }
+__device__ __forceinline__ void load_part(const T* row, int c, Part<T>& p) {
+    constexpr int n = (int)sizeof(T) / 2;
 #pragma unroll
     for (int i = 0; i < n; ++i) {
-        reinterpret_cast<uint4*>(to + 8 * c)[i] = x[i];
-        reinterpret_cast<uint4*>(to + kHalf + 8 * c)[i] = x[n + i];
+        p.x[i] = reinterpret_cast<const uint4*>(row + 8 * c)[i];
+        p.x[n + i] = reinterpret_cast<const uint4*>(row + kHalf + 8 * c)[i];
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* row, int c, const Part<T>& p) {
+    constexpr int n = (int)sizeof(T) / 2;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        reinterpret_cast<uint4*>(row + 8 * c)[i] = p.x[i];
+        reinterpret_cast<uint4*>(row + kHalf + 8 * c)[i] = p.x[n + i];
+    }
+}
+__device__ __forceinline__ void unpack(const Part<float>& p, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4*>(x + 4 * i) = p.x[i];
+}
+__device__ __forceinline__ void unpack(const Part<__nv_bfloat16>& p, float* x) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const unsigned w[4] = {p.x[i].x, p.x[i].y, p.x[i].z, p.x[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            x[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+            x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        }
     }
 }
 
-// A thread has a token's pairs 8c .. 8c+7 for a run of heads: the angles are
-// evaluated once for the run.  Bound by memory: each value is read and written once.
 template <typename T>
-__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(32 * kWarps) append_kernel(const __grid_constant__ AppendArgs a) {
     using R = typename RotOf<T>::type;
+    __shared__ __align__(16) float turn[kWarps][8][2][kHalf];      // cos and sin of the tokens' angles
     grid_dependency_sync();
-    const int runs = (a.c.Hkv + a.heads - 1) / a.heads;
-    const long long items = (long long)a.N * runs * 4;
-    const long long it = blockIdx.x * (long long)blockDim.x + threadIdx.x;
-    if (it >= items) return;
-    const int c = (int)(it & 3), run = (int)((it >> 2) % runs), n = (int)((it >> 2) / runs);
-    const int pos = a.positions[n], seq = a.seqs ? a.seqs[n] : n;
-    if (pos < 0 || seq < 0) return;                  // padding
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, s = lane >> 2, c = lane & 3;
+    const int token = a.per > 1 ? s / a.c.Hkv : 0, h0 = s - token * a.c.Hkv;
+    const long long first = ((long long)blockIdx.x * kWarps + warp) * a.per, n = first + token;
+    if (first >= a.N) return;
+    bool there = token < a.per && n < a.N && h0 < a.c.Hkv;
+    const T* from_k = static_cast<const T*>(a.k) + n * a.k_token;
+    const T* from_v = static_cast<const T*>(a.v) + n * a.v_token;
+    Part<T> k, v;
+    int pos = -1;
     unsigned row = 0;
-    const int slot = a.slots ? a.slots[n] : pos;
-    if (seq >= a.c.seqs || !locate(a.c, a.c.table + (size_t)seq * a.c.pages_per_seq, slot, row)) {
-        raise_status(a.status, kStatusPage);
-        return;
+    if (there) {
+        load_part(from_k + h0 * a.k_head, c, k);
+        load_part(from_v + h0 * a.v_head, c, v);
+        pos = a.positions[n];
+        const int seq = a.seqs ? a.seqs[n] : (int)n, slot = a.slots ? a.slots[n] : pos;
+        if (pos < 0 || seq < 0) {
+            there = false;                             // padding
+        } else if (seq >= a.c.seqs || !locate(a.c, a.c.table + (size_t)seq * a.c.pages_per_seq, slot, row)) {
+            there = false;
+            if (c == 0 && h0 == 0) raise_status(a.status, kStatusPage);
+        }
     }
-    float cs[8], sn[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) rope_cs_f32(a.c.rope, 8 * c + u, pos, cs[u], sn[u]);
+    for (int j = 0; j < a.per; ++j) {                  // the first head of token j is in lane 4 j Hkv
+        const int at = __shfl_sync(kAll, pos, a.per > 1 ? 4 * j * a.c.Hkv : 0);
+        rope_cs_f32(a.c.rope, lane, max(at, 0), turn[warp][j][0][lane], turn[warp][j][1][lane]);
+    }
+    __syncwarp();
+    if (!there) return;
+    const float *cs = turn[warp][token][0] + 8 * c, *sn = turn[warp][token][1] + 8 * c;
     float largest = 0.f;
-    const int h1 = min(a.c.Hkv, (run + 1) * a.heads);
-    for (int h = run * a.heads; h < h1; ++h) {
-        const size_t at = (size_t)(row + h * a.c.head_stride) * kHeadDim;
+    for (int h = h0; h < a.c.Hkv; h += 8) {            // (more than once for a token of more than eight heads)
+        if (h != h0) {
+            load_part(from_k + h * a.k_head, c, k);
+            load_part(from_v + h * a.v_head, c, v);
+        }
+        const size_t to = (size_t)(row + h * a.c.head_stride) * kHeadDim;
         float x[16];
-        load_chunk(static_cast<const T*>(a.k) + n * a.k_token + h * a.k_head, c, x);
-        copy_chunk(static_cast<const T*>(a.v) + n * a.v_token + h * a.v_head, static_cast<T*>(a.c.v) + at, c);
+        unpack(k, x);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const float p = x[u], q = x[8 + u];
@@ -61,7 +105,8 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
             x[8 + u] = q * cs[u] + p * sn[u];
             largest = fmaxf(largest, fmaxf(fabsf(x[u]), fabsf(x[8 + u])));
         }
-        store_chunk(static_cast<R*>(a.c.k) + at, c, x);
+        store_chunk(static_cast<R*>(a.c.k) + to, c, x);
+        store_part(static_cast<T*>(a.c.v) + to, c, v);
     }
     if (sizeof(R) == 2 && largest >= 65520.f) raise_status(a.status, kStatusRange);   // rounds to infinity in fp16
 }
@@ -70,11 +115,11 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
 
 cudaError_t launch_append(const AppendArgs& args, bool bf16, cudaStream_t st) {
     AppendArgs a = args;
-    a.heads = (long long)a.N * a.c.Hkv * 4 > 152 * 2048 ? a.c.Hkv : 1;
-    const long long items = (long long)a.N * ((a.c.Hkv + a.heads - 1) / a.heads) * 4;
-    const dim3 grid((unsigned)((items + 255) / 256));
-    return bf16 ? launch_kernel(append_kernel<__nv_bfloat16>, grid, dim3(256), 0, st, a)
-                : launch_kernel(append_kernel<float>, grid, dim3(256), 0, st, a);
+    a.per = a.c.Hkv > 4 ? 1 : 8 / a.c.Hkv;
+    const long long warps = ((long long)a.N + a.per - 1) / a.per;
+    const dim3 grid((unsigned)((warps + kWarps - 1) / kWarps)), block(32 * kWarps);
+    return bf16 ? launch_kernel(append_kernel<__nv_bfloat16>, grid, block, 0, st, a)
+                : launch_kernel(append_kernel<float>, grid, block, 0, st, a);
 }
 
 }  // namespace cache
