@@ -5,23 +5,23 @@
 // p (1-w) and p w.
 //
 // A warp has one token and eight of its query heads: those of one key/value head, or
-// of several (kRun), as far as eight go.  32 rows at a time: each lane finds one row
-// through the page table, for all heads; then the rows are loaded straight into the
-// fragments of m16n8k16 products, one key/value head ahead of the products.  The
-// eight heads are rows 0-7 of the first operand and what their rounding to 16 bits
-// left is rows 8-15, so that q (two fp16 halves, 22 bits) and p (two bf16 halves, 16
-// bits) come with the products' idle half and fp32 sums.  A product with the rows of
-// one key/value head is right for its own query heads; the others' scores are not
-// taken, and their weights are 0 in its product with the values, so that all eight
-// share one set of sums, one softmax and one way out.
-//   Scores: a lane of column n holds 16 of row n's 64 dims, as they lie in memory;
-// the order of dims within a product is free as long as q has the same.
-//   Values: the sum runs over rows, of which a lane needs four and of each a part, so
-// that loads into registers meet in the same banks; they go through shared memory,
-// 16 bytes at a time, and are transposed on their way out of it.
-// Bound by memory where there are many sequences: 4096 single tokens of 8 heads 43.0 us,
-// 5.2 TB/s; by the chain of look-ups, loads and products of few resident warps where rows
-// come from L2 (8 chunks of 256 tokens 12.1 us) or there are few (one token 3.1 us).
+// of several, as far as eight go.  32 rows at a time: each lane finds one row through
+// the page table, for all heads; then m16n8k16 products take them.  The eight heads
+// are rows 0-7 of the first operand and what their rounding to 16 bits left is rows
+// 8-15, so that q (two fp16 halves, 22 bits) and p (two bf16 halves, 16 bits) come
+// with the products' idle half and fp32 sums.  A product with the rows of one
+// key/value head is right for its own query heads; the others' scores are not taken,
+// and their weights are 0 in its product with the values, so that all eight share one
+// set of sums, one softmax and one way out.
+//   Keys, then values, of one head after another go through a ring of shared memory,
+// 16 bytes at a time, and into the products' fragments by matrix loads, transposed for
+// the values, whose sum runs over rows; neither copies nor loads meet in a bank.
+// Bound by memory where there are many sequences: 4096 single tokens of 8 heads 39 to
+// 42 us, 5.3 to 5.7 TB/s of rows of 128 bytes; by the chain of look-ups, copies and products of the 16
+// warps that an SM holds where rows come from L2 (8 chunks of 256 tokens 12.6 us) or where
+// there are few (one token 3.1 us).  Keys straight into registers and values through
+// a ring of two took 43.0, 12.1 and 3.1 us, and 164 instead of 140 us for 128 chunks; two
+// stages and five blocks an SM 38.7, 12.9 and 3.2 at the best heads a warp for each.
 #include <algorithm>
 
 #include "cache_rows.cuh"
@@ -42,27 +42,19 @@ __device__ __forceinline__ void fit_half(float largest, float& up, float& down) 
     down = __uint_as_float((unsigned)(254 - e) << 23);
 }
 
-constexpr unsigned kBytes = 32 * kHeadDim * 2;       // of 32 rows of a head
-struct Places { unsigned k[4], v[8]; };              // where rows lie, for key/value head 0: 8i + g; 4i + lane / 8
+constexpr int kStages = 3;                           // of the ring
+constexpr unsigned kBytes = 32 * kHeadDim * 2;       // 32 rows of a head
 
-// Row 8i + g's part.
-__device__ __forceinline__ void load_keys(const AttnArgs& a, unsigned row, int t, unsigned* x) {
-    const __half* from = static_cast<const __half*>(a.c.k) + 16 * t + (size_t)row * kHeadDim;
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
-                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7])
-                 : "l"(from));
-}
-// Chunk c (16 bytes) of row r lies at r * 128 + 16 (c ^ r % 8): neither these writes nor
-// the reads below meet in a bank.
-__device__ __forceinline__ void load_values(const AttnArgs& a, const Places& p, unsigned head, int lane, unsigned to) {
+// 32 rows of a key/value head into a stage, eight lanes to a row; rows: this lane's, for
+// head 0.  Chunk c (16 bytes) of row r lies at r * 128 + 16 (c ^ r % 8).
+__device__ __forceinline__ void copy_rows(const void* pool, const unsigned (&rows)[8], unsigned head, int lane, unsigned to) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int r = 4 * i + (lane >> 3), c = lane & 7;
-        const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.c.v) + 8 * c + (size_t)(p.v[i] + head) * kHeadDim;
+        const __half* from = static_cast<const __half*>(pool) + 8 * c + (size_t)(rows[i] + head) * kHeadDim;
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n"
                      :: "r"(to + r * 128 + ((c ^ (r & 7)) << 4)), "l"(from) : "memory");
     }
-    asm volatile("cp.async.commit_group;\n" ::: "memory");
 }
 
 // A product of the heads' weights of 16 rows with these rows' values, for each of eight
@@ -81,8 +73,7 @@ __device__ __forceinline__ void add_values(float (&acc)[8][4], const unsigned* p
 // kMany: queries read more than 32 rows.
 template <bool kMany, bool kTree>
 __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kernel(const __grid_constant__ AttnArgs a) {
-    __shared__ __align__(128) unsigned char values[kWarps][2][kBytes];
-    __shared__ __align__(16) float turn[kWarps][2][kHalf];         // cos and sin of the token's angles
+    __shared__ __align__(128) unsigned char ring[kWarps][kStages][kBytes];
     grid_dependency_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const unsigned unit = blockIdx.x * kWarps + warp;
@@ -95,14 +86,12 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kern
     const int own = (int)part * 8 + g - mine * a.G;
     const bool real = mine < heads && own < a.G;
     const int head = (h0 + mine) * a.G + own;
-    uint4 qa[2] = {}, qb[2] = {};                      // dims 16t .. 16t+15 and those that they turn with
+    unsigned raw[8] = {};                              // dims 8c + 2t and the next, c < 8
     if (real) {
-        const uint4* row = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + n * a.q_token +
-                                                          head * a.q_head);
-        qa[0] = row[2 * t];
-        qa[1] = row[2 * t + 1];
-        qb[0] = row[2 * (t ^ 2)];
-        qb[1] = row[2 * (t ^ 2) + 1];
+        const unsigned* row = reinterpret_cast<const unsigned*>(static_cast<const __nv_bfloat16*>(a.q) + n * a.q_token +
+                                                                head * a.q_head);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) raw[c] = row[4 * c + t];
     }
     const int* pages = a.c.table + (size_t)max(seq, 0) * a.c.pages_per_seq;
     const bool padding = pos < 0 || seq < 0;
@@ -130,63 +119,73 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kern
         // a row that is not read stands for one that is: its score counts for nothing
         const unsigned some = __shfl_sync(kAll, place, __ffs(live) - 1);
         if (!lives) place = some;
-        Places at;
+        unsigned rows[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) at.k[i] = __shfl_sync(kAll, place, 8 * i + g);
+        for (int i = 0; i < 8; ++i) rows[i] = __shfl_sync(kAll, place, 4 * i + (lane >> 3));
+        // the ring: keys of each of the warp's key/value heads, then their values
+        const unsigned base_at = mma::smem_u32(ring[warp][0]), step = a.c.head_stride, first = h0 * step;
+        auto issue = [&](int item, int stage) {
+            if (item < 2 * heads)
+                copy_rows(item < heads ? a.c.k : a.c.v, rows, first + (item < heads ? item : item - heads) * step, lane,
+                          base_at + stage * kBytes);
+            asm volatile("cp.async.commit_group;\n" ::: "memory");
+        };
+        if (kMany) __syncwarp();                       // what is written over has been read
 #pragma unroll
-        for (int i = 0; i < 8; ++i) at.v[i] = __shfl_sync(kAll, place, 4 * i + (lane >> 3));
-        // of the warp's key/value heads, the keys of one and the values of two are under way
-        unsigned k[4][8];
-        const unsigned vs = mma::smem_u32(values[warp][0]), step = a.c.head_stride, first = h0 * step;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_keys(a, at.k[i] + first, t, k[i]);
-        if (kMany) __syncwarp();                       // the values of the rows before have been read
-        load_values(a, at, first, lane, vs);
-        if (heads > 1) load_values(a, at, first + step, lane, vs + kBytes);
+        for (int i = 0; i < kStages; ++i) issue(i, i);
         if (!turned) {
             turned = true;
-            rope_cs_f32(a.c.rope, lane, pos, turn[warp][0][lane], turn[warp][1][lane]);
-            __syncwarp();
-            const unsigned w[8] = {qa[0].x, qa[0].y, qa[0].z, qa[0].w, qa[1].x, qa[1].y, qa[1].z, qa[1].w};
-            const unsigned o[8] = {qb[0].x, qb[0].y, qb[0].z, qb[0].w, qb[1].x, qb[1].y, qb[1].z, qb[1].w};
-            const float sign = t < 2 ? -1.f : 1.f;
-            float y[16], largest = 0.f;
+            float cs, sn, y[16], largest = 0.f;
+            rope_cs_f32(a.c.rope, lane, pos, cs, sn);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float cs = turn[warp][0][16 * (t & 1) + i], sn = turn[warp][1][16 * (t & 1) + i] * sign;
-                const float u = __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
-                const float v = __uint_as_float(i & 1 ? o[i >> 1] & 0xffff0000u : o[i >> 1] << 16);
-                y[i] = u * cs + v * sn;
-                largest = fmaxf(largest, fabsf(y[i]));
-            }
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int m_ = 8 * c + 2 * t + e;
+                    const float co = __shfl_sync(kAll, cs, m_), si = __shfl_sync(kAll, sn, m_);
+                    const float u = __uint_as_float(e ? raw[c] & 0xffff0000u : raw[c] << 16);
+                    const float v = __uint_as_float(e ? raw[c + 4] & 0xffff0000u : raw[c + 4] << 16);
+                    y[2 * c + e] = u * co - v * si;
+                    y[8 + 2 * c + e] = v * co + u * si;
+                    largest = fmaxf(largest, fmaxf(fabsf(y[2 * c + e]), fabsf(y[8 + 2 * c + e])));
+                }
             float up, down;
             fit_half(mma::quad_max(largest), up, down);
             sc = down * a.scale;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float y0 = y[2 * i] * up, y1 = y[2 * i + 1] * up;
+            for (int c = 0; c < 8; ++c) {
+                const float y0 = y[2 * c] * up, y1 = y[2 * c + 1] * up;
                 const __half2 hi = __floats2half2_rn(y0, y1);
-                qf[i >> 1][2 * (i & 1)] = *reinterpret_cast<const unsigned*>(&hi);
+                qf[c >> 1][2 * (c & 1)] = *reinterpret_cast<const unsigned*>(&hi);
                 const float2 f = __half22float2(hi);
-                qf[i >> 1][2 * (i & 1) + 1] = mma::pack_f16(y0 - f.x, y1 - f.y);
+                qf[c >> 1][2 * (c & 1) + 1] = mma::pack_f16(y0 - f.x, y1 - f.y);
             }
         }
         float s[4][2];
+        int stage = 0;
 #pragma unroll 1
         for (int j = 0; j < heads; ++j) {
+            asm volatile("cp.async.wait_group %0;\n" :: "n"(kStages - 1) : "memory");
+            __syncwarp();
+            const unsigned from = base_at + stage * kBytes + (lane & 7) * 128 + (((lane >> 3) ^ (lane & 7)) << 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
+                unsigned k[8];
+                mma::ldsm_x4(from + i * 1024, k[0], k[1], k[2], k[3]);
+                mma::ldsm_x4((from + i * 1024) ^ 64, k[4], k[5], k[6], k[7]);
                 float c[4];
-                mma::mma_f16_16816_z(c, qf[0], k[i][0], k[i][1]);
-                mma::mma_f16_16816(c, qf[1], k[i][2], k[i][3]);
-                mma::mma_f16_16816(c, qf[2], k[i][4], k[i][5]);
-                mma::mma_f16_16816(c, qf[3], k[i][6], k[i][7]);
-                if (j + 1 < heads) load_keys(a, at.k[i] + first + (j + 1) * step, t, k[i]);
+                mma::mma_f16_16816_z(c, qf[0], k[0], k[1]);
+                mma::mma_f16_16816(c, qf[1], k[2], k[3]);
+                mma::mma_f16_16816(c, qf[2], k[4], k[5]);
+                mma::mma_f16_16816(c, qf[3], k[6], k[7]);
                 if (j == 0 || mine == j) {
                     s[i][0] = c[0] + c[2];
                     s[i][1] = c[1] + c[3];
                 }
             }
+            __syncwarp();                              // all lanes have read what is written over
+            issue(j + kStages, stage);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
         }
         const unsigned pairs = __ballot_sync(kAll, row.pair);
         float weight[4][2], top = -INFINITY;
@@ -224,19 +223,17 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kern
         if (!kMany) clear();
 #pragma unroll 1
         for (int j = 0; j < heads; ++j) {
-            if (j + 1 < heads) asm volatile("cp.async.wait_group 1;\n" ::: "memory");
-            else asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+            asm volatile("cp.async.wait_group %0;\n" :: "n"(kStages - 1) : "memory");
             __syncwarp();
             unsigned pj[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) pj[i] = mine == j ? p[i >> 1][i & 1] : 0u;
-            const unsigned from = vs + (j & 1) * kBytes + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+            const unsigned from = base_at + stage * kBytes + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
             add_values(acc, pj, from);
             add_values(acc, pj + 4, from + 16 * 128);
-            if (j + 2 < heads) {
-                __syncwarp();                          // all lanes have read what is written over
-                load_values(a, at, first + (j + 2) * step, lane, vs + (j & 1) * kBytes);
-            }
+            __syncwarp();
+            issue(heads + j + kStages, stage);
+            stage = stage == kStages - 1 ? 0 : stage + 1;
         }
     }
     l = mma::quad_sum(l);
@@ -270,10 +267,10 @@ cudaError_t launch_attention_mma(const AttnArgs& args, cudaStream_t st) {
     AttnArgs a = args;
     // Key/value heads of a warp, as far as its eight query heads go: the rows are looked up
     // once for all, but few warps leave the GPU waiting.  Of 8, one token each, us: 256 tokens
-    // with 1, 2, 4 heads a warp 5.2, 4.7, 5.1; 512 tokens 8.5, 6.2, 6.7; 1024 tokens with 2, 4,
-    // 8 heads 13.7, 11.2, 13.9; 4096 tokens 48.4, 43.1, 42.7.
-    const int units = a.N * a.c.Hkv, most = std::min(8 / std::min(a.G, 8), a.c.Hkv);
-    a.run = a.r.total > 32 || units < 2048 ? 1 : std::min(most, std::max(2, units / 2048));
+    // with 1, 2, 4 heads a warp 5.4, 4.8, 5.0; 512 tokens 8.7, 6.4, 6.1; 1024 tokens with 2, 4,
+    // 8 heads 12.6, 10.7, 10.6; 4096 tokens 44.2, 40.1, 39.2.
+    const int most = std::min(8 / std::min(a.G, 8), a.c.Hkv);
+    a.run = a.r.total > 32 ? 1 : std::max(1, std::min(most, a.N * a.c.Hkv / 1024));
     const unsigned parts = (a.G + 7) / 8, runs = (a.c.Hkv + a.run - 1) / a.run;
     a.units = (unsigned)a.N * runs * parts;
     a.dRest = FastDiv::make(runs * parts);
