@@ -420,7 +420,9 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
  * integer, p - floor(d_k) - 1: its own key and value too, which have to be
  * appended before.  opts: scale, no_dedup and round_offsets are used; the other
  * fields have to be zero (rope_base is the cache's).  Products and sums are fp32;
- * q is rotated in fp32 and not rounded.  Limits of W, K and alpha as for
+ * q is rotated in fp32 and not rounded (bf16: q keeps 22 bits, the weights of the
+ * values 16).  A key or value that is not finite gives outputs that are not, of the
+ * heads that read it and of no others.  Limits of W, K and alpha as for
  * fibattn_fwd; 0 <= N, N * H < 2^31. */
 int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
                        void* out, float* lse, const int* positions, const int* seqs, int N, int H, int W,

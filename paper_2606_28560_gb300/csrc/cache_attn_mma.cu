@@ -221,19 +221,48 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kern
             p[i][1] = mma::pack_bf16(p0 - __uint_as_float(p[i][0] << 16), p1 - __uint_as_float(p[i][0] & 0xffff0000u));
         }
         if (!kMany) clear();
+        // the weights of this lane's query head, 0 for the rows of another key/value head
+        auto add = [&](float (&to)[8][4], int j, unsigned at) {
+            unsigned pj[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pj[i] = mine == j ? p[i >> 1][i & 1] : 0u;
+            const unsigned from = at + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
+            add_values(to, pj, from);
+            add_values(to, pj + 4, from + 16 * 128);
+            __syncwarp();                              // all lanes have read what is written over
+        };
 #pragma unroll 1
         for (int j = 0; j < heads; ++j) {
             asm volatile("cp.async.wait_group %0;\n" :: "n"(kStages - 1) : "memory");
             __syncwarp();
-            unsigned pj[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) pj[i] = mine == j ? p[i >> 1][i & 1] : 0u;
-            const unsigned from = base_at + stage * kBytes + (lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
-            add_values(acc, pj, from);
-            add_values(acc, pj + 4, from + 16 * 128);
-            __syncwarp();
+            add(acc, j, base_at + stage * kBytes);
             issue(heads + j + kStages, stage);
             stage = stage == kStages - 1 ? 0 : stage + 1;
+        }
+        if (!kMany && heads > 1) {
+            // 0 times a value that is not finite is NaN: if there is one, the heads' sums are
+            // taken again and kept apart, so that it stays with the heads that read it
+            float zero = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) zero = fmaf(acc[j][e], 0.f, zero);
+            if (__any_sync(kAll, !(zero == 0.f))) {
+#pragma unroll 1
+                for (int j = 0; j < heads; ++j) {
+                    issue(heads + j, 0);
+                    asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+                    __syncwarp();
+                    float one[8][4] = {};
+                    add(one, j, base_at);
+                    if (mine == j) {
+#pragma unroll
+                        for (int d = 0; d < 8; ++d)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[d][e] = one[d][e];
+                    }
+                }
+            }
         }
     }
     l = mma::quad_sum(l);

@@ -345,6 +345,29 @@ def test_values_that_are_not_finite():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("N,H,Hkv", [(3, 8, 8), (300, 8, 8), (1100, 8, 8), (1500, 8, 4), (1500, 6, 3), (700, 22, 2)])
+def test_values_that_are_not_finite_stay_with_their_heads(N, H, Hkv, dtype):
+    cache, g = filled([20], 32, Hkv, dtype, 5)
+    page = int(cache.block_table[0, 0])
+    q = tokens(g, N, H, dtype)
+    pos, seqs = torch.full((N,), 19, dtype=torch.int32, device="cuda"), torch.zeros(N, dtype=torch.int32, device="cuda")
+    before = fa.cached_fwd(q, cache, 1.0, [], 4, pos, seqs=seqs)
+    for pool, value in ((cache.v_pages, "nan"), (cache.v_pages, "inf"), (cache.k_pages, "nan"), (cache.k_pages, "inf")):
+        kept = pool[page, 17, 1].clone()
+        pool[page, 17, 1, 3] = float(value)
+        out, lse = fa.cached_fwd(q, cache, 1.0, [], 4, pos, seqs=seqs)
+        pool[page, 17, 1] = kept
+        others = [h for h in range(H) if h // (H // Hkv) != 1]
+        assert torch.equal(out[:, others], before[0][:, others]) and torch.equal(lse[:, others], before[1][:, others])
+        mine = out[:, H // Hkv:2 * H // Hkv]
+        if pool is cache.v_pages:
+            assert not torch.isfinite(mine[..., 3]).any() and torch.equal(lse, before[1])
+        elif value == "nan":
+            assert torch.isnan(mine).all()
+
+
+@pytest.mark.gpu
 def test_what_does_not_exist_is_not_read():
     lengths = [30, 30, 30, 30]
     cache, g = filled(lengths, 8, 2, BF, 8)
