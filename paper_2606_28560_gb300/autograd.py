@@ -134,6 +134,22 @@ class FibAttention(torch.nn.Module):
                                           self.dedup, None if alpha is None else float(alpha))
 
 
+    @torch.no_grad()
+    def cached(self, q, cache, positions, *, seqs=None, parents=None, slots=None, alpha=None, out=None, lse=None):
+        """Generating with the layer: its attention for new tokens over a ``PagedCache``
+        (``cached_fwd``), or for trees of drafts (``tree_fwd``, when ``parents`` and
+        ``slots`` are given).  q [tokens, H, 64]; the tokens' own keys and values have
+        to be in the cache.  Returns (out, lse); no gradients."""
+        if cache.rope_base != self.rope_base:
+            raise ValueError(f"the cache turns its keys by rope_base {cache.rope_base}, the layer by {self.rope_base}")
+        alpha = self.alpha if alpha is None else float(alpha)
+        if parents is None and slots is None:
+            return B.cached_fwd(q, cache, alpha, self.offsets, self.W, positions, seqs=seqs, scale=self.scale,
+                                dedup=self.dedup, out=out, lse=lse)
+        return B.tree_fwd(q, cache, alpha, self.offsets, self.W, positions, parents, slots, seqs=seqs, scale=self.scale,
+                          dedup=self.dedup, out=out, lse=lse)
+
+
 def theta_of_alpha(alpha: float) -> float:
     """Inverse of alpha_of_theta on [0.5, 1.5] (fibattn_theta_of_alpha); the
     ends map to -/+ infinity, clamped to -/+ 30."""

@@ -308,6 +308,22 @@ def test_cached_default_sequences_and_scale(N, H, Hkv):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,Hkv", [(8, 8), (8, 2), (6, 3), (20, 2)])
+def test_a_token_by_itself_and_in_a_batch(H, Hkv, dtype):
+    """The same bits, whatever batch a token is in."""
+    cache, g = filled([300, 77, 12], 16, Hkv, dtype, 2)
+    N = 2500
+    seqs = torch.randint(0, 3, (N,), generator=g).int().cuda()
+    positions = (torch.rand(N, generator=g).cuda() * torch.tensor([300, 77, 12]).cuda()[seqs.long()]).int()
+    q = tokens(g, N, H, dtype)
+    out, lse = fa.cached_fwd(q, cache, 0.8, FIB, 8, positions, seqs=seqs)
+    for some in (slice(7, 8), slice(100, 400)):
+        few = fa.cached_fwd(q[some], cache, 0.8, FIB, 8, positions[some].clone(), seqs=seqs[some].clone())
+        assert torch.equal(few[0], out[some]) and torch.equal(few[1], lse[some])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_extreme_scores(dtype):
     """Scores of thousands, apart by more than any exponent, and equal ones."""
     cache, g = filled([50, 50], 16, 1, dtype, 3)

@@ -1,0 +1,65 @@
+"""The example model generating: its layers over the library's paged cache."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_2606_28560_gb300 as fa
+from tests.test_training_example import load
+
+
+@pytest.mark.gpu
+def test_steps_are_the_model():
+    """Prompts in two pieces and single tokens, in fp32: the states of the whole
+    sequence.  A layer's attention is within 1e-4 of the definition both ways; norms and
+    products of 128 random weights of one layer keep that below 1e-3 of the state."""
+    m = load()
+    torch.manual_seed(1)
+    model = m.Model(2, 128).cuda()
+    tokens = torch.randint(0, 256, (3, 50)).cuda()
+    with torch.no_grad():
+        want = model.states(tokens)
+        caches, at, got = model.caches(50, 3, torch.float32), 0, []
+        for n in (20, 1, 1, 27, 1):
+            positions = torch.arange(at, at + n, device="cuda", dtype=torch.int32).repeat(3)
+            seqs = torch.arange(3, device="cuda", dtype=torch.int32).repeat_interleave(n)
+            got.append(model.steps(tokens[:, at:at + n].reshape(-1), caches, positions, seqs, model.alphas()).view(3, n, -1))
+            at += n
+    got = torch.cat(got, 1)
+    assert float((got - want).norm() / want.norm()) <= 1e-3
+    assert fa.check_status() == 0
+
+
+@pytest.mark.gpu
+def test_generates():
+    m = load()
+    torch.manual_seed(1)
+    model = m.Model(2, 128).cuda()
+    prompts = torch.randint(0, 256, (2, 33)).cuda()
+    text = model.generate(prompts, 40)
+    assert text.shape == (2, 40) and int(text.min()) >= 0 and int(text.max()) < 256
+    assert torch.equal(model.generate(prompts[1:], 7)[0], model.generate(prompts[1:], 40)[0, :7])
+    assert fa.check_status() == 0
+
+
+@pytest.mark.gpu
+def test_layer_over_a_cache():
+    """The module's call, for tokens and for a tree, is the library's; another rotation is refused."""
+    layer = fa.FibAttention(W=5, theta=0.3, scale=0.2, dedup=False).cuda()
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4)
+    cache = fa.PagedCache.empty(4, 8, 2, table, dtype=torch.float32)
+    positions = torch.arange(30, dtype=torch.int32, device="cuda")
+    seqs = torch.zeros(30, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(30, h, 64, device="cuda") for h in (4, 2, 2))
+    fa.cache_append(cache, k, v, positions, seqs=seqs)
+    q.requires_grad_()
+    out, lse = layer.cached(q, cache, positions, seqs=seqs)
+    whole = layer(*(t.detach().transpose(0, 1)[None].contiguous() for t in (q, k, v)))
+    assert not out.requires_grad and (out - whole[0].transpose(0, 1)).abs().max() <= 2e-4
+    parents = positions - 1
+    tree = layer.cached(q, cache, positions, seqs=seqs, parents=parents, slots=positions, alpha=layer.alpha)
+    assert torch.equal(tree[0], out) and torch.equal(tree[1], lse)
+    with pytest.raises(ValueError, match="parents and slots"):
+        layer.cached(q, cache, positions, seqs=seqs, parents=parents)
+    with pytest.raises(ValueError, match="rope_base"):
+        layer.cached(q, fa.PagedCache.empty(4, 8, 2, table, dtype=torch.float32, rope_base=5e5), positions, seqs=seqs)
