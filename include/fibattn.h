@@ -433,9 +433,9 @@ int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_
  * sequence itself; its position is one more than its parent's.  The ancestor at
  * distance j, j steps up (0: the token itself), is read from storage slot
  * slots[ancestor], where fibattn_cache_append put it; what lies further back than
- * the root from the slot of its position.  A parent that is not before its child
- * counts as one that does not exist (above).  That it belongs to the child's
- * sequence is not checked: its slot would be looked up in the child's pages. */
+ * the root from the slot of its position.  A parent that is not before its child, and
+ * an ancestor that is read but is of another sequence or at another position, count
+ * as ones that do not exist (above). */
 int fibattn_tree_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
                      void* out, float* lse, const int* positions, const int* parents, const int* slots,
                      const int* seqs, int N, int H, int W,

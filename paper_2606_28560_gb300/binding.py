@@ -765,8 +765,7 @@ def tree_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, par
     its ancestors in place of the positions they stand at, and the cached sequence
     behind the root.  parents [N] int32: the row of this batch, before n, that token
     n continues, or -1; slots [N] int32: where ``cache_append`` put each token.  The
-    rest as for ``cached_fwd``.  A parent is of its child's sequence, its position one
-    less (not checked: another's slot would be looked up in the child's pages).
+    rest as for ``cached_fwd``.  A parent is of its child's sequence, its position one less.
     Accepted tokens are appended again, at their
     positions."""
     if stream is not None:

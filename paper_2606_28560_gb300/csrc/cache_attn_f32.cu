@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_f32_kernel(const __g
         if (!alive) continue;
         int slot;
         unsigned at = 0;
-        bool found = slot_of<kTree>(a, n, pos, row.distance, live, slot);
+        bool found = slot_of<kTree>(a, n, pos, seq, row.distance, live, slot);
         if (found && live) found = locate(a.c, pages, slot, at);
         bad = __any_sync(kAll, !found);
         if (bad) break;

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kern
         const bool lives = live >> lane & 1u;
         int slot;
         unsigned place = 0;
-        bool found = slot_of<kTree>(a, n, pos, row.distance, lives, slot);
+        bool found = slot_of<kTree>(a, n, pos, seq, row.distance, lives, slot);
         if (found && lives) found = locate(a.c, pages, slot, place);
         bad = __any_sync(kAll, !found);
         if (bad) break;

@@ -34,9 +34,10 @@ __device__ __forceinline__ RowOf row_of(const Rows& r, int i) {
 // the ancestor `distance` steps up, where the tree reaches that far.  All lanes walk
 // together; the parents come 32 at a time, one to a lane, so that a step is an
 // exchange between lanes and no load.  Returns false if a parent is not before its
-// child; a parent is less than its child, so the walk ends.
+// child, or an ancestor that is read is of another sequence or stands elsewhere; a
+// parent is less than its child, so the walk ends.
 template <bool kTree>
-__device__ __forceinline__ bool slot_of(const AttnArgs& a, int n, int pos, int distance, bool live, int& slot) {
+__device__ __forceinline__ bool slot_of(const AttnArgs& a, int n, int pos, int seq, int distance, bool live, int& slot) {
     slot = pos - distance;
     if (!kTree) return true;
     const int furthest = __reduce_max_sync(kAll, live ? distance : -1), lane = threadIdx.x & 31;
@@ -53,8 +54,10 @@ __device__ __forceinline__ bool slot_of(const AttnArgs& a, int n, int pos, int d
         if (up < 0) break;
         cur = up;
     }
-    if (live && mine >= 0) slot = a.slots[mine];
-    return true;
+    if (!live || mine < 0) return true;
+    const int at = a.positions[mine], of = a.seqs ? a.seqs[mine] : mine;
+    slot = a.slots[mine];
+    return at == pos - distance && of == seq;
 }
 
 }  // namespace cache

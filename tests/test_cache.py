@@ -517,6 +517,31 @@ def test_parents_that_do_not_exist():
     assert torch.isnan(out[5]).all() and torch.isfinite(out[0]).all()
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_parents_elsewhere(dtype):
+    """A parent of another sequence, at another position, or that is padding."""
+    cache, g = filled([20, 20], 8, 1, dtype, 4, more=8)
+    seqs = torch.tensor([0, 1, 0, 0, 0, -1, 0, 0]).int()
+    positions = torch.tensor([20, 20, 21, 21, 22, 21, 22, 22]).int()
+    parents = torch.tensor([-1, -1, 1, 0, 0, 0, 5, 3]).int()     # 2: of sequence 1; 4: skips one; 6: of padding
+    slots = torch.tensor([20, 20, 21, 22, 23, 24, 25, 26]).int()
+    q, k, v = tokens(g, 8, 2, dtype), tokens(g, 8, 1, dtype), tokens(g, 8, 1, dtype)
+    fa.cache_append(cache, k, v, positions.cuda(), seqs=seqs.cuda(), slots=slots.cuda())
+    clear()
+    args = [t.cuda() for t in (positions, parents, slots)]
+    out, lse = fa.tree_fwd(q, cache, 0.8, FIB, 8, *args, seqs=seqs.cuda())
+    with pytest.raises(fa.FibattnError) as e:
+        fa.check_status()
+    assert e.value.flags == 8
+    bad = torch.tensor([False, False, True, False, True, False, True, False])
+    assert torch.equal(torch.isnan(out).all(2).all(1).cpu(), bad) and torch.equal(torch.isnan(lse).all(1).cpu(), bad)
+    assert not out[5].any()
+    # an ancestor that is not read does not matter: the token alone
+    out, lse = fa.tree_fwd(q, cache, 1.0, [], 0, *args, seqs=seqs.cuda())
+    assert torch.isfinite(out).all() and fa.check_status() == 0
+
+
 # ------------------------------------------------------------ run together ----
 
 @pytest.mark.gpu
