@@ -6,9 +6,10 @@
 // of one token, or of several), four lanes to a row, so that a rotation's pair stays
 // in its lane.  What is read does not wait for where it goes: the loads are under way
 // while the warp looks up pages and evaluates its tokens' 32 angles, one to a lane,
-// once for all heads.  Of 64 prompts of 1024 tokens (8 heads, bf16, 268 MB) 42.0 us,
-// 6.4 TB/s; two steps of a warp at once take 44.6, blocks of eight warps 42.9 but the
-// 256 tokens of a decoding batch 3.0 us instead of 2.6.
+// once for all heads.  64 prompts of 1024 tokens (8 heads, bf16, 269 MB) take 42.0 us,
+// 6.4 TB/s; a token's thread with all its heads took 46.8, two and four steps of a warp
+// at once 2 and 18 % longer, blocks of eight warps 2 % less there but a batch of 256
+// single tokens 3.0 us instead of 2.5.
 #include "cache.cuh"
 
 namespace fibattn {
