@@ -620,7 +620,8 @@ class PagedCache:
     k_pages, v_pages [pages, rows of a page, Hkv, 64]: pools on one device, of the
     same shape and strides; the rotated keys in fp16 and the values in bf16, or
     both in fp32.  Any strides that are multiples of 64, the last dimension
-    contiguous (a layer of a larger pool, a transposed pool with the heads first).
+    contiguous (a layer of a larger pool, a transposed pool with the heads first);
+    they start on 32 bytes.
     block_table [seqs, pages of a sequence] int32: where the pages of each sequence
     lie; entries may change between calls, unused ones are -1 or anything else.
 
@@ -782,8 +783,8 @@ def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, sca
     p = _ints(positions, each, index, "positions")
     b = None if seqs is None else _ints(seqs, each, index, "seqs")
     _check_device(index)
-    f, K, alive = _offset_table(offsets)
-    o, kept = _opt_struct(scale, dedup, round_offsets)
+    f, K, alive = _offset_table(offsets)              # noqa: F841 (alive, kept: until the call is over)
+    o, kept = _opt_struct(scale, dedup, round_offsets)   # noqa: F841
     if out is None:
         out = torch.empty(shape, dtype=cache.dtype, device=cache.device)
     elif out.dtype is not cache.dtype or out.shape != shape or out.get_device() != index or not out.is_contiguous():

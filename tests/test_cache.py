@@ -20,6 +20,7 @@ import ctypes
 import math
 import os
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -615,6 +616,30 @@ def test_captured_and_replayed():
             assert all(torch.equal(a, b) for a, b in zip(want, step()))
             assert torch.equal(want[0], want[2]) and torch.isfinite(want[0]).all()
     assert fa.check_status() == 0
+
+
+FIRST = """
+import torch, paper_2606_28560_gb300 as fa
+table = torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4)
+pos = torch.arange(30, dtype=torch.int32, device="cuda")
+seqs, f = torch.zeros_like(pos), [1.0, 2.0, 3.0, 5.0, 8.0]
+for dtype in (torch.bfloat16, torch.float32):
+    cache = fa.PagedCache.empty(4, 8, 2, table, dtype=dtype)
+    q, k = (torch.randn(30, h, 64, device="cuda").to(dtype) for h in (4, 2))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fa.cache_append(cache, k, k, pos, seqs=seqs)
+        got = (*fa.cached_fwd(q, cache, 0.8, f, 4, pos, seqs=seqs), *fa.tree_fwd(q, cache, 0.8, f, 4, pos, pos - 1, pos, seqs=seqs))
+    graph.replay()
+    want = fa.cached_fwd(q, cache, 0.8, f, 4, pos, seqs=seqs)
+    assert all(torch.equal(a, b) for a, b in zip(got, (*want, *want))) and fa.check_status() == 0
+"""
+
+
+@pytest.mark.gpu
+def test_captured_as_the_first_calls_of_a_program():
+    subprocess.run([sys.executable, "-c", FIRST], cwd=ROOT, check=True, timeout=300)
 
 
 @pytest.mark.gpu
