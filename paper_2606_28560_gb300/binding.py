@@ -729,8 +729,9 @@ def cache_append(cache: PagedCache, k, v, positions, *, seqs=None, slots=None, s
     the way (fibattn_cache_append).  k, v [N, Hkv, 64]: views of a fused projection
     will do.  positions [N] int32: where each token stands; seqs [N] int32: whose
     it is (default: token n is sequence n's); slots [N] int32: where it is stored
-    (default: at its position; drafted tokens lie elsewhere).  A negative position or
-    sequence is padding.  Nothing is returned."""
+    (default: at its position; drafted tokens lie elsewhere); two tokens of one call at
+    one slot leave a mixture there.  A negative position or sequence is padding.
+    Nothing is returned."""
     if stream is not None:
         return _on_stream(stream, cache_append, cache, k, v, positions, seqs=seqs, slots=slots)
     index, shape = cache.index, k.shape
@@ -753,7 +754,8 @@ def cached_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, *
     and rungs, read from the pages.  q [N, H, 64] (views of a fused projection will
     do), positions and seqs as for ``cache_append``; the tokens' own keys and values
     have to be in the cache.  One token per sequence, chunks of a prompt, or any mix.
-    Returns (out [N, H, 64], lse [N, H] fp32); padding has out 0 and lse -infinity."""
+    Returns (out [N, H, 64], lse [N, H] fp32), without gradients; padding has out 0 and
+    lse -infinity.  A token has the same bits in whatever batch it is."""
     if stream is not None:
         return _on_stream(stream, cached_fwd, q, cache, alpha, offsets, W, positions, seqs=seqs, scale=scale, dedup=dedup,
                           round_offsets=round_offsets, out=out, lse=lse)
@@ -765,10 +767,9 @@ def tree_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, par
     """Attention of drafted tokens that form trees (fibattn_tree_fwd): a token sees
     its ancestors in place of the positions they stand at, and the cached sequence
     behind the root.  parents [N] int32: the row of this batch, before n, that token
-    n continues, or -1; slots [N] int32: where ``cache_append`` put each token.  The
-    rest as for ``cached_fwd``.  A parent is of its child's sequence, its position one less.
-    Accepted tokens are appended again, at their
-    positions."""
+    n continues, or -1 (a parent is of its child's sequence, its position one less);
+    slots [N] int32: where ``cache_append`` put each token.  The rest as for
+    ``cached_fwd``.  Accepted tokens are appended again, at their positions."""
     if stream is not None:
         return _on_stream(stream, tree_fwd, q, cache, alpha, offsets, W, positions, parents, slots, seqs=seqs, scale=scale,
                           dedup=dedup, round_offsets=round_offsets, out=out, lse=lse)
