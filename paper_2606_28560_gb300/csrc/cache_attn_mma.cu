@@ -21,7 +21,8 @@
 // warps that an SM holds where rows come from L2 (8 chunks of 256 tokens 12.6 us) or where
 // there are few (one token 3.1 us).  Keys straight into registers and values through
 // a ring of two took 43.0, 12.1 and 3.1 us, and 164 instead of 140 us for 128 chunks; two
-// stages and five blocks an SM 38.7, 12.9 and 3.2 at the best heads a warp for each.
+// stages and 20 warps an SM 38.7, 12.9 and 3.2 at the best heads a warp for each; blocks
+// of four warps 1 to 2 % more for single tokens.
 #include <algorithm>
 
 #include "cache_rows.cuh"
@@ -32,7 +33,7 @@ namespace cache {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 2;
 
 // 2^k for scaling q to fp16's upper range, from the exponent of its largest value,
 // and 2^-k: halves of fp16 then keep 22 bits of every q, whatever its size.
@@ -72,7 +73,7 @@ __device__ __forceinline__ void add_values(float (&acc)[8][4], const unsigned* p
 
 // kMany: queries read more than 32 rows.
 template <bool kMany, bool kTree>
-__global__ void __launch_bounds__(32 * kWarps, kMany ? 3 : 4) attention_mma_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(32 * kWarps, kMany ? 6 : 8) attention_mma_kernel(const __grid_constant__ AttnArgs a) {
     __shared__ __align__(128) unsigned char ring[kWarps][kStages][kBytes];
     grid_dependency_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
