@@ -259,6 +259,8 @@ SETS = {  # W, alpha, offsets, options
     "usual": (8, 0.8, FIB, {}), "window alone": (4, 1.0, [], {}), "one key": (0, 1.0, [], {}),
     "integers": (8, 1.0, FIB, {}), "every rung": (5, 1.3, POW, {"dedup": False}), "rounded": (2, 0.77, FIB, {"round_offsets": True}),
     "rungs alone": (0, 1.499, [k + 0.4 for k in range(1, 33)], {}), "wide window": (300, 0.9, FIB, {}),
+    "40 rows": (20, 0.8, FIB, {}), "64 rows": (31, 1.1, [32.0 + 3 * k for k in range(16)], {}),
+    "65 rows": (32, 1.1, [32.0 + 3 * k for k in range(16)], {}), "dead halves": (0, 1.3, [200.1 + k for k in range(30)], {}),
     "near rungs": (3, 0.6, [0.0, 0.3, 1.0, 1.5, 2.25, 4.0], {"dedup": False}),
 }
 
@@ -309,18 +311,22 @@ def test_cached_default_sequences_and_scale(N, H, Hkv):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("W", [8, 25, 90])
 @pytest.mark.parametrize("H,Hkv", [(8, 8), (8, 2), (6, 3), (20, 2)])
-def test_a_token_by_itself_and_in_a_batch(H, Hkv, dtype):
+def test_a_token_by_itself_and_in_a_batch(H, Hkv, W, dtype):
     """The same bits, whatever batch a token is in."""
     cache, g = filled([300, 77, 12], 16, Hkv, dtype, 2)
     N = 2500
     seqs = torch.randint(0, 3, (N,), generator=g).int().cuda()
     positions = (torch.rand(N, generator=g).cuda() * torch.tensor([300, 77, 12]).cuda()[seqs.long()]).int()
     q = tokens(g, N, H, dtype)
-    out, lse = fa.cached_fwd(q, cache, 0.8, FIB, 8, positions, seqs=seqs)
+    out, lse = fa.cached_fwd(q, cache, 0.8, FIB, W, positions, seqs=seqs)
     for some in (slice(7, 8), slice(100, 400)):
-        few = fa.cached_fwd(q[some], cache, 0.8, FIB, 8, positions[some].clone(), seqs=seqs[some].clone())
+        few = fa.cached_fwd(q[some], cache, 0.8, FIB, W, positions[some].clone(), seqs=seqs[some].clone())
         assert torch.equal(few[0], out[some]) and torch.equal(few[1], lse[some])
+    at = torch.randperm(N, generator=g)[:20]
+    want = Model(cache).attention(q[at.cuda()], positions.cpu()[at], seqs.cpu()[at], slots_of(W, 0.8, FIB))
+    check((out[at.cuda()], lse[at.cuda()]), want, W, len(FIB))
 
 
 @pytest.mark.gpu
@@ -363,17 +369,18 @@ def test_values_that_are_not_finite():
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("W", [4, 40])
 @pytest.mark.parametrize("N,H,Hkv", [(3, 8, 8), (300, 8, 8), (1100, 8, 8), (1500, 8, 4), (1500, 6, 3), (700, 22, 2)])
-def test_values_that_are_not_finite_stay_with_their_heads(N, H, Hkv, dtype):
-    cache, g = filled([20], 32, Hkv, dtype, 5)
+def test_values_that_are_not_finite_stay_with_their_heads(N, H, Hkv, W, dtype):
+    cache, g = filled([60], 64, Hkv, dtype, 5)
     page = int(cache.block_table[0, 0])
     q = tokens(g, N, H, dtype)
-    pos, seqs = torch.full((N,), 19, dtype=torch.int32, device="cuda"), torch.zeros(N, dtype=torch.int32, device="cuda")
-    before = fa.cached_fwd(q, cache, 1.0, [], 4, pos, seqs=seqs)
+    pos, seqs = torch.full((N,), 19 if W == 4 else 56, dtype=torch.int32, device="cuda"), torch.zeros(N, dtype=torch.int32, device="cuda")
+    before = fa.cached_fwd(q, cache, 1.0, [], W, pos, seqs=seqs)
     for pool, value in ((cache.v_pages, "nan"), (cache.v_pages, "inf"), (cache.k_pages, "nan"), (cache.k_pages, "inf")):
         kept = pool[page, 17, 1].clone()
         pool[page, 17, 1, 3] = float(value)
-        out, lse = fa.cached_fwd(q, cache, 1.0, [], 4, pos, seqs=seqs)
+        out, lse = fa.cached_fwd(q, cache, 1.0, [], W, pos, seqs=seqs)
         pool[page, 17, 1] = kept
         others = [h for h in range(H) if h // (H // Hkv) != 1]
         assert torch.equal(out[:, others], before[0][:, others]) and torch.equal(lse[:, others], before[1][:, others])
@@ -438,7 +445,7 @@ def drafted(g, lengths, sizes, chain=0.9, wide=6):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("which", ["usual", "one key", "every rung", "rungs alone", "wide window", "near rungs"])
+@pytest.mark.parametrize("which", ["usual", "one key", "every rung", "rungs alone", "wide window", "40 rows", "near rungs"])
 @pytest.mark.parametrize("H,Hkv,rows,wide", [(1, 1, 1, 3), (8, 2, 16, 6), (6, 3, 13, 1), (3, 3, 100, 70)])
 def test_tree(H, Hkv, rows, wide, which, dtype):
     """Trees of 1 to 150 drafts behind 0 to 700 tokens: bushy ones and chains (wide = 1)."""
