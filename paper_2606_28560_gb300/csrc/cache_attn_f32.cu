@@ -4,13 +4,13 @@
 // its score is (1-w) s_floor + w s_far and its rows have weights p (1-w) and p w.
 //
 // A warp has one token and key/value head, its group of query heads or a part of it.
-// 32 rows at a time: each lane finds one row through the page table; then all lanes
-// load keys, eight lanes to a row (32 bytes of it each), while the values are copied to
-// shared memory.  Eight partial dot products per lane are exchanged so that a lane ends
-// with the score of the row it looked up, and the softmax is one value per lane.  The
-// weights of all heads are kept, then each value is read from shared memory once.
-// Bound by memory where there are many sequences: 2048 single tokens of 8 heads 40.7 us,
-// 5.5 TB/s; by the chain of look-ups and loads where there are few: one token 3.6 us.
+// Rows go 32 to a part: each lane finds one of a part through the page table; then all
+// lanes load keys, eight lanes to a row (32 bytes of it each), while the values are
+// copied to shared memory.  Eight partial dot products per lane are exchanged so that a
+// lane ends with the score of the row it looked up, and the softmax is one value per
+// lane and part.  The weights of all heads are kept, then the values are read.
+// Bound by memory where there are many sequences: 2048 single tokens of 8 heads 38.1 us,
+// 5.9 TB/s; by the chain of look-ups and loads where there are few: one token 3.3 us.
 #include <algorithm>
 
 #include "cache_rows.cuh"
@@ -21,8 +21,8 @@ namespace cache {
 
 namespace {
 
-constexpr int kWarps = 4;
 constexpr int kHeads = 8;                            // query heads of a warp, at most
+constexpr int warps_of(int parts) { return parts == 1 ? 4 : 2; }   // of a block: 45 and 41 KB of shared memory
 
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -75,26 +75,28 @@ __device__ __forceinline__ void write_out(float* out, const float (&acc)[8], flo
     *reinterpret_cast<float2*>(out + (up2 ? kHalf : 0) + 4 * (lane & 7) + (up1 ? 2 : 0)) = make_float2(x[0] * by, x[1] * by);
 }
 
+template <int kParts>
 struct Shared {
-    float values[32][kHeadDim];                      // in the order of the lanes that found the rows
-    float p[kHeads][32];                             // weights, in the same order
-    float q[kHeadDim];                               // a rotated query
+    float values[kParts][32][kHeadDim];              // in the order of the lanes that found the rows
+    float p[kParts][kHeads][32];                     // scores, then weights, in the same order
+    float q[kHeads][kHeadDim];                       // rotated queries
 };
 
-// kMany: queries read more than 32 rows; a warp then has one query head.
-template <bool kMany, bool kTree>
-__global__ void __launch_bounds__(32 * kWarps, 4) attention_f32_kernel(const __grid_constant__ AttnArgs a) {
-    __shared__ __align__(16) Shared shared[kWarps];
+// kParts: of 32 rows each, taken together; kMany: queries read more than these (a warp then
+// has one query head).
+template <int kParts, bool kMany, bool kTree>
+__global__ void __launch_bounds__(32 * warps_of(kParts), kParts == 1 ? 4 : 5) attention_f32_kernel(const __grid_constant__ AttnArgs a) {
+    __shared__ __align__(16) Shared<kParts> shared[warps_of(kParts)];
     grid_dependency_sync();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c = lane & 7, group = lane >> 3;
-    const unsigned unit = blockIdx.x * kWarps + warp;
+    const unsigned unit = blockIdx.x * warps_of(kParts) + warp;
     if (unit >= a.units) return;
-    Shared& sh = shared[warp];
+    Shared<kParts>& sh = shared[warp];
     const unsigned n = fdiv(unit, a.dRest), rest = unit - n * a.dRest.d, h = fdiv(rest, a.dParts);
-    const int part = rest - h * a.dParts.d, g0 = h * a.G + part * a.run, heads = min(a.run, a.G - part * a.run);
+    const int part = rest - h * a.dParts.d, g0 = h * a.G + part * a.run, heads = kMany ? 1 : min(a.run, a.G - part * a.run);
     const int pos = a.positions[n], seq = a.seqs ? a.seqs[n] : (int)n;
     const float* q = static_cast<const float*>(a.q) + n * a.q_token + g0 * a.q_head;
-    float qx = q[lane], qy = q[lane + kHalf];
+    const float qx = q[lane], qy = q[lane + kHalf];
     float* out = static_cast<float*>(a.out) + ((size_t)n * a.H + g0) * kHeadDim;
     float* lse = a.lse + (size_t)n * a.H + g0;
     const int* pages = a.c.table + (size_t)max(seq, 0) * a.c.pages_per_seq;
@@ -103,103 +105,147 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_f32_kernel(const __g
     float m = -INFINITY, l = 0.f, acc[8];            // (kMany: over the rows so far)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    float cs = 0.f, sn = 0.f;
-    if (!padding) rope_cs_f32(a.c.rope, lane, pos, cs, sn);
-    for (int r0 = 0; r0 < (kMany ? a.r.total : 1) && !padding && !bad; r0 += 32) {
-        // lane (group, c) has row 4c + group: the scores are exchanged to that order
-        const int i = r0 + 4 * c + group;
-        const RowOf row = row_of(a.r, i);
-        const bool live = i < a.r.total && pos >= row.need;
-        const unsigned alive = __ballot_sync(kAll, live);
-        if (!alive) continue;
-        int slot;
-        unsigned at = 0;
-        bool found = slot_of<kTree>(a, n, pos, seq, row.distance, live, slot);
-        if (found && live) found = locate(a.c, pages, slot, at);
-        bad = __any_sync(kAll, !found);
+    for (int r0 = 0; r0 < (kMany ? a.r.total : 1) && !padding && !bad; r0 += 32 * kParts) {
+        // where the rows lie; one that is not read stands for one that is: its score counts for nothing
+        float share[kParts];
+        bool live[kParts], pair[kParts], any = false;
+        unsigned at[kParts], some = 0;
+#pragma unroll
+        for (int b = 0; b < kParts; ++b) {
+            // lane (group, c) has row 4c + group: the scores are exchanged to that order
+            const int i = r0 + 32 * b + 4 * c + group;
+            const RowOf row = row_of(a.r, i);
+            live[b] = i < a.r.total && pos >= row.need;
+            pair[b] = row.pair;
+            share[b] = row.weight;
+            at[b] = 0;
+            const unsigned alive = __ballot_sync(kAll, live[b]);
+            if (!alive) continue;
+            int slot;
+            bool found = slot_of<kTree>(a, n, pos, seq, row.distance, live[b], slot);
+            if (found && live[b]) found = locate(a.c, pages, slot, at[b]);
+            bad |= __any_sync(kAll, !found);
+            some = __shfl_sync(kAll, at[b], __ffs(alive) - 1);
+            any = true;
+        }
         if (bad) break;
-        // a row that is not read stands for one that is: its score counts for nothing
-        const unsigned some = __shfl_sync(kAll, at, __ffs(alive) - 1);
-        at = (live ? at : some) + h * a.c.head_stride;
+        if (!any) continue;
+        if (kMany) __syncwarp();                     // what is written over has been read
+        // the second part has 16 rows or fewer: the first four of every eight in the lanes' order
+        const bool few = kParts > 1 && a.r.total <= 48;
         float k[8][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            load_keys(static_cast<const float*>(a.c.k) + (size_t)__shfl_sync(kAll, at, 8 * group + j) * kHeadDim + 8 * c, k[j]);
-        if (kMany) __syncwarp();                     // the values of the rows before have been read
+        for (int b = 0; b < kParts; ++b) {
+            at[b] = (live[b] ? at[b] : some) + h * a.c.head_stride;
+            if (b == 0)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int r = 2 * j + (lane >> 4);
-            const float* from = static_cast<const float*>(a.c.v) + (size_t)__shfl_sync(kAll, at, r) * kHeadDim + 4 * (lane & 15);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n"
-                         :: "r"(mma::smem_u32(&sh.values[r][4 * (lane & 15)])), "l"(from) : "memory");
+                for (int j = 0; j < 8; ++j)
+                    load_keys(static_cast<const float*>(a.c.k) + (size_t)__shfl_sync(kAll, at[0], 8 * group + j) * kHeadDim + 8 * c, k[j]);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                if (b > 0 && j % 4 >= 2 && few) continue;
+                const int r = 2 * j + (lane >> 4);
+                const float* from = static_cast<const float*>(a.c.v) + (size_t)__shfl_sync(kAll, at[b], r) * kHeadDim + 4 * (lane & 15);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n"
+                             :: "r"(mma::smem_u32(&sh.values[b][r][4 * (lane & 15)])), "l"(from) : "memory");
+            }
         }
         asm volatile("cp.async.commit_group;\n" ::: "memory");
-        for (int g = 0; g < (kMany ? 1 : heads); ++g) {
-            if (!kMany || !turned) {
-                turned = true;
-                __syncwarp();
-                sh.q[lane] = (qx * cs - qy * sn) * a.scale;
-                sh.q[lane + kHalf] = (qy * cs + qx * sn) * a.scale;
-                __syncwarp();
-                if (g + 1 < heads) {
-                    qx = q[(g + 1) * a.q_head + lane];
-                    qy = q[(g + 1) * a.q_head + lane + kHalf];
-                }
-            }
-            const float4 qa = *reinterpret_cast<const float4*>(&sh.q[8 * c]), qb = *reinterpret_cast<const float4*>(&sh.q[8 * c + 4]);
-            float s[8];
+        if (!turned) {
+            turned = true;
+            float cs, sn;
+            rope_cs_f32(a.c.rope, lane, pos, cs, sn);
+            // (roundings as written, so that a head has the same bits wherever in a warp it is)
+            auto turn = [&](float* to, float x, float y) {
+                to[lane] = __fmul_rn(__fmaf_rn(x, cs, -__fmul_rn(y, sn)), a.scale);
+                to[lane + kHalf] = __fmul_rn(__fmaf_rn(y, cs, __fmul_rn(x, sn)), a.scale);
+            };
+            turn(sh.q[0], qx, qy);
+#pragma unroll 4
+            for (int g = 1; g < heads; ++g) turn(sh.q[g], q[g * a.q_head + lane], q[g * a.q_head + lane + kHalf]);
+            __syncwarp();
+        }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                float2 t = __fmul2_rn(make_float2(k[j][0], k[j][1]), make_float2(qa.x, qa.y));
-                t = __ffma2_rn(make_float2(k[j][2], k[j][3]), make_float2(qa.z, qa.w), t);
-                t = __ffma2_rn(make_float2(k[j][4], k[j][5]), make_float2(qb.x, qb.y), t);
-                t = __ffma2_rn(make_float2(k[j][6], k[j][7]), make_float2(qb.z, qb.w), t);
-                s[j] = t.x + t.y;
+        for (int b = 0; b < kParts; ++b) {
+            if (b > 0)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j < 4 || !few)
+                        load_keys(static_cast<const float*>(a.c.k) + (size_t)__shfl_sync(kAll, at[b], 8 * group + j) * kHeadDim + 8 * c, k[j]);
+            for (int g = 0; g < heads; ++g) {
+                const float4 qa = *reinterpret_cast<const float4*>(&sh.q[g][8 * c]);
+                const float4 qb = *reinterpret_cast<const float4*>(&sh.q[g][8 * c + 4]);
+                float s[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float2 t = __fmul2_rn(make_float2(k[j][0], k[j][1]), make_float2(qa.x, qa.y));
+                    t = __ffma2_rn(make_float2(k[j][2], k[j][3]), make_float2(qa.z, qa.w), t);
+                    t = __ffma2_rn(make_float2(k[j][4], k[j][5]), make_float2(qb.x, qb.y), t);
+                    t = __ffma2_rn(make_float2(k[j][6], k[j][7]), make_float2(qb.z, qb.w), t);
+                    s[j] = t.x + t.y;
+                }
+                float score = sum_own(s, c) * share[b];
+                const float other = __shfl_xor_sync(kAll, score, 8);
+                if (pair[b]) score += other;
+                sh.p[b][g][lane] = live[b] ? score : -INFINITY;
             }
-            float score = sum_own(s, c) * row.weight;
-            const float other = __shfl_xor_sync(kAll, score, 8);
-            if (row.pair) score += other;
-            if (!live) score = -INFINITY;
-            const float now = fmaxf(kMany ? m : -INFINITY, warp_max(score));
+        }
+        for (int g = 0; g < heads; ++g) {            // (each lane reads what it wrote)
+            float top = sh.p[0][g][lane];
+            if (kParts > 1) top = fmaxf(top, sh.p[kParts - 1][g][lane]);
+            const float now = fmaxf(kMany ? m : -INFINITY, warp_max(top));
             const float base = now == -INFINITY ? 0.f : now;       // no finite score so far: every weight is 0
-            const float p = exp2f(score - base) * row.weight;
+            float p[kParts], sum = 0.f;
+#pragma unroll
+            for (int b = 0; b < kParts; ++b) sum += p[b] = exp2f(sh.p[b][g][lane] - base) * share[b];
             if (kMany) {
                 const float shrink = exp2f(m - base);
-                l = l * shrink + p;
+                l = l * shrink + sum;
                 m = now;
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] *= shrink;
             } else {
-                l = warp_sum(p);
+                l = warp_sum(sum);
                 if (lane == 0) lse[g] = (now + log2f(l)) * kLn2;
             }
-            sh.p[g][lane] = kMany ? p : p / l;
+#pragma unroll
+            for (int b = 0; b < kParts; ++b) sh.p[b][g][lane] = kMany ? p[b] : p[b] / l;
         }
         asm volatile("cp.async.wait_group 0;\n" ::: "memory");
         __syncwarp();
-        float v[8][8];                               // of rows 8 group + j: dims 4c .. 4c+3 and 32 more
+        // rows 8 group + j: dims 4c .. 4c+3 and 32 more; one part's stay in registers for all heads
+        float v[8][8];
+        auto fetch = [&](int b, int j) {
+            *reinterpret_cast<float4*>(v[j]) = *reinterpret_cast<const float4*>(&sh.values[b][8 * group + j][4 * c]);
+            *reinterpret_cast<float4*>(v[j] + 4) = *reinterpret_cast<const float4*>(&sh.values[b][8 * group + j][kHalf + 4 * c]);
+        };
+        if (kParts == 1) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            *reinterpret_cast<float4*>(v[j]) = *reinterpret_cast<const float4*>(&sh.values[8 * group + j][4 * c]);
-            *reinterpret_cast<float4*>(v[j] + 4) = *reinterpret_cast<const float4*>(&sh.values[8 * group + j][kHalf + 4 * c]);
+            for (int j = 0; j < 8; ++j) fetch(0, j);
         }
-        for (int g = 0; g < (kMany ? 1 : heads); ++g) {
+        for (int g = 0; g < heads; ++g) {
             if (!kMany) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[j] = 0.f;
             }
-            float p[8];
-            *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(&sh.p[g][8 * group]);
-            *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(&sh.p[g][8 * group + 4]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int b = 0; b < kParts; ++b) {
+                float p[8];
+                *reinterpret_cast<float4*>(p) = *reinterpret_cast<const float4*>(&sh.p[b][g][8 * group]);
+                *reinterpret_cast<float4*>(p + 4) = *reinterpret_cast<const float4*>(&sh.p[b][g][8 * group + 4]);
 #pragma unroll
-                for (int e = 0; e < 8; e += 2) {
-                    const float2 t = __ffma2_rn(make_float2(p[j], p[j]), make_float2(v[j][e], v[j][e + 1]),
-                                                make_float2(acc[e], acc[e + 1]));
-                    acc[e] = t.x;
-                    acc[e + 1] = t.y;
+                for (int j = 0; j < 8; ++j) {
+                    if (b > 0 && j == 4 && few) break;
+                    if (kParts > 1) fetch(b, j);
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2) {
+                        const float2 t = __ffma2_rn(make_float2(p[j], p[j]), make_float2(v[j][e], v[j][e + 1]),
+                                                    make_float2(acc[e], acc[e + 1]));
+                        acc[e] = t.x;
+                        acc[e + 1] = t.y;
+                    }
                 }
+            }
             if (!kMany) write_out(out + g * kHeadDim, acc, 1.f, lane);
         }
     }
@@ -216,11 +262,12 @@ __global__ void __launch_bounds__(32 * kWarps, 4) attention_f32_kernel(const __g
     }
 }
 
-template <bool kMany>
+template <int kParts, bool kMany>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
-    const dim3 grid((a.units + kWarps - 1) / kWarps), block(32 * kWarps);
-    return a.parents ? launch_kernel(attention_f32_kernel<kMany, true>, grid, block, 0, st, a)
-                     : launch_kernel(attention_f32_kernel<kMany, false>, grid, block, 0, st, a);
+    constexpr int warps = warps_of(kParts);
+    const dim3 grid((a.units + warps - 1) / warps), block(32 * warps);
+    return a.parents ? launch_kernel(attention_f32_kernel<kParts, kMany, true>, grid, block, 0, st, a)
+                     : launch_kernel(attention_f32_kernel<kParts, kMany, false>, grid, block, 0, st, a);
 }
 
 }  // namespace
@@ -231,12 +278,15 @@ cudaError_t launch_attention_f32(const AttnArgs& args, cudaStream_t st) {
     // waiting.  One token each, us: 256 tokens of 8 heads over 1 with 1, 2, 4, 8 heads a warp 5.6,
     // 5.2, 5.9, 8.5; 1024 tokens of 8 over 2 with 1, 2, 4 heads 15.8, 11.2, 9.0.
     const int all = a.N * a.H;
-    a.run = a.r.total > 32 || all < 2048 ? 1 : std::min({a.G, kHeads, std::max(2, all / 2048)});
+    a.run = a.r.total > 64 || (a.r.total > 32 && a.G == 1) || all < 2048 ? 1 : std::min({a.G, kHeads, std::max(2, all / 2048)});
     const unsigned parts = (a.G + a.run - 1) / a.run;
     a.units = (unsigned)a.N * a.c.Hkv * parts;
     a.dRest = FastDiv::make(a.c.Hkv * parts);
     a.dParts = FastDiv::make(parts);
-    return a.r.total > 32 ? launch<true>(a, st) : launch<false>(a, st);
+    // More than 32 rows part by part, but up to 64 at once where heads share them: 1024 tokens with
+    // every rung (37 rows), us: 8 heads over 8 28.8 and 34.2, 8 over 2 22.3 and 18.1.  (Not by the heads
+    // of a warp: a token would have other bits in another batch.)
+    return a.r.total <= 32 ? launch<1, false>(a, st) : a.r.total <= 64 && a.G > 1 ? launch<2, false>(a, st) : launch<1, true>(a, st);
 }
 
 }  // namespace cache
