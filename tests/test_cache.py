@@ -259,6 +259,7 @@ SETS = {  # W, alpha, offsets, options
     "usual": (8, 0.8, FIB, {}), "window alone": (4, 1.0, [], {}), "one key": (0, 1.0, [], {}),
     "integers": (8, 1.0, FIB, {}), "every rung": (5, 1.3, POW, {"dedup": False}), "rounded": (2, 0.77, FIB, {"round_offsets": True}),
     "rungs alone": (0, 1.499, [k + 0.4 for k in range(1, 33)], {}), "wide window": (300, 0.9, FIB, {}),
+    "the most rows": (1024, 1.0, [1030.5 + 5 * k for k in range(32)], {}),
     "40 rows": (20, 0.8, FIB, {}), "64 rows": (31, 1.1, [32.0 + 3 * k for k in range(16)], {}),
     "65 rows": (32, 1.1, [32.0 + 3 * k for k in range(16)], {}), "dead halves": (0, 1.3, [200.1 + k for k in range(30)], {}),
     "near rungs": (3, 0.6, [0.0, 0.3, 1.0, 1.5, 2.25, 4.0], {"dedup": False}),
