@@ -626,7 +626,23 @@ class PagedCache:
     lie; entries may change between calls, unused ones are -1 or anything else.
 
     The object keeps the three tensors and what follows from them; their memory is
-    the caller's.  ``PagedCache.empty`` makes pools."""
+    the caller's.  The library is told of them once: they cannot be replaced (a wider
+    table, another pool: make a new cache, which costs a few microseconds), and are
+    not to be given other memory (``set_``, ``resize_``).  ``PagedCache.empty`` makes
+    pools."""
+
+    _fixed = frozenset({"k_pages", "v_pages", "block_table", "rope_base", "dtype", "Hkv", "index", "device", "unit", "_struct",
+                        "_at"})
+
+    def __setattr__(self, name, value):
+        if name in self._fixed and name in self.__dict__:
+            raise AttributeError(f"{name} of a PagedCache cannot be replaced: make a new one")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._fixed:
+            raise AttributeError(f"{name} of a PagedCache cannot be taken out: make a new one")
+        object.__delattr__(self, name)
 
     def __init__(self, k_pages, v_pages, block_table, *, rope_base: float = 1e4):
         if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or k_pages.shape[3] != 64:

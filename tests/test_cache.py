@@ -842,6 +842,26 @@ def test_binding_refuses_caches(library):   # noqa: F811
         fa.PagedCache.empty(4, 8, 2, t, dtype=torch.float16)
 
 
+@pytest.mark.parametrize("name", ["k_pages", "v_pages", "block_table", "rope_base", "dtype", "Hkv", "index", "device"])
+def test_a_caches_parts_stay(name, library):   # noqa: F811
+    """What the library was told of at the start cannot be replaced behind its back."""
+    cache = fake_cache()
+    was = {n: getattr(cache, n) for n in ("k_pages", "v_pages", "block_table")}
+    with pytest.raises(AttributeError, match="make a new"):
+        setattr(cache, name, torch.empty(3, 9, dtype=torch.int32, device="cuda:0"))
+    with pytest.raises(AttributeError, match="make a new"):
+        delattr(cache, name)
+    with pytest.raises(AttributeError, match="make a new"):
+        cache.__init__(*was.values())
+    assert all(getattr(cache, n) is t for n, t in was.items())
+    cache.note = "layer 3"                                                   # a caller's own attribute
+    cache.note = "layer 4"
+    assert cache.note == "layer 4"
+    del cache.note
+    assert not hasattr(cache, "note")
+
+
+
 def test_binding_refuses_tokens(library):   # noqa: F811
     cache = fake_cache()
     library.calls.clear()
