@@ -421,9 +421,11 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
  * appended before.  opts: scale, no_dedup and round_offsets are used; the other
  * fields have to be zero (rope_base is the cache's).  Products and sums are fp32;
  * q is rotated in fp32 and not rounded (bf16: q keeps 22 bits, the weights of the
- * values 16).  A key or value that is not finite gives outputs that are not, of the
- * heads that read it and of no others.  Limits of W, K and alpha as for
- * fibattn_fwd; 0 <= N, N * H < 2^31. */
+ * values 16).  A value that is not finite gives outputs that are not, of the heads
+ * that read it and of no others.  So does a key, but for scores of -infinity, which
+ * count for nothing (where there are no others out is NaN and lse -infinity): an
+ * infinite key gives those, or NaN, by the signs of q's rotated values that meet it.
+ * Limits of W, K and alpha as for fibattn_fwd; 0 <= N, N * H < 2^31. */
 int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
                        void* out, float* lse, const int* positions, const int* seqs, int N, int H, int W,
                        float alpha, const float* offsets, int K, const fibattn_opts* opts, void* stream);

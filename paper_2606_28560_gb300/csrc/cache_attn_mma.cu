@@ -44,6 +44,14 @@ __device__ __forceinline__ void fit_half(float largest, float& up, float& down) 
     down = __uint_as_float((unsigned)(254 - e) << 23);
 }
 
+// A score from the sums of q's upper and lower halves.  Where a key is infinite the upper
+// half's sum has the score's sign (or is NaN), the lower half's that of a rounding: it is left
+// out where it makes NaN of the two.  (128 chunks 143.3 us with this, 141.1 without.)
+__device__ __forceinline__ float whole(float upper, float lower) {
+    const float s = upper + lower;
+    return s == s ? s : upper;
+}
+
 constexpr int kStages = 3;                           // of the ring
 constexpr unsigned kBytes = 32 * kHeadDim * 2;       // 32 rows of a head
 
@@ -215,8 +223,8 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 6 : 8) attention_mma_kern
                     mma::mma_f16_16816(d, qf[2], k[4], k[5]);
                     mma::mma_f16_16816(d, qf[3], k[6], k[7]);
                     if (j == 0 || mine == j) {
-                        s[c][i][0] = d[0] + d[2];
-                        s[c][i][1] = d[1] + d[3];
+                        s[c][i][0] = whole(d[0], d[2]);
+                        s[c][i][1] = whole(d[1], d[3]);
                     }
                 }
                 advance();

@@ -393,6 +393,54 @@ def test_values_that_are_not_finite_stay_with_their_heads(N, H, Hkv, W, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("W", [4, 90])
+@pytest.mark.parametrize("N,H,Hkv", [(3, 8, 8), (1100, 8, 8), (1500, 8, 2), (700, 22, 2)])
+def test_infinite_keys(N, H, Hkv, W, dtype):
+    """A score of -infinity leaves its slot out, in a window or a rung; one that is +infinity
+    or none makes the output of its token and head NaN, whatever q's roundings are."""
+    cache, g = filled([200], 256, Hkv, dtype, 5)
+    page = int(cache.block_table[0, 0])
+    f = [W + 6.5, W + 16.0]
+    slots = slots_of(W, 1.0, f)
+    pos, seqs = torch.full((N,), 190).int(), torch.zeros(N).int()
+    q = tokens(g, N, H, dtype)
+    turned = rotated(q.cpu(), pos)
+    few = list(range(0, N, max(1, N // 40)))
+    for distance, gone in ((0, 0), (2, 2), (W + 6, W + 1), (W + 7, W + 1), (W + 16, W + 2)):
+        left = [s for i, s in enumerate(slots) if i != gone]
+        want = Model(cache).attention(q[few], pos[few], seqs[few], left)
+        kept = cache.k_pages[page, 190 - distance].clone()
+        key = torch.randn(Hkv, D, generator=g)
+        key[:, 7], key[::2, 40] = -math.inf, math.inf
+        cache.k_pages[page, 190 - distance] = key.to(cache.k_pages.dtype)
+        out, lse = fa.cached_fwd(q, cache, 1.0, f, W, pos.cuda(), seqs=seqs.cuda())
+        cache.k_pages[page, 190 - distance] = kept
+        score = (turned * key.repeat_interleave(H // Hkv, 0)).sum(-1)
+        dropped = score == -math.inf
+        assert dropped.any() and (~dropped).any() and not torch.isfinite(score).any()
+        assert torch.isnan(out.cpu()[~dropped]).all() and not torch.isfinite(lse.cpu()[~dropped]).any()
+        at = dropped[few]
+        part = [t.cpu()[few].where(at if t.dim() == 2 else at[..., None], w.to(t.dtype)) for t, w in zip((out, lse), want)]
+        check(part, want, W, len(f))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_infinite_keys_alone(dtype):
+    """Nothing is left: 0 / 0, and a sum of nothing."""
+    cache, g = filled([1], 16, 2, dtype, 5)
+    page = int(cache.block_table[0, 0])
+    cache.k_pages[page, 0, 0, 3] = -math.inf
+    q = tokens(g, 1, 16, dtype)
+    out, lse = fa.cached_fwd(q, cache, 1.0, FIB, 8, torch.zeros(1, dtype=torch.int32, device="cuda"))
+    dropped = q[0, :8, 3] > 0                                                # (position 0: q as it is)
+    assert dropped.any() and torch.isnan(out[0, :8]).all()
+    assert (lse[0, :8][dropped] == -math.inf).all() and not torch.isfinite(lse[0, :8]).any()
+    assert torch.isfinite(out[0, 8:]).all() and torch.isfinite(lse[0, 8:]).all()
+
+
+@pytest.mark.gpu
 def test_what_does_not_exist_is_not_read():
     lengths = [30, 30, 30, 30]
     cache, g = filled(lengths, 8, 2, BF, 8)
@@ -859,7 +907,6 @@ def test_a_caches_parts_stay(name, library):   # noqa: F811
     assert cache.note == "layer 4"
     del cache.note
     assert not hasattr(cache, "note")
-
 
 
 def test_binding_refuses_tokens(library):   # noqa: F811
