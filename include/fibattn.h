@@ -420,8 +420,9 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
  * integer, p - floor(d_k) - 1: its own key and value too, which have to be
  * appended before.  opts: scale, no_dedup and round_offsets are used; the other
  * fields have to be zero (rope_base is the cache's).  Products and sums are fp32;
- * q is rotated in fp32 and not rounded (bf16: q keeps 22 bits, the weights of the
- * values 16).  A value that is not finite gives outputs that are not, of the heads
+ * q is rotated in fp32 and not rounded (bf16: the weights of the values keep 16 bits;
+ * q keeps 22 bits of what is 2^-29 of its head's largest value or more, and of smaller
+ * values all but 2^-50 of that largest).  A value that is not finite gives outputs that are not, of the heads
  * that read it and of no others.  So does a key, but for scores of -infinity, which
  * count for nothing (where there are no others out is NaN and lse -infinity): an
  * infinite key gives those, or NaN, by the signs of q's rotated values that meet it.

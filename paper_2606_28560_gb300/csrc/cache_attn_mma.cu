@@ -36,19 +36,23 @@ namespace {
 
 constexpr int kWarps = 2;
 
-// 2^k for scaling q to fp16's upper range, from the exponent of its largest value,
-// and 2^-k: halves of fp16 then keep 22 bits of every q, whatever its size.
+// 2^k for scaling q to fp16's upper range, from the exponent of a head's largest value, which
+// comes to lie in [2^14, 2^15), and 2^-k.  With the lower half times kLow, two halves of fp16
+// keep 22 bits of a value down to 2^-29 of the largest, from where on the upper half is
+// subnormal, and of smaller ones all but 2^-50 of the largest.
 __device__ __forceinline__ void fit_half(float largest, float& up, float& down) {
     const int e = min(268 - (int)(__float_as_uint(largest) >> 23), 253);
     up = __uint_as_float((unsigned)e << 23);
     down = __uint_as_float((unsigned)(254 - e) << 23);
 }
 
+constexpr float kLow = 2048.f;                       // 2^11: a lower half to the size of its upper one
+
 // A score from the sums of q's upper and lower halves.  Where a key is infinite the upper
 // half's sum has the score's sign (or is NaN), the lower half's that of a rounding: it is left
 // out where it makes NaN of the two.  (128 chunks 143.3 us with this, 141.1 without.)
 __device__ __forceinline__ float whole(float upper, float lower) {
-    const float s = upper + lower;
+    const float s = fmaf(lower, 1.f / kLow, upper);
     return s == s ? s : upper;
 }
 
@@ -186,11 +190,11 @@ __global__ void __launch_bounds__(32 * kWarps, kMany ? 6 : 8) attention_mma_kern
             sc = down * a.scale;
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
-                const float y0 = y[2 * c] * up, y1 = y[2 * c + 1] * up;
-                const __half2 hi = __floats2half2_rn(y0, y1);
+                const float2 x = __fmul2_rn(make_float2(y[2 * c], y[2 * c + 1]), make_float2(up, up));
+                const __half2 hi = __float22half2_rn(x);
                 qf[c >> 1][2 * (c & 1)] = *reinterpret_cast<const unsigned*>(&hi);
-                const float2 f = __half22float2(hi);
-                qf[c >> 1][2 * (c & 1) + 1] = mma::pack_f16(y0 - f.x, y1 - f.y);
+                const float2 low = __ffma2_rn(__half22float2(hi), make_float2(-kLow, -kLow), __fmul2_rn(x, make_float2(kLow, kLow)));
+                qf[c >> 1][2 * (c & 1) + 1] = mma::pack_f16(low.x, low.y);
             }
         }
         float s[kParts][4][2];

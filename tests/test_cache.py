@@ -441,6 +441,28 @@ def test_infinite_keys_alone(dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("outlier", [2.0 ** 12, 2.0 ** 20, 2.0 ** 28])
+def test_an_outlier_in_a_query(outlier, dtype):
+    """One pair of q's dims far above the others, where the keys are 0: the others keep their
+    bits.  bf16: q's halves keep 22 bits down to 2^-29 of a head's largest value and all but
+    2^-50 of that below it: at most 2^-21.9 of a key here, which the 96 u A of `check` allow
+    where sum |q k| is above 2^-4.5 sum |k| (of 62 normal values each: about 2^-0.3)."""
+    H = 8
+    cache, g = filled([400], 16, H, dtype, 4)
+    N = 64
+    pos, seqs = torch.randint(0, 400, (N,), generator=g).int(), torch.zeros(N).int()
+    q = tokens(g, N, H, dtype).clone()
+    cache.k_pages.mul_(8.0)
+    for h in range(H):
+        m = 4 * h + 1
+        cache.k_pages[..., h, m] = cache.k_pages[..., h, m + 32] = 0
+        q[:, h, m], q[:, h, m + 32] = outlier, -outlier / 3
+    got = fa.cached_fwd(q, cache, 0.8, FIB, 8, pos.cuda(), seqs=seqs.cuda())
+    check(got, Model(cache).attention(q, pos, seqs, slots_of(8, 0.8, FIB)), 8, 15)
+
+
+@pytest.mark.gpu
 def test_what_does_not_exist_is_not_read():
     lengths = [30, 30, 30, 30]
     cache, g = filled(lengths, 8, 2, BF, 8)
