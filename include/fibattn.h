@@ -415,18 +415,19 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
 
 /* Attention of N tokens over the cache: q [N][H][64] as k above (H a multiple of
  * the cache's Hkv; query head h reads head h / (H / Hkv)), out [N][H][64]
- * contiguous, lse [N][H] fp32.  The query at position p reads slots p .. p-W and,
- * for every active rung with d_k <= p, slots p - floor(d_k) and, where d_k is no
- * integer, p - floor(d_k) - 1: its own key and value too, which have to be
- * appended before.  opts: scale, no_dedup and round_offsets are used; the other
- * fields have to be zero (rope_base is the cache's).  Products and sums are fp32;
- * q is rotated in fp32 and not rounded (bf16: the weights of the values keep 16 bits;
- * q keeps 22 bits of what is 2^-29 of its head's largest value or more, and of smaller
- * values all but 2^-50 of that largest).  A value that is not finite gives outputs that are not, of the heads
- * that read it and of no others.  So does a key, but for scores of -infinity, which
- * count for nothing (where there are no others out is NaN and lse -infinity): an
- * infinite key gives those, or NaN, by the signs of q's rotated values that meet it.
- * Limits of W, K and alpha as for fibattn_fwd; 0 <= N, N * H < 2^31. */
+ * contiguous and on 16 bytes, lse [N][H] fp32, contiguous.  The query at position p
+ * reads slots p .. p-W and, for every active rung with d_k <= p, slots p - floor(d_k)
+ * and, where d_k is no integer, p - floor(d_k) - 1: its own key and value too, which
+ * have to be appended before.  opts: scale, no_dedup and round_offsets are used; the
+ * other fields have to be zero (rope_base is the cache's).  Products and sums are
+ * fp32; q is rotated in fp32 and not rounded (bf16: the weights of the values keep 16
+ * bits; q keeps 22 bits of what is 2^-29 of its head's largest value or more, and of
+ * smaller values all but 2^-50 of that largest).  A value that is not finite gives
+ * outputs that are not, of the heads that read it and of no others.  So does a key,
+ * but for scores of -infinity, which count for nothing (where there are no others out
+ * is NaN and lse -infinity): an infinite key gives those, or NaN, by the signs of q's
+ * rotated values that meet it.  Limits of W, K and alpha as for fibattn_fwd;
+ * 0 <= N, N * H < 2^31. */
 int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
                        void* out, float* lse, const int* positions, const int* seqs, int N, int H, int W,
                        float alpha, const float* offsets, int K, const fibattn_opts* opts, void* stream);

@@ -73,8 +73,9 @@ int attention(const fibattn_cache* c, const void* q, long long q_token, long lon
     if (N == 0) return FIBATTN_OK;
     if (!q || !out || !lse || !positions || (parents && !slots))
         return set_error(FIBATTN_ERR_INVALID_ARG, "NULL tensor pointer");
-    if (misaligned16(q) || misaligned16(out) || misaligned16(lse) || !strides_ok(*c, q_token, q_head))
-        return set_error(FIBATTN_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, strides multiples of 16 bytes");
+    if (misaligned16(q) || misaligned16(out) || ((uintptr_t)lse & 3u) || !strides_ok(*c, q_token, q_head))
+        return set_error(FIBATTN_ERR_INVALID_ARG,
+                         "tensor pointers must be 16-byte aligned (lse: 4-byte), strides multiples of 16 bytes");
     cache::AttnArgs a;
     std::memset(&a, 0, sizeof(a));
     a.c = view_of(*c);

@@ -463,6 +463,25 @@ def test_an_outlier_in_a_query(outlier, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("W", [8, 90])
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_lse_anywhere(offset, W, dtype):
+    """lse may be a part of a larger tensor, at any offset; what is beside it stays."""
+    cache, g = filled([30, 120], 16, 2, dtype, 2)
+    pos, q = torch.tensor([29, 119]).int().cuda(), tokens(g, 2, 4, dtype)
+    want = fa.cached_fwd(q, cache, 0.8, FIB, W, pos)
+    whole = torch.full((16,), 5.0, device="cuda")
+    lse = whole[offset:offset + 8].view(2, 4)
+    _, z = fa.cached_fwd(q, cache, 0.8, FIB, W, pos, lse=lse)
+    assert z is lse and torch.equal(lse, want[1]) and (whole[:offset] == 5).all() and (whole[offset + 8:] == 5).all()
+    whole.fill_(5.0)
+    roots = torch.full((2,), -1, dtype=torch.int32, device="cuda")
+    fa.tree_fwd(q, cache, 0.8, FIB, W, pos, roots, pos, lse=lse)
+    assert torch.equal(lse, want[1]) and (whole[:offset] == 5).all() and (whole[offset + 8:] == 5).all()
+
+
+@pytest.mark.gpu
 def test_what_does_not_exist_is_not_read():
     lengths = [30, 30, 30, 30]
     cache, g = filled(lengths, 8, 2, BF, 8)
@@ -850,6 +869,13 @@ def attend(c, tree, opts=None, **k):
     call = B.lib().fibattn_tree_fwd if tree else B.lib().fibattn_cached_fwd
     rc = call(c and ctypes.addressof(c), *a.values(), opts and ctypes.addressof(opts), None)
     return rc, B.lib().fibattn_last_error().decode()
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_attention_refuses_an_lse_between_values(tree):
+    c, _, _ = init()
+    rc, message = attend(c, tree, lse=258)
+    assert rc == 1 and "lse: 4-byte" in message
 
 
 @pytest.mark.parametrize("tree", [False, True])
