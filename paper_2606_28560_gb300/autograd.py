@@ -139,10 +139,18 @@ class FibAttention(torch.nn.Module):
         """Generating with the layer: its attention for new tokens over a ``PagedCache``
         (``cached_fwd``), or for trees of drafts (``tree_fwd``, when ``parents`` and
         ``slots`` are given).  q [tokens, H, 64]; the tokens' own keys and values have
-        to be in the cache.  Returns (out, lse); no gradients."""
+        to be in the cache.  Returns (out, lse); no gradients.
+
+        ``alpha``: the host value of 0.5 + sigmoid(theta) (``layer.alpha``, read once).
+        Without it a theta on the GPU is read at every call, which waits for the work
+        before it and cannot be captured into a graph."""
         if cache.rope_base != self.rope_base:
             raise ValueError(f"the cache turns its keys by rope_base {cache.rope_base}, the layer by {self.rope_base}")
-        alpha = self.alpha if alpha is None else float(alpha)
+        if alpha is None:
+            if self.theta.is_cuda and torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("theta on the GPU cannot be read in a capture: give alpha, read before it (layer.alpha)")
+            alpha = self.alpha
+        alpha = float(alpha)
         if parents is None and slots is None:
             return B.cached_fwd(q, cache, alpha, self.offsets, self.W, positions, seqs=seqs, scale=self.scale,
                                 dedup=self.dedup, out=out, lse=lse)

@@ -63,3 +63,32 @@ def test_layer_over_a_cache():
         layer.cached(q, cache, positions, seqs=seqs, parents=parents)
     with pytest.raises(ValueError, match="rope_base"):
         layer.cached(q, fa.PagedCache.empty(4, 8, 2, table, dtype=torch.float32, rope_base=5e5), positions, seqs=seqs)
+
+
+@pytest.mark.gpu
+def test_layer_in_a_capture():
+    """With alpha given, the layer's call is captured; without, theta would be read from the
+    GPU: refused, and the capture goes on."""
+    layer = fa.FibAttention(W=5, theta=0.3).cuda()
+    table = torch.arange(4, dtype=torch.int32, device="cuda").view(1, 4)
+    cache = fa.PagedCache.empty(4, 8, 2, table, dtype=torch.float32)
+    positions = torch.arange(30, dtype=torch.int32, device="cuda")
+    seqs = torch.zeros(30, dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn(30, h, 64, device="cuda") for h in (4, 2, 2))
+    fa.cache_append(cache, k, v, positions, seqs=seqs)
+    alpha = layer.alpha
+    want = layer.cached(q, cache, positions, seqs=seqs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(RuntimeError, match="alpha"):
+            layer.cached(q, cache, positions, seqs=seqs)
+        got = layer.cached(q, cache, positions, seqs=seqs, alpha=alpha)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    fixed = fa.FibAttention(W=5, theta=0.3, learned=False)           # theta on the CPU: read without waiting
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph := torch.cuda.CUDAGraph()):
+        got = fixed.cached(q, cache, positions, seqs=seqs)
+    graph.replay()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
