@@ -125,7 +125,7 @@ class FibAttention(torch.nn.Module):
 
     @property
     def alpha(self) -> float:
-        return alpha_of_theta(float(self.theta))
+        return alpha_of_theta(float(self.theta.detach()))
 
     def forward(self, q, k, v, alpha=None):
         """``alpha``: the host value of 0.5 + sigmoid(theta), when the caller

@@ -1,6 +1,8 @@
 """The example model generating: its layers over the library's paged cache."""
 from __future__ import annotations
 
+import warnings
+
 import pytest
 import torch
 
@@ -92,3 +94,14 @@ def test_layer_in_a_capture():
         got = fixed.cached(q, cache, positions, seqs=seqs)
     graph.replay()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_alpha_is_read_without_a_warning():
+    layer, always = fa.FibAttention(theta=0.3), torch.is_warn_always_enabled()
+    torch.set_warn_always(True)
+    try:
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            assert abs(layer.alpha - 1.0744425) < 1e-6
+    finally:
+        torch.set_warn_always(always)
