@@ -144,7 +144,7 @@ class FibAttention(torch.nn.Module):
         ``alpha``: the host value of 0.5 + sigmoid(theta) (``layer.alpha``, read once).
         Without it a theta on the GPU is read at every call, which waits for the work
         before it and cannot be captured into a graph."""
-        if cache.rope_base != self.rope_base:
+        if cache.rope_base != (self.rope_base or 1e4):          # (0: the library's own)
             raise ValueError(f"the cache turns its keys by rope_base {cache.rope_base}, the layer by {self.rope_base}")
         if alpha is None:
             if self.theta.is_cuda and torch.cuda.is_current_stream_capturing():

@@ -659,7 +659,7 @@ class PagedCache:
         if strides != _pool_strides(v_pages):
             raise ValueError("k_pages and v_pages must have the same strides")
         self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
-        self.rope_base = float(rope_base)
+        self.rope_base = float(rope_base) or 1e4          # (0: the library's own)
         self.dtype, self.Hkv, self.index, self.device = v_pages.dtype, k_pages.shape[2], index, k_pages.device
         self.unit = 16 // v_pages.element_size()          # strides of tokens are multiples of this
         pages, rows, heads, D = k_pages.shape

@@ -957,6 +957,21 @@ def test_a_caches_parts_stay(name, library):   # noqa: F811
     assert not hasattr(cache, "note")
 
 
+@pytest.mark.parametrize("layers", [0, 0.0, 1e4, 10000])
+@pytest.mark.parametrize("caches", [0, 0.0, 1e4, 10000])
+def test_a_rope_base_of_zero_is_the_librarys_own(layers, caches, library):   # noqa: F811
+    """0 and 1e4 are one rotation, as they are for `fwd`: a layer of one takes a cache of the other."""
+    layer = fa.FibAttention(rope_base=layers)
+    table = torch.empty(3, 5, dtype=torch.int32, device="cuda:0")
+    cache = fa.PagedCache.empty(4, 8, 2, table, rope_base=caches)
+    q = torch.empty(5, 2, 64, dtype=BF, device="cuda:0")
+    library.calls.clear()
+    layer.cached(q, cache, i32(5), alpha=1.0)
+    assert [name for name, _ in library.calls] == ["fibattn_cached_fwd"]
+    with pytest.raises(ValueError, match="rope_base"):
+        fa.FibAttention(rope_base=5e5).cached(q, cache, i32(5), alpha=1.0)
+
+
 def test_binding_refuses_tokens(library):   # noqa: F811
     cache = fake_cache()
     library.calls.clear()
