@@ -655,6 +655,8 @@ class PagedCache:
             raise ValueError("the pools and block_table must be on one CUDA device")
         if block_table.dim() != 2 or block_table.dtype != torch.int32 or not block_table.is_contiguous():
             raise ValueError("block_table must be a contiguous int32 tensor [seqs, pages of a sequence]")
+        if max(*k_pages.shape, *block_table.shape) > _MOST:
+            raise ValueError("the sizes of the pools and of block_table must be below 2^31")
         strides = _pool_strides(k_pages)
         if strides != _pool_strides(v_pages):
             raise ValueError("k_pages and v_pages must have the same strides")
@@ -686,11 +688,16 @@ def _pool_strides(t):
     return tuple(64 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()))
 
 
+_MOST = 2 ** 31 - 1                     # of an int of the library: ctypes would cut a larger one short
+
+
 def _tokens(t, cache, name):
     """(pointer, token stride, head stride) of tokens [N, heads, 64] as the library takes them."""
     shape = t.shape
     if len(shape) != 3 or shape[2] != 64 or t.dtype is not cache.dtype or t.get_device() != cache.index:
         raise ValueError(f"{name} must be [tokens, heads, 64] of the cache's dtype, on its device")
+    if shape[0] * shape[1] > _MOST:
+        raise ValueError(f"{name}: tokens times heads must be below 2^31")
     token, head, last = t.stride()
     if shape[0] == 1:
         token = 0
@@ -800,6 +807,9 @@ def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, sca
     p = _ints(positions, each, index, "positions")
     b = None if seqs is None else _ints(seqs, each, index, "seqs")
     _check_device(index)
+    W = int(W)
+    if not -_MOST <= W <= _MOST:
+        raise ValueError(f"W must be in [0, 1024] (got {W})")
     f, K, alive = _offset_table(offsets)              # noqa: F841 (alive, kept: until the call is over)
     o, kept = _opt_struct(scale, dedup, round_offsets)   # noqa: F841
     if out is None:
@@ -811,11 +821,11 @@ def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, sca
     elif lse.dtype is not torch.float32 or lse.shape != (N, H) or lse.get_device() != index or not lse.is_contiguous():
         raise ValueError("lse must be a contiguous fp32 tensor [N, H] on q's device")
     if parents is None:
-        rc = lib().fibattn_cached_fwd(cache._at, *at, out.data_ptr(), lse.data_ptr(), p, b, N, H, int(W), float(alpha), f, K,
+        rc = lib().fibattn_cached_fwd(cache._at, *at, out.data_ptr(), lse.data_ptr(), p, b, N, H, W, float(alpha), f, K,
                                       o, _raw_stream(index))
     else:
         rc = lib().fibattn_tree_fwd(cache._at, *at, out.data_ptr(), lse.data_ptr(), p, _ints(parents, each, index, "parents"),
-                                    _ints(slots, each, index, "slots"), b, N, H, int(W), float(alpha), f, K, o,
+                                    _ints(slots, each, index, "slots"), b, N, H, W, float(alpha), f, K, o,
                                     _raw_stream(index))
     if rc:
         _check(rc)

@@ -972,6 +972,25 @@ def test_a_rope_base_of_zero_is_the_librarys_own(layers, caches, library):   # n
         fa.FibAttention(rope_base=5e5).cached(q, cache, i32(5), alpha=1.0)
 
 
+def test_binding_refuses_sizes_beyond_an_int(library):   # noqa: F811
+    """More than 31 bits would arrive at the library cut short: 2^32 + 1 tokens as one."""
+    cache = fake_cache()
+    library.calls.clear()
+    one, n = torch.empty(1, 2, 64, dtype=BF, device="cuda:0"), 2 ** 32 + 1
+    many, p = one.expand(n, 2, 64), i32(n)
+    for call in (lambda: fa.cache_append(cache, many, many, p), lambda: fa.cached_fwd(many, cache, 1.0, [1.0], 8, p),
+                 lambda: fa.tree_fwd(many, cache, 1.0, [1.0], 8, p, p, p)):
+        with pytest.raises(ValueError, match="2.31"):
+            call()
+    for W in (2 ** 32 + 8, 2 ** 31, -2 ** 32):
+        with pytest.raises(ValueError, match="W must"):
+            fa.cached_fwd(one, cache, 1.0, [1.0], W, i32(1))
+    for table in ((n, 5), (3, n)):
+        with pytest.raises(ValueError, match="2.31"):
+            fa.PagedCache.empty(4, 8, 2, torch.empty(table, dtype=torch.int32, device="cuda:0"))
+    assert not library.calls
+
+
 def test_binding_refuses_tokens(library):   # noqa: F811
     cache = fake_cache()
     library.calls.clear()
