@@ -16,6 +16,9 @@ constexpr unsigned kReady = 0xf1bac4e1u;
 constexpr long long kMaxSlots = 1LL << 30;           // storage slots of a sequence
 
 bool misaligned16(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+bool misaligned4(const void* a, const void* b, const void* c, const void* d) {
+    return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 3u) != 0;
+}
 
 int launch_failed(cudaError_t e, const char* what) {
     return set_errorf(FIBATTN_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
@@ -73,6 +76,8 @@ int attention(const fibattn_cache* c, const void* q, long long q_token, long lon
     if (N == 0) return FIBATTN_OK;
     if (!q || !out || !lse || !positions || (parents && !slots))
         return set_error(FIBATTN_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (misaligned4(positions, parents, slots, seqs))
+        return set_error(FIBATTN_ERR_INVALID_ARG, "positions, parents, slots and seqs must be 4-byte aligned");
     if (misaligned16(q) || misaligned16(out) || ((uintptr_t)lse & 3u) || !strides_ok(*c, q_token, q_head))
         return set_error(FIBATTN_ERR_INVALID_ARG,
                          "tensor pointers must be 16-byte aligned (lse: 4-byte), strides multiples of 16 bytes");
@@ -167,6 +172,8 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
         return set_errorf(FIBATTN_ERR_INVALID_ARG, "N must not be negative and N * Hkv below 2^31 (got N %d)", N);
     if (N == 0) return FIBATTN_OK;
     if (!k || !v || !positions) return set_error(FIBATTN_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (misaligned4(positions, slots, seqs, nullptr))
+        return set_error(FIBATTN_ERR_INVALID_ARG, "positions, slots and seqs must be 4-byte aligned");
     if (misaligned16(k) || misaligned16(v) || !strides_ok(*c, k_token_stride, k_head_stride) ||
         !strides_ok(*c, v_token_stride, v_head_stride))
         return set_error(FIBATTN_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned, strides multiples of 16 bytes");

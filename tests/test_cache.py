@@ -902,6 +902,20 @@ def test_attention_refuses(change, words, tree):
     assert attend(c, tree, o)[0] == 1
 
 
+@pytest.mark.parametrize("which", ["positions", "slots", "seqs", "parents"])
+def test_integers_between_values_are_refused(which):
+    c, _, _ = init()
+    calls = [(lambda k: attend(c, True, **k))]
+    if which != "parents":
+        calls.append(lambda k: append(c, **k))
+    if which in ("positions", "seqs"):
+        calls.append(lambda k: attend(c, False, **k))
+    for call in calls:
+        for at in (257, 258, 259):
+            rc, message = call({which: at})
+            assert rc == 1 and "4-byte aligned" in message and which in message
+
+
 def test_tree_refuses_no_parents():
     c, _, _ = init()
     assert attend(c, True, parents=None)[0] == 1 and attend(c, True, slots=None)[0] == 1
