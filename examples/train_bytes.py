@@ -86,6 +86,8 @@ class Model(torch.nn.Module):
     def generate(self, prompts, n):
         """The n likeliest bytes after each of the prompts [B, T], one after another."""
         B, T = prompts.shape
+        if n < 1:
+            return prompts.new_empty(B, 0)
         caches, alphas = self.caches(T + n, B, torch.bfloat16), self.alphas()
         out, tokens = [], prompts.reshape(-1)
         seqs = torch.arange(B, dtype=torch.int32, device="cuda")

@@ -44,6 +44,12 @@ def test_generates():
     assert fa.check_status() == 0
 
 
+def test_generates_nothing():
+    model = load().Model(1, 64)
+    text = model.generate(torch.zeros(2, 5, dtype=torch.int64), 0)
+    assert text.shape == (2, 0) and text.dtype == torch.int64
+
+
 @pytest.mark.gpu
 def test_layer_over_a_cache():
     """The module's call, for tokens and for a tree, is the library's; another rotation is refused."""
