@@ -67,10 +67,10 @@ cudaError_t launch_append(const AppendArgs& a, bool bf16, cudaStream_t st);
 cudaError_t launch_attention_f32(const AttnArgs& a, cudaStream_t st);
 cudaError_t launch_attention_mma(const AttnArgs& a, cudaStream_t st);          // bf16
 
-// cos and sin of the angle of pair m at position pos, to fp32 rounding: the phase
-// is an integer fraction of a turn (RopeParams), so its quadrant is taken off
-// exactly and the rest, at most an eighth of a turn, has an error of 2^-25 of
-// itself; rope_cs, with 2^-21, would show in fp32 keys.
+// cos and sin of the angle of pair m at position pos, to fp32 rounding: the phase is
+// an integer fraction of a turn (RopeParams), cut to 2^-32 of one (1.5e-9 in the
+// angle); its quadrant is taken off exactly, and rounding what is left, at most an
+// eighth of a turn, costs 2^-24 of it.  rope_cs, with 2^-21, would show in fp32 keys.
 __device__ __forceinline__ void rope_cs_f32(const RopeParams& rp, int m, int pos, float& c, float& s) {
     const unsigned turn = (unsigned)(((unsigned long long)(unsigned)pos * rp.F[m]) >> 32);   // of 2^32
     const unsigned quarter = (turn + (1u << 29)) >> 30;
