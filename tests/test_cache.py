@@ -555,6 +555,39 @@ def test_tree(H, Hkv, rows, wide, which, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("W", [8, 20])
+@pytest.mark.parametrize("H,Hkv", [(8, 2), (3, 3), (8, 8), (22, 2)])
+def test_many_trees_and_few(H, Hkv, W, dtype):
+    """2500 drafts, where a warp takes several key/value heads (bf16) or query heads (fp32):
+    the definition, and the same bits as a few sequences at a time; a value that is not
+    finite stays with its head."""
+    lengths = [(37 * b) % 900 for b in range(50)]
+    cache, g = filled(lengths, 16, Hkv, dtype, W, more=50)
+    seqs, positions, slots, parents = drafted(g, lengths, [50] * 50)
+    i32 = [t.cuda() for t in (positions, parents, slots, seqs)]
+    k, v = (tokens(g, 2500, Hkv, dtype, 1) for _ in range(2))
+    fa.cache_append(cache, k, v, i32[0], seqs=i32[3], slots=i32[2])
+    q = tokens(g, 2500, H, dtype, 2)
+    out, lse = fa.tree_fwd(q, cache, 0.8, FIB, W, *i32[:3], seqs=i32[3])
+    for b, m in ((0, 1), (7, 3), (48, 2)):                                   # sequences b .. b + m - 1
+        at = slice(50 * b, 50 * (b + m))
+        up = torch.where(i32[1][at] < 0, -1, i32[1][at] - 50 * b)
+        few = fa.tree_fwd(q[at], cache, 0.8, FIB, W, i32[0][at], up, i32[2][at], seqs=i32[3][at])
+        assert torch.equal(few[0], out[at]) and torch.equal(few[1], lse[at])
+        want = Model(cache).attention(q[at], positions[at], seqs[at], slots_of(W, 0.8, FIB), parents=up.cpu(), at=slots[at])
+        check((out[at], lse[at]), want, W, len(FIB))
+    page = int(cache.block_table[7, int(slots[350]) // 16])                  # of a root that others read
+    cache.v_pages[page, int(slots[350]) % 16, 1, 3] = float("nan")
+    again, z = fa.tree_fwd(q, cache, 0.8, FIB, W, *i32[:3], seqs=i32[3])
+    mine = torch.arange(H) // (H // Hkv) == 1
+    hit = torch.isnan(again[:, mine]).any(-1).any(-1).cpu()
+    assert hit[350] and hit.sum() > 1 and (seqs[hit] == 7).all() and torch.equal(z, lse)
+    assert torch.equal(again[:, ~mine], out[:, ~mine]) and torch.equal(again[~hit], out[~hit])
+    assert fa.check_status() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_a_chain_of_drafts_is_the_sequence(dtype):
     """A chain of 100 drafts at their positions' slots, verified, is what cached_fwd computes."""
     cache, g = filled([400], 16, 2, dtype, 1)
