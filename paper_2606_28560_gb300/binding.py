@@ -627,7 +627,7 @@ class PagedCache:
 
     The object keeps the three tensors and what follows from them; their memory is
     the caller's.  The library is told of them once: they cannot be replaced (a wider
-    table, another pool: make a new cache, which costs a few microseconds), and are
+    table, another pool: make a new cache, some 10 us), and are
     not to be given other memory (``set_``, ``resize_``).  ``PagedCache.empty`` makes
     pools."""
 
@@ -635,7 +635,7 @@ class PagedCache:
                         "_at"})
 
     def __setattr__(self, name, value):
-        if name in self._fixed and name in self.__dict__:
+        if name in self._fixed:
             raise AttributeError(f"{name} of a PagedCache cannot be replaced: make a new one")
         object.__setattr__(self, name, value)
 
@@ -645,6 +645,8 @@ class PagedCache:
         object.__delattr__(self, name)
 
     def __init__(self, k_pages, v_pages, block_table, *, rope_base: float = 1e4):
+        if hasattr(self, "_at"):
+            raise AttributeError("a PagedCache cannot be set up again: make a new one")
         if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or k_pages.shape[3] != 64:
             raise ValueError("k_pages and v_pages must be [pages, rows, Hkv, 64], alike")
         want = {torch.bfloat16: torch.float16, torch.float32: torch.float32}.get(v_pages.dtype)
@@ -660,15 +662,23 @@ class PagedCache:
         strides = _pool_strides(k_pages)
         if strides != _pool_strides(v_pages):
             raise ValueError("k_pages and v_pages must have the same strides")
-        self.k_pages, self.v_pages, self.block_table = k_pages, v_pages, block_table
-        self.rope_base = float(rope_base) or 1e4          # (0: the library's own)
-        self.dtype, self.Hkv, self.index, self.device = v_pages.dtype, k_pages.shape[2], index, k_pages.device
-        self.unit = 16 // v_pages.element_size()          # strides of tokens are multiples of this
         pages, rows, heads, D = k_pages.shape
-        self._struct = CacheStruct()
-        self._at = ctypes.addressof(self._struct)
-        _check(lib().fibattn_cache_init(self._at, k_pages.data_ptr(), v_pages.data_ptr(), pages, rows, heads, D, *strides,
+        struct = CacheStruct()
+        at = ctypes.addressof(struct)
+        _check(lib().fibattn_cache_init(at, k_pages.data_ptr(), v_pages.data_ptr(), pages, rows, heads, D, *strides,
                                         block_table.data_ptr(), *block_table.shape, _dtype_code(v_pages), float(rope_base)))
+        put = object.__setattr__                               # (past the refusal above)
+        put(self, "k_pages", k_pages)
+        put(self, "v_pages", v_pages)
+        put(self, "block_table", block_table)
+        put(self, "rope_base", float(rope_base) or 1e4)        # (0: the library's own)
+        put(self, "dtype", v_pages.dtype)
+        put(self, "Hkv", heads)
+        put(self, "index", index)
+        put(self, "device", k_pages.device)
+        put(self, "unit", 16 // v_pages.element_size())        # strides of tokens are multiples of this
+        put(self, "_struct", struct)
+        put(self, "_at", at)
 
     @classmethod
     def empty(cls, pages: int, rows: int, Hkv: int, block_table, *, dtype=torch.bfloat16, rope_base: float = 1e4):
@@ -696,8 +706,6 @@ def _tokens(t, cache, name):
     shape = t.shape
     if len(shape) != 3 or shape[2] != 64 or t.dtype is not cache.dtype or t.get_device() != cache.index:
         raise ValueError(f"{name} must be [tokens, heads, 64] of the cache's dtype, on its device")
-    if shape[0] * shape[1] > _MOST:
-        raise ValueError(f"{name}: tokens times heads must be below 2^31")
     token, head, last = t.stride()
     if shape[0] == 1:
         token = 0
@@ -761,12 +769,14 @@ def cache_append(cache: PagedCache, k, v, positions, *, seqs=None, slots=None, s
     k_at, v_at = _tokens(k, cache, "k"), _tokens(v, cache, "v")
     if v.shape != shape or shape[1] != cache.Hkv:
         raise ValueError("k and v must be [tokens, the cache's Hkv, 64]")
-    each = shape[:1]
+    each, N = shape[:1], shape[0]
+    if N > _MOST:
+        raise ValueError("tokens times heads must be below 2^31")
     p = _ints(positions, each, index, "positions")
     b = None if seqs is None else _ints(seqs, each, index, "seqs")
     at = None if slots is None else _ints(slots, each, index, "slots")
     _check_device(index)
-    rc = lib().fibattn_cache_append(cache._at, *k_at, *v_at, p, at, b, shape[0], _raw_stream(index))
+    rc = lib().fibattn_cache_append(cache._at, *k_at, *v_at, p, at, b, N, _raw_stream(index))
     if rc:
         _check(rc)
 
@@ -804,6 +814,8 @@ def tree_fwd(q, cache: PagedCache, alpha: float, offsets, W: int, positions, par
 def _attention(q, cache, alpha, offsets, W, positions, parents, slots, seqs, scale, dedup, round_offsets, out, lse):
     at, index, shape = _tokens(q, cache, "q"), cache.index, q.shape
     each, N, H = shape[:1], shape[0], shape[1]
+    if N * H > _MOST:
+        raise ValueError("tokens times heads must be below 2^31")
     p = _ints(positions, each, index, "positions")
     b = None if seqs is None else _ints(seqs, each, index, "seqs")
     _check_device(index)
