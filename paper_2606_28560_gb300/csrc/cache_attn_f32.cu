@@ -276,7 +276,8 @@ cudaError_t launch_attention_f32(const AttnArgs& args, cudaStream_t st) {
     AttnArgs a = args;
     // Query heads of a warp: they share the rows' look-up and loads, but few warps leave the GPU
     // waiting.  One token each, us: 256 tokens of 8 heads over 1 with 1, 2, 4, 8 heads a warp 5.6,
-    // 5.2, 5.9, 8.5; 1024 tokens of 8 over 2 with 1, 2, 4 heads 15.8, 11.2, 9.0.
+    // 5.2, 5.9, 8.5.  With 1, 2, 4 heads of 8 over 2: 1024 tokens 13.9, 10.5, 9.0; 4096 52.6, 40.5, 40.0;
+    // chunks 8 x 256 23.8, 18.2, 14.1; drafts 64 x 32 27.8, 20.1, 15.7.
     const int all = a.N * a.H;
     a.run = a.r.total > 64 || (a.r.total > 32 && a.G == 1) || all < 2048 ? 1 : std::min({a.G, kHeads, std::max(2, all / 2048)});
     const unsigned parts = (a.G + a.run - 1) / a.run;

@@ -7,10 +7,9 @@
 // A warp has one token and eight of its query heads: those of one key/value head, or
 // of several, as far as eight go.  Rows go 32 to a part, up to 64 at once: each lane
 // finds one of a part through the page table, for all heads; then m16n8k16 products
-// take them.  The eight heads
-// are rows 0-7 of the first operand and what their rounding to 16 bits left is rows
-// 8-15, so that q (two fp16 halves, 22 bits) and p (two bf16 halves, 16 bits) come
-// with the products' idle half and fp32 sums.  A product with the rows of one
+// take them.  The eight heads are rows 0-7 of the first operand and what their rounding
+// to 16 bits left is rows 8-15, so that q (two fp16 halves, 22 bits: fit_half) and p (two
+// bf16 halves, 16 bits) come with the products' idle half and fp32 sums.  A product with the rows of one
 // key/value head is right for its own query heads; the others' scores are not taken,
 // and their weights are 0 in its product with the values, so that all eight share one
 // set of sums, one softmax and one way out.
@@ -19,11 +18,11 @@
 // the values, whose sum runs over rows; neither copies nor loads meet in a bank.
 // Bound by memory where there are many sequences: 4096 single tokens of 8 heads 39 to
 // 42 us, 5.3 to 5.7 TB/s of rows of 128 bytes; by the chain of look-ups, copies and products of the 16
-// warps that an SM holds where rows come from L2 (8 chunks of 256 tokens 12.6 us) or where
-// there are few (one token 3.1 us).  Keys straight into registers and values through
-// a ring of two took 43.0, 12.1 and 3.1 us, and 164 instead of 140 us for 128 chunks; two
-// stages and 20 warps an SM 38.7, 12.9 and 3.2 at the best heads a warp for each; blocks
-// of four warps 1 to 2 % more for single tokens.
+// warps that an SM holds where rows come from L2 (8 chunks of 256 tokens 12.8 us) or where
+// there are few (one token 3.2 us).  Keys straight into registers and values through
+// a ring of two took 43.0, 12.1 and 3.1 us, and 164 us for 128 chunks where this way took
+// 140; two stages and 20 warps an SM 38.7, 12.9 and 3.2 at the best heads a warp for each;
+// blocks of four warps 1 to 2 % more for single tokens.
 #include <algorithm>
 
 #include "cache_rows.cuh"
@@ -349,9 +348,11 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
 cudaError_t launch_attention_mma(const AttnArgs& args, cudaStream_t st) {
     AttnArgs a = args;
     // Key/value heads of a warp, as far as its eight query heads go: the rows are looked up
-    // once for all, but few warps leave the GPU waiting.  Of 8, one token each, us: 256 tokens
-    // with 1, 2, 4 heads a warp 5.4, 4.8, 5.0; 512 tokens 8.7, 6.4, 6.1; 1024 tokens with 2, 4,
-    // 8 heads 12.6, 10.7, 10.6; 4096 tokens 44.2, 40.1, 39.2.
+    // once for all, but few warps leave the GPU waiting.  With 1, 2, 4, 8 heads a warp, us, of 8
+    // heads over 8: 256 single tokens 5.4, 4.8, 5.0; 512 8.7, 6.4, 6.1; 1024 16.5, 12.6, 11.1,
+    // 10.9; 4096 56.5, 45.1, 40.3, 39.7; chunks 8 x 64 8.7, 6.6, 6.2, 6.9, 8 x 256 25.9, 18.1, 14.3,
+    // 13.2; drafts 16 x 32 10.4, 7.3, 7.0, 7.7, 64 x 32 30.9, 21.2, 16.3, 13.8.  Of 8 over 2: 1024
+    // single tokens 5.5, 5.2, chunks 8 x 256 8.7, 6.7, drafts 64 x 32 10.2, 7.5.
     const int most = std::min(8 / std::min(a.G, 8), a.c.Hkv);
     a.run = a.r.total > 64 ? 1 : std::max(1, std::min(most, a.N * a.c.Hkv / 1024));
     const unsigned parts = (a.G + 7) / 8, runs = (a.c.Hkv + a.run - 1) / a.run;
@@ -359,7 +360,8 @@ cudaError_t launch_attention_mma(const AttnArgs& args, cudaStream_t st) {
     a.dRest = FastDiv::make(runs * parts);
     a.dParts = FastDiv::make(parts);
     // All of a query's rows at once as far as 64 go, 16 by 16: 4096 tokens of 35 rows (W = 16) 52.5 us
-    // with three halves, 59 with four, 96 part by part (which also keeps a warp at one head).
+    // with three halves, 59 with four (which keep 26 bytes a thread in memory), 96 part by part (which also
+    // keeps a warp at one head).
     const int halves = (a.r.total + 15) / 16;
     return halves <= 1 ? launch<1, false>(a, st) : halves == 2 ? launch<2, false>(a, st) : halves == 3 ? launch<3, false>(a, st)
          : halves == 4 ? launch<4, false>(a, st) : launch<4, true>(a, st);
