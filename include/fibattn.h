@@ -426,8 +426,8 @@ int fibattn_cache_append(const fibattn_cache* c, const void* k, long long k_toke
  * outputs that are not, of the heads that read it and of no others.  So does a key,
  * but for scores of -infinity, which count for nothing (where there are no others out
  * is NaN and lse -infinity): an infinite key gives those, or NaN, by the signs of q's
- * rotated values that meet it.  Limits of W, K and alpha as for fibattn_fwd;
- * 0 <= N, N * H < 2^31. */
+ * rotated values that meet it (NaN also for 0, in bf16 for what is below 2^-39 of the
+ * head's largest).  Limits of W, K and alpha as for fibattn_fwd; 0 <= N, N * H < 2^31. */
 int fibattn_cached_fwd(const fibattn_cache* c, const void* q, long long q_token_stride, long long q_head_stride,
                        void* out, float* lse, const int* positions, const int* seqs, int N, int H, int W,
                        float alpha, const float* offsets, int K, const fibattn_opts* opts, void* stream);
